@@ -21,8 +21,12 @@ STATUS_NAMES = {0: "DIFR_OK", -1: "DIFR_ERR_INVALID_ARG", -2: "DIFR_ERR_SHAPE", 
 EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_gm", "difr_score_ipt",
            "difr_score_both", "difr_score_gm_filtered", "difr_score_ipt_filtered", "difr_score_gm_static",
            "difr_admissible", "difr_exfiltratable_bits", "difr_detect", "difr_expand_seeds", "difr_logits", "difr_philox",
+           "difr_mx_codes_bytes", "difr_mx_scales_bytes", "difr_mx_quantize", "difr_mx_dequantize", "difr_rms_norm",
+           "difr_mx_logits",
            "difr_selftest_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
+DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
+DIFR_MX8, DIFR_MX4 = 8, 4
 
 
 class DifrError(RuntimeError):
@@ -49,6 +53,12 @@ class _CFilter(ctypes.Structure):
     _fields_ = [("top_k", ctypes.c_int32), ("top_p", ctypes.c_float), ("s", ctypes.c_int32),
                 ("top_k_rows", ctypes.c_void_p), ("top_p_rows", ctypes.c_void_p),
                 ("min_p", ctypes.c_float), ("min_p_rows", ctypes.c_void_p), ("any_size", ctypes.c_int32)]
+
+
+class _CNormOut(ctypes.Structure):
+    _fields_ = [("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64), ("h", ctypes.c_void_p),
+                ("ldh", ctypes.c_int64), ("mx_format", ctypes.c_int32), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
 
 
 _lib = None
@@ -104,6 +114,19 @@ def lib() -> ctypes.CDLL:
         L.difr_status_string.restype = ctypes.c_char_p
         L.difr_status_string.argtypes = [ctypes.c_int]
         L.difr_version.restype = ctypes.c_int
+        v, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+        L.difr_mx_codes_bytes.restype = ctypes.c_size_t
+        L.difr_mx_codes_bytes.argtypes = [i32, i64, i64]
+        L.difr_mx_scales_bytes.restype = ctypes.c_size_t
+        L.difr_mx_scales_bytes.argtypes = [i64, i64]
+        L.difr_mx_quantize.restype = ctypes.c_int
+        L.difr_mx_quantize.argtypes = [v, i32, i64, i64, i64, i32, v, v, v]
+        L.difr_mx_dequantize.restype = ctypes.c_int
+        L.difr_mx_dequantize.argtypes = [v, v, i32, i64, i64, v, i32, i64, v]
+        L.difr_rms_norm.restype = ctypes.c_int
+        L.difr_rms_norm.argtypes = [v, i64, v, i64, v, i32, i64, i64, ctypes.c_float, ctypes.POINTER(_CNormOut), v]
+        L.difr_mx_logits.restype = ctypes.c_int
+        L.difr_mx_logits.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, v, v]
         _lib = L
     return _lib
 
@@ -364,3 +387,178 @@ def difr_philox(ctr, key, out, stream=None):
     if rc != DIFR_OK:
         raise DifrError(rc, "difr_philox")
     return out
+
+
+# ------------------------------------------------- around the LM head: the final norm, heads in 8 or 4 bits
+def difr_mx_codes_bytes(format: int, rows: int, d: int) -> int:
+    return int(lib().difr_mx_codes_bytes(format, rows, d))
+
+
+def difr_mx_scales_bytes(rows: int, d: int) -> int:
+    return int(lib().difr_mx_scales_bytes(rows, d))
+
+
+@dataclass
+class MxTensor:
+    """A microscaled tensor of `rows` x `d` values (layout in include/difr.h)."""
+    codes: "object"   # uint8 [rows, pitch bytes]
+    scales: "object"  # uint8 [difr_mx_scales_bytes(rows, d)]
+    format: int       # DIFR_MX8 or DIFR_MX4
+    rows: int
+    d: int
+
+    @staticmethod
+    def allocate(rows: int, d: int, format: int, device="cuda"):
+        import torch
+
+        if rows > 0 and difr_mx_codes_bytes(format, rows, d) == 0:
+            raise ValueError(f"no microscaled tensor of {rows} x {d} values in format {format}")
+        # (the bytes of rows behind the last are nobody's: zeros, so that two equal tensors have equal buffers)
+        return MxTensor(torch.empty(rows, (d + 31) // 32 * 4 * format, dtype=torch.uint8, device=device),
+                        torch.zeros(difr_mx_scales_bytes(rows, d), dtype=torch.uint8, device=device), format, rows, d)
+
+
+@dataclass
+class NormOut:
+    """Output tensors of difr_rms_norm (mirrors `difr_norm_out`); None: not wanted."""
+    h: "object" = None         # bf16 [T, d]
+    residual: "object" = None  # [T, d] of x's type
+    mx: MxTensor = None
+
+
+def _matrix(t, name, dtypes, shape=None, device=None):
+    """A CUDA matrix whose rows are contiguous; returns (C dtype, row stride)."""
+    import torch
+
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise TypeError(f"{name} must be a CUDA matrix")
+    code = {torch.bfloat16: DIFR_BF16, torch.float16: DIFR_F16, torch.float32: DIFR_F32}.get(t.dtype)
+    if code not in dtypes:
+        raise TypeError(f"{name}: {t.dtype} is not supported here")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise TypeError(f"{name} is on {t.device}, not on {device}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise TypeError(f"{name}: the rows must be contiguous and must not overlap")
+    return code, ld
+
+
+def _check_mx(mx, name, device):
+    import torch
+
+    if not isinstance(mx, MxTensor) or mx.format not in (DIFR_MX8, DIFR_MX4):
+        raise TypeError(f"{name} must be an MxTensor of 8 or 4 bits")
+    for t, what, n in ((mx.codes, "codes", mx.rows * ((mx.d + 31) // 32 * 4 * mx.format)),
+                       (mx.scales, "scales", (mx.rows + 127) // 128 * ((mx.d + 127) // 128) * 512)):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != n:
+            raise TypeError(f"{name}.{what} must be {n} contiguous bytes (uint8)")
+        if t.device != device:
+            raise TypeError(f"{name}.{what} is on {t.device}, not on {device}")
+
+
+class _on_device:
+    """Makes a tensor's device current for a call; the stream is the given one or that device's current one."""
+
+    def __init__(self, device, stream):
+        import torch
+
+        if stream is not None and stream.device != device:
+            raise TypeError(f"the stream is on {stream.device}, the tensors on {device}")
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        self.stream = stream
+        self.device = device
+
+    def __enter__(self):
+        import torch
+
+        if self.guard is not None:
+            self.guard.__enter__()
+        s = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
+        return ctypes.c_void_p(s.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def difr_mx_quantize(x, out: MxTensor, stream=None) -> MxTensor:
+    """Microscaled codes and scales of a matrix (bf16, fp16 or fp32); see include/difr.h."""
+    dtype, ld = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
+    _check_mx(out, "out", x.device)
+    if (out.rows, out.d) != tuple(x.shape):
+        raise TypeError(f"out is {out.rows} x {out.d}, x {tuple(x.shape)}")
+    with _on_device(x.device, stream) as s:
+        rc = lib().difr_mx_quantize(_ptr(x), dtype, out.rows, out.d, ld, out.format, _ptr(out.codes), _ptr(out.scales), s)
+    if rc != DIFR_OK:
+        raise DifrError(rc, "difr_mx_quantize")
+    return out
+
+
+def difr_mx_dequantize(mx: MxTensor, out, stream=None):
+    """The values of a microscaled tensor, as bf16 (what the scoring calls take) or fp32."""
+    dtype, ld = _matrix(out, "out", (DIFR_BF16, DIFR_F32))
+    _check_mx(mx, "mx", out.device)
+    if (mx.rows, mx.d) != tuple(out.shape):
+        raise TypeError(f"out is {tuple(out.shape)}, the tensor {mx.rows} x {mx.d}")
+    with _on_device(out.device, stream) as s:
+        rc = lib().difr_mx_dequantize(_ptr(mx.codes), _ptr(mx.scales), mx.format, mx.rows, mx.d, _ptr(out), dtype, ld, s)
+    if rc != DIFR_OK:
+        raise DifrError(rc, "difr_mx_dequantize")
+    return out
+
+
+def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> NormOut:
+    """Final root-mean-square norm of x (+ residual); `out.h` feeds the scoring calls, `out.mx` difr_mx_logits."""
+    import torch
+
+    dtype, ldx = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
+    shape, device = x.shape, x.device
+    if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.device != device
+            or tuple(weight.shape) != (shape[1],) or not weight.is_contiguous()):
+        raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {device}")
+    c = _CNormOut()
+    ldr = 0
+    if residual is not None:
+        ldr = _matrix(residual, "residual", (dtype,), shape, device)[1]
+    if out.residual is not None:
+        c.ld_residual = _matrix(out.residual, "out.residual", (dtype,), shape, device)[1]
+        c.residual = out.residual.data_ptr()
+    if out.h is not None:
+        c.ldh = _matrix(out.h, "out.h", (DIFR_BF16,), shape, device)[1]
+        c.h = out.h.data_ptr()
+    if out.mx is not None:
+        _check_mx(out.mx, "out.mx", device)
+        if (out.mx.rows, out.mx.d) != tuple(shape):
+            raise TypeError(f"out.mx is {out.mx.rows} x {out.mx.d}, x {tuple(shape)}")
+        c.mx_format, c.codes, c.scales = out.mx.format, out.mx.codes.data_ptr(), out.mx.scales.data_ptr()
+    with _on_device(device, stream) as s:
+        rc = lib().difr_rms_norm(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), dtype, shape[0], shape[1], float(eps),
+                                 ctypes.byref(c), s)
+    if rc != DIFR_OK:
+        raise DifrError(rc, "difr_rms_norm")
+    return out
+
+
+def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=None):
+    """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format."""
+    import torch
+
+    dtype, ld = _matrix(logits, "logits", (DIFR_F32, DIFR_BF16))
+    device = logits.device
+    _check_mx(h, "h", device)
+    _check_mx(W, "W", device)
+    if h.format != W.format or h.d != W.d:
+        raise TypeError(f"h has {h.d} values of {h.format} bits per row, W {W.d} of {W.format}")
+    if tuple(logits.shape) != (h.rows, W.rows):
+        raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
+    if device_status is not None:
+        _check(device_status, torch.int32, (1,), "device_status")
+    with _on_device(device, stream) as s:
+        rc = lib().difr_mx_logits(_ptr(h.codes), _ptr(h.scales), _ptr(W.codes), _ptr(W.scales), h.format, h.rows, h.d,
+                                  W.rows, _ptr(logits), dtype, ld, _ptr(device_status), s)
+    if rc != DIFR_OK:
+        raise DifrError(rc, "difr_mx_logits")
+    return logits

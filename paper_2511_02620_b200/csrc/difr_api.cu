@@ -12,28 +12,13 @@
 #include <vector>
 
 #include "../../include/difr.h"
+#include "difr_host.h"
 #include "difr_kernels.h"
 #include "difr_plan.h"
 
 namespace {
 
 using namespace difr;
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn() {
-  static EncodeTiledFn fn = nullptr;
-  if (fn == nullptr) {
-    void* sym = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &q) == cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(sym);
-  }
-  return fn;
-}
 
 // bf16 [rows, cols] row-major, box = 64 columns (128 bytes, 128-byte swizzle) x box_rows rows.
 bool encode_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows) {
@@ -134,8 +119,6 @@ K1Params k1_params(const Plan& pl, int64_t T, int64_t d, int64_t V, float temper
 }
 
 int k1_grid(const Plan& pl, int pairs) { return 2 * (pl.n_units < pairs ? pl.n_units : pairs); }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // kind: 0 Token-DiFR, 1 Token-IPT-DiFR, 2 both.
 difr_status score_common(int ipt, const void* h, const void* W, const int32_t* tokens, const uint64_t* seeds,
@@ -739,6 +722,6 @@ const char* difr_status_string(difr_status status) {
   return "unknown status";
 }
 
-int difr_version(void) { return 221; }
+int difr_version(void) { return 300; }
 
 }  // extern "C"

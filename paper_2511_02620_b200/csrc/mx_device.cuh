@@ -1,0 +1,258 @@
+// Device-side building blocks of the microscaled formats and of the block-scaled tensor-core product.
+//
+// A microscaled tensor [rows, d] keeps blocks of 32 values along a row: every value is a code of an 8-bit (e4m3,
+// largest 448 = 1.75 * 2^8) or 4-bit (e2m1, largest 6 = 1.5 * 2^2) floating-point format, every block has one
+// power-of-two scale, stored as its exponent + 127 in a byte (255: the block held a NaN or an infinity).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "difr_device.cuh"
+
+namespace difr {
+
+constexpr int kMx8 = 8, kMx4 = 4;  // bits per code; the values of difr_mx_format
+constexpr int kMxBlock = 32;
+constexpr int kSfWordRows = 128, kSfWordBytes = 512;  // a scale word: four scales of each of 128 rows
+
+__host__ __device__ constexpr int mx_emax(int fmt) { return fmt == kMx8 ? 8 : 2; }
+__host__ __device__ __forceinline__ int64_t mx_blocks(int64_t d) { return (d + kMxBlock - 1) / kMxBlock; }
+__host__ __device__ __forceinline__ int64_t mx_words(int64_t d) { return (mx_blocks(d) + 3) / 4; }
+__host__ __device__ __forceinline__ int64_t mx_pitch_bytes(int fmt, int64_t d) {
+  return mx_blocks(d) * kMxBlock * fmt / 8;
+}
+// Byte offset of the four scales of blocks 4 w .. 4 w + 3 of a row: what the tensor core reads as a 128 x 4 block is
+// 512 consecutive bytes, 16 per lane (row % 32), 4 of them per quarter (row / 32) of the 128 rows.
+__device__ __forceinline__ int64_t mx_scale_offset(int64_t row, int64_t w, int64_t words) {
+  return ((row >> 7) * words + w) * kSfWordBytes + (row & 31) * 16 + ((row >> 5) & 3) * 4;
+}
+
+// Scale byte of a block from the bits of its largest magnitude: exponent floor(log2 amax) - emax, at least -127.  The
+// exponent field of an fp32 is floor(log2) + 127 for normal numbers; zero and subnormal maxima end at the smallest
+// scale, where their codes are still exact or round to zero.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits) {
+  const int e = (int)(amax_bits >> 23);
+  return e == 255 ? 255u : (uint32_t)max(e - mx_emax(FMT), 0);
+}
+// 2^(127 - byte), what a value is multiplied by before it is rounded: exact, since it is a power of two.  0 for the
+// blocks that are not numbers: their codes are then written as 0 (0 * infinity is NaN, so they are cleared apart).
+__device__ __forceinline__ float mx_inverse_scale(uint32_t byte) {
+  return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
+}
+// 2^(byte - 127); NaN for 255.
+__device__ __forceinline__ float mx_scale_value(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u)
+                                                                 : __uint_as_float(byte << 23);
+}
+
+// Rounding to the formats: nearest, ties to even, magnitudes above the largest become the largest.
+__device__ __forceinline__ uint32_t cvt_e4m3x4(float a0, float a1, float a2, float a3) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(lo) : "f"(a0), "f"(a1));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(hi) : "f"(a2), "f"(a3));
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
+__device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&a)[8]) {
+  uint32_t r;
+  asm("{\n"
+      ".reg .b8 b0, b1, b2, b3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+      "mov.b32 %0, {b0, b1, b2, b3};\n"
+      "}\n"
+      : "=r"(r)
+      : "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]), "f"(a[4]), "f"(a[5]), "f"(a[6]), "f"(a[7]));
+  return r;
+}
+// Codes back to values (exact in fp16: e4m3 and e2m1 are subsets of it).
+__device__ __forceinline__ float2 half2_bits_to_float2(uint32_t h2) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&h2));
+}
+__device__ __forceinline__ float2 cvt_e4m3x2_to_float2(uint32_t two_codes) {
+  uint32_t h2;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"((uint16_t)two_codes));
+  return half2_bits_to_float2(h2);
+}
+__device__ __forceinline__ float2 cvt_e2m1x2_to_float2(uint32_t two_codes) {
+  uint32_t h2;
+  asm("{\n"
+      ".reg .b8 b;\n"
+      "cvt.u8.u32 b, %1;\n"
+      "cvt.rn.f16x2.e2m1x2 %0, b;\n"
+      "}\n"
+      : "=r"(h2)
+      : "r"(two_codes));
+  return half2_bits_to_float2(h2);
+}
+
+// Quantises 8 consecutive values held by each lane.  A block of 32 is four neighbouring lanes (lane % 4 == 0 starts
+// one), a scale word (four blocks) sixteen; every lane of the warp takes part, lanes past the row hold zeros.  `codes`
+// receives 8 codes (4 or 8 bytes), the returned word is the four scale bytes of the lane's sixteen.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_quantize8(const float (&v)[8], bool past_end, uint32_t (&codes)[2]) {
+  // magnitudes compare like their bits, and a NaN's bits are above every number's
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+  const uint32_t byte = past_end ? 0u : mx_scale_byte<FMT>(m);
+  const float inv = mx_inverse_scale(byte);
+  float q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = byte == 255u ? 0.f : v[i] * inv;
+  if (FMT == kMx8) {
+    codes[0] = cvt_e4m3x4(q[0], q[1], q[2], q[3]);
+    codes[1] = cvt_e4m3x4(q[4], q[5], q[6], q[7]);
+  } else {
+    codes[0] = cvt_e2m1x8(q);
+    codes[1] = 0;
+  }
+  uint32_t word = byte << (((threadIdx.x >> 2) & 3) * 8);
+  word |= __shfl_xor_sync(0xffffffffu, word, 4);
+  word |= __shfl_xor_sync(0xffffffffu, word, 8);
+  return word;
+}
+
+// ---------------------------------------------------------------- element types of inputs and outputs
+template <typename X>
+__device__ __forceinline__ float to_float(X x);
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <>
+__device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
+template <>
+__device__ __forceinline__ float to_float<float>(float x) { return x; }
+template <typename X>
+__device__ __forceinline__ X from_float(float x);
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+
+// Elements e0 .. e0 + 7 of a row of d, zeros past its end.  `vec`: the row starts on a 16-byte boundary.  (Plain loads,
+// not the read-only path: a call may write its result over its input.)
+template <typename X>
+__device__ __forceinline__ void load8(const X* row, int e0, int d, bool vec, float (&v)[8]) {
+  if (vec && e0 + 8 <= d) {
+    __align__(16) X raw[8];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(X) * 8 / 16; ++i)
+      reinterpret_cast<uint4*>(raw)[i] = reinterpret_cast<const uint4*>(row + e0)[i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_float<X>(raw[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = e0 + i < d ? to_float<X>(row[e0 + i]) : 0.f;
+  }
+}
+template <typename X>
+__device__ __forceinline__ void store8(X* row, int e0, int d, bool vec, const float (&v)[8]) {
+  if (vec && e0 + 8 <= d) {
+    __align__(16) X raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = from_float<X>(v[i]);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(X) * 8 / 16; ++i)
+      reinterpret_cast<uint4*>(row + e0)[i] = reinterpret_cast<const uint4*>(raw)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (e0 + i < d) row[e0 + i] = from_float<X>(v[i]);
+  }
+}
+
+// ------------------------------------------------------- PTX: TMA and tcgen05 of the block-scaled product
+// Three-dimensional form of tma_load_2d_pair.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tmap, int x, int y, int z,
+                                                 uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint "
+      "[%0], [%1, {%2, %3, %4}], [%5], %6;"
+      ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
+      : "memory");
+}
+
+// Copies one scale word (32 lanes x 16 bytes, in each CTA of the pair from its own shared memory) to four TMEM
+// columns, repeated in all four lane quarters.  Issued by the thread that issues the MMAs; a following MMA sees it.
+__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t sdesc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+// Shared-memory descriptor of a scale word: no swizzle, 8 x 16-byte core matrices 128 bytes apart.
+__device__ __forceinline__ uint64_t umma_desc_scales(uint32_t smem_addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(128 >> 4) << 16;
+  d |= (uint64_t)(128 >> 4) << 32;
+  d |= (uint64_t)1 << 46;  // descriptor version of sm_100
+  return d;
+}
+
+// Instruction descriptor of the block-scaled kinds: fp32 accumulator, both operands K-major, power-of-two scales.
+// The operands' type field is 0 for e4m3 among the 8-bit formats and 1 for e2m1 of the 4-bit kind.
+template <int FMT>
+__host__ __device__ constexpr uint32_t umma_idesc_mx(int M, int N) {
+  return (FMT == kMx8 ? 0u : ((1u << 7) | (1u << 10))) | ((uint32_t)(N >> 3) << 17) | (1u << 23) |
+         ((uint32_t)(M >> 4) << 24);
+}
+// Which byte of the scales' 32-bit TMEM cells the MMA starts with, for both operands.
+__host__ __device__ constexpr uint32_t umma_idesc_scale_byte(uint32_t b) { return (b << 4) | (b << 29); }
+
+// D[tmem] (+)= (A * scales_a) (B * scales_b)^T, 256 x N x 32 bytes of codes along K, issued by one thread of the
+// pair's first CTA.  Each CTA's TMEM holds the scales of its own 128 rows of A and of all N rows of B.
+template <int FMT>
+__device__ __forceinline__ void umma_mx_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                             uint32_t tmem_sa, uint32_t tmem_sb, uint32_t accumulate) {
+  if (FMT == kMx8) {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n"
+        "}\n"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        : "memory");
+  } else {
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n"
+        "}\n"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(tmem_sa), "r"(tmem_sb)
+        : "memory");
+  }
+}
+
+// 32 lanes x 32 consecutive fp32 columns, and the wait for it (see tmem_ld_32x16 and tmem_ld_wait).
+__device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]),
+                 "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]),
+                 "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
+
+}  // namespace difr

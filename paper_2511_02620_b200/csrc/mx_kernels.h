@@ -1,0 +1,60 @@
+// Parameter blocks and launchers of the norm, the microscaled formats and their product (host-visible part).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace difr {
+
+// Element types of inputs and outputs: the values of difr_dtype.
+constexpr int kBf16 = 0, kF16 = 1, kF32 = 2;
+
+struct NormParams {
+  const void* x;         // [T][ldx]
+  const void* residual;  // [T][ld_residual], nullable
+  const void* weight;    // [d]
+  void* residual_out;    // [T][ld_residual_out], nullable: x + residual, rounded to the inputs' type
+  void* h;               // bf16 [T][ldh], nullable
+  unsigned char* codes;  // nullable: microscaled output
+  unsigned char* scales;
+  int64_t T, ldx, ld_residual, ld_residual_out, ldh;
+  int d, fmt;
+  float eps;
+  int threads_per_row, rows_per_cta;
+  bool vec_x, vec_residual, vec_residual_out, vec_h, vec_weight;  // rows start on 16-byte boundaries
+};
+constexpr int kNormMaxD = 32768;
+cudaError_t launch_rms_norm(const NormParams& p, int dtype, cudaStream_t stream);
+
+struct MxConvertParams {
+  const void* in;        // quantise: [rows][ld]
+  void* out;             // dequantise: [rows][ld]
+  unsigned char* codes;
+  unsigned char* scales;
+  int64_t rows, ld;
+  int d, fmt;
+  bool vec;              // rows of `in` / `out` start on 16-byte boundaries
+};
+cudaError_t launch_mx_quantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
+cudaError_t launch_mx_dequantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
+
+struct MxLogitsParams {
+  void* logits;          // [T][ld]
+  int64_t ld;
+  int32_t* device_status;
+  int T, V;
+  int k_steps;           // 128-byte slices of a row of codes
+  int last_mmas;         // MMAs (32 bytes of codes each) of the last slice
+  int n_vt, n_tt;        // vocabulary tiles of 256 ids, token tiles
+  int group;             // token tiles per raster group
+  int n_tiles;
+  bool pack_pairs;       // bf16 logits: two neighbouring ids leave in one 4-byte store
+};
+constexpr int kMxPairM = 256;  // vocabulary ids per tile of a CTA pair
+// `tokens_per_tile`: 16, 32, 64, 128 or 256; maps: codes of W and h, scales of W and h.
+cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
+                             const CUtensorMap& sw, const CUtensorMap& sh, const MxLogitsParams& p, int grid,
+                             cudaStream_t stream);
+int mx_logits_max_resident_pairs();
+
+}  // namespace difr
