@@ -426,74 +426,82 @@ class NormOut:
     mx: MxTensor = None
 
 
+_DTYPES = {}  # torch dtype -> difr_dtype
+
+
+def _dtypes():
+    if not _DTYPES:
+        import torch
+
+        _DTYPES.update({torch.bfloat16: DIFR_BF16, torch.float16: DIFR_F16, torch.float32: DIFR_F32})
+    return _DTYPES
+
+
 def _matrix(t, name, dtypes, shape=None, device=None):
     """A CUDA matrix whose rows are contiguous; returns (C dtype, row stride)."""
-    import torch
-
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+    if getattr(t, "is_cuda", None) is not True or t.dim() != 2:
         raise TypeError(f"{name} must be a CUDA matrix")
-    code = {torch.bfloat16: DIFR_BF16, torch.float16: DIFR_F16, torch.float32: DIFR_F32}.get(t.dtype)
+    code = _dtypes().get(t.dtype)
     if code not in dtypes:
         raise TypeError(f"{name}: {t.dtype} is not supported here")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise TypeError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
     if device is not None and t.device != device:
         raise TypeError(f"{name} is on {t.device}, not on {device}")
     rows, cols = t.shape
-    ld = t.stride(0) if rows > 1 else max(t.stride(0), cols)
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+    ld, step = t.stride()
+    if rows <= 1 and ld < cols:
+        ld = cols
+    if (step != 1 and cols > 1) or ld < cols:
         raise TypeError(f"{name}: the rows must be contiguous and must not overlap")
     return code, ld
 
 
 def _check_mx(mx, name, device):
-    import torch
-
     if not isinstance(mx, MxTensor) or mx.format not in (DIFR_MX8, DIFR_MX4):
         raise TypeError(f"{name} must be an MxTensor of 8 or 4 bits")
-    for t, what, n in ((mx.codes, "codes", mx.rows * ((mx.d + 31) // 32 * 4 * mx.format)),
-                       (mx.scales, "scales", (mx.rows + 127) // 128 * ((mx.d + 127) // 128) * 512)):
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous() or t.numel() != n:
-            raise TypeError(f"{name}.{what} must be {n} contiguous bytes (uint8)")
-        if t.device != device:
-            raise TypeError(f"{name}.{what} is on {t.device}, not on {device}")
+    _check_bytes(mx.codes, mx.rows * ((mx.d + 31) // 32 * 4 * mx.format), name, "codes", device)
+    _check_bytes(mx.scales, (mx.rows + 127) // 128 * ((mx.d + 127) // 128) * 512, name, "scales", device)
 
 
-class _on_device:
-    """Makes a tensor's device current for a call; the stream is the given one or that device's current one."""
+def _check_bytes(t, n, name, what, device):
+    import torch
 
-    def __init__(self, device, stream):
-        import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous():
+        raise TypeError(f"{name}.{what} must be {n} contiguous bytes (uint8)")
+    if t.device != device:
+        raise TypeError(f"{name}.{what} is on {t.device}, not on {device}")
 
-        if stream is not None and stream.device != device:
-            raise TypeError(f"the stream is on {stream.device}, the tensors on {device}")
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-        self.stream = stream
-        self.device = device
 
-    def __enter__(self):
-        import torch
+def _call(name, device, stream, *args):
+    """Calls an entry point with `device` current, on the given stream or that device's current one."""
+    import torch
 
-        if self.guard is not None:
-            self.guard.__enter__()
-        s = torch.cuda.current_stream(self.device) if self.stream is None else self.stream
-        return ctypes.c_void_p(s.cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+    if stream is None:
+        # (the handle alone: building a torch.cuda.Stream costs 2 us a call)
+        raw = torch._C._cuda_getCurrentRawStream(device.index)
+    elif stream.device != device:
+        raise TypeError(f"the stream is on {stream.device}, the tensors on {device}")
+    else:
+        raw = stream.cuda_stream
+    fn = getattr(_lib or lib(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, raw)
+    if rc != DIFR_OK:
+        raise DifrError(rc, name)
 
 
 def difr_mx_quantize(x, out: MxTensor, stream=None) -> MxTensor:
     """Microscaled codes and scales of a matrix (bf16, fp16 or fp32); see include/difr.h."""
     dtype, ld = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
     _check_mx(out, "out", x.device)
-    if (out.rows, out.d) != tuple(x.shape):
+    if (out.rows, out.d) != x.shape:
         raise TypeError(f"out is {out.rows} x {out.d}, x {tuple(x.shape)}")
-    with _on_device(x.device, stream) as s:
-        rc = lib().difr_mx_quantize(_ptr(x), dtype, out.rows, out.d, ld, out.format, _ptr(out.codes), _ptr(out.scales), s)
-    if rc != DIFR_OK:
-        raise DifrError(rc, "difr_mx_quantize")
+    _call("difr_mx_quantize", x.device, stream, x.data_ptr(), dtype, out.rows, out.d, ld, out.format,
+          out.codes.data_ptr(), out.scales.data_ptr())
     return out
 
 
@@ -501,12 +509,10 @@ def difr_mx_dequantize(mx: MxTensor, out, stream=None):
     """The values of a microscaled tensor, as bf16 (what the scoring calls take) or fp32."""
     dtype, ld = _matrix(out, "out", (DIFR_BF16, DIFR_F32))
     _check_mx(mx, "mx", out.device)
-    if (mx.rows, mx.d) != tuple(out.shape):
+    if (mx.rows, mx.d) != out.shape:
         raise TypeError(f"out is {tuple(out.shape)}, the tensor {mx.rows} x {mx.d}")
-    with _on_device(out.device, stream) as s:
-        rc = lib().difr_mx_dequantize(_ptr(mx.codes), _ptr(mx.scales), mx.format, mx.rows, mx.d, _ptr(out), dtype, ld, s)
-    if rc != DIFR_OK:
-        raise DifrError(rc, "difr_mx_dequantize")
+    _call("difr_mx_dequantize", out.device, stream, mx.codes.data_ptr(), mx.scales.data_ptr(), mx.format, mx.rows, mx.d,
+          out.data_ptr(), dtype, ld)
     return out
 
 
@@ -517,7 +523,7 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     dtype, ldx = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
     shape, device = x.shape, x.device
     if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.device != device
-            or tuple(weight.shape) != (shape[1],) or not weight.is_contiguous()):
+            or weight.shape != shape[1:] or not weight.is_contiguous()):
         raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {device}")
     c = _CNormOut()
     ldr = 0
@@ -531,14 +537,11 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
         c.h = out.h.data_ptr()
     if out.mx is not None:
         _check_mx(out.mx, "out.mx", device)
-        if (out.mx.rows, out.mx.d) != tuple(shape):
+        if (out.mx.rows, out.mx.d) != shape:
             raise TypeError(f"out.mx is {out.mx.rows} x {out.mx.d}, x {tuple(shape)}")
         c.mx_format, c.codes, c.scales = out.mx.format, out.mx.codes.data_ptr(), out.mx.scales.data_ptr()
-    with _on_device(device, stream) as s:
-        rc = lib().difr_rms_norm(_ptr(x), ldx, _ptr(residual), ldr, _ptr(weight), dtype, shape[0], shape[1], float(eps),
-                                 ctypes.byref(c), s)
-    if rc != DIFR_OK:
-        raise DifrError(rc, "difr_rms_norm")
+    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+          weight.data_ptr(), dtype, shape[0], shape[1], eps, ctypes.byref(c))
     return out
 
 
@@ -552,13 +555,13 @@ def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=
     _check_mx(W, "W", device)
     if h.format != W.format or h.d != W.d:
         raise TypeError(f"h has {h.d} values of {h.format} bits per row, W {W.d} of {W.format}")
-    if tuple(logits.shape) != (h.rows, W.rows):
+    if logits.shape != (h.rows, W.rows):
         raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
     if device_status is not None:
         _check(device_status, torch.int32, (1,), "device_status")
-    with _on_device(device, stream) as s:
-        rc = lib().difr_mx_logits(_ptr(h.codes), _ptr(h.scales), _ptr(W.codes), _ptr(W.scales), h.format, h.rows, h.d,
-                                  W.rows, _ptr(logits), dtype, ld, _ptr(device_status), s)
-    if rc != DIFR_OK:
-        raise DifrError(rc, "difr_mx_logits")
+        if device_status.device != device:
+            raise TypeError(f"device_status is on {device_status.device}, not on {device}")
+    _call("difr_mx_logits", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
+          W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld,
+          None if device_status is None else device_status.data_ptr())
     return logits

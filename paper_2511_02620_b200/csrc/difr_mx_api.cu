@@ -54,6 +54,15 @@ difr_status device_pairs(int* pairs) {
   return DIFR_OK;
 }
 
+int common_divisor(int a, int b) {
+  while (b != 0) {
+    const int r = a % b;
+    a = b;
+    b = r;
+  }
+  return a;
+}
+
 // Codes of a microscaled tensor as bytes: box of 128 bytes (128-byte swizzle) x box_rows rows.
 bool codes_tmap(CUtensorMap* map, const void* base, int fmt, int64_t rows, int64_t d, int box_rows) {
   EncodeTiledFn fn = encode_tiled_fn();
@@ -80,6 +89,19 @@ bool scales_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t d, in
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The logits [T, V] as the epilogue stores them: pieces of 128 ids x some tokens.
+bool logits_tmap(CUtensorMap* map, void* base, int32_t dtype, int64_t T, int64_t V, int64_t ld) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)V, (cuuint64_t)T};
+  const cuuint64_t strides[1] = {(cuuint64_t)(ld * elem_bytes(dtype))};
+  const cuuint32_t box[2] = {128, (cuuint32_t)mx_out_tokens(elem_bytes(dtype))};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, dtype == DIFR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims,
+            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool mx_supported(int64_t rows, int64_t d) { return rows <= kMaxRows && d <= kMaxD; }
@@ -119,7 +141,7 @@ difr_status difr_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
   MxConvertParams p;
   memset(&p, 0, sizeof p);
   p.in = x; p.codes = static_cast<unsigned char*>(codes); p.scales = static_cast<unsigned char*>(scales);
-  p.rows = rows; p.ld = ldx; p.d = (int)d; p.fmt = format; p.vec = vector_rows(x, ldx, dtype);
+  p.rows = rows; p.ld = ldx; p.d = (int)d; p.fmt = format; p.vec = d % 8 == 0 && vector_rows(x, ldx, dtype);
   return launch_mx_quantize(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
 }
 
@@ -137,7 +159,7 @@ difr_status difr_mx_dequantize(const void* codes, const void* scales, int32_t fo
   p.out = out;
   p.codes = static_cast<unsigned char*>(const_cast<void*>(codes));
   p.scales = static_cast<unsigned char*>(const_cast<void*>(scales));
-  p.rows = rows; p.ld = ldo; p.d = (int)d; p.fmt = format; p.vec = vector_rows(out, ldo, dtype);
+  p.rows = rows; p.ld = ldo; p.d = (int)d; p.fmt = format; p.vec = d % 8 == 0 && vector_rows(out, ldo, dtype);
   return launch_mx_dequantize(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK
                                                                                               : DIFR_ERR_CUDA;
 }
@@ -172,11 +194,10 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
   p.codes = static_cast<unsigned char*>(out->codes); p.scales = static_cast<unsigned char*>(out->scales);
   p.T = T; p.ldx = ldx; p.ld_residual = ld_residual; p.ld_residual_out = out->ld_residual; p.ldh = out->ldh;
   p.d = (int)d; p.fmt = out->mx_format; p.eps = eps;
-  p.vec_x = vector_rows(x, ldx, dtype);
-  p.vec_residual = residual && vector_rows(residual, ld_residual, dtype);
-  p.vec_residual_out = out->residual && vector_rows(out->residual, out->ld_residual, dtype);
-  p.vec_h = out->h && vector_rows(out->h, out->ldh, DIFR_BF16);
-  p.vec_weight = aligned16(weight);
+  p.vec = d % 8 == 0 && vector_rows(x, ldx, dtype) && aligned16(weight) &&
+          (!residual || vector_rows(residual, ld_residual, dtype)) &&
+          (!out->residual || vector_rows(out->residual, out->ld_residual, dtype)) &&
+          (!out->h || vector_rows(out->h, out->ldh, DIFR_BF16));
   return launch_rms_norm(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
 }
 
@@ -206,7 +227,10 @@ difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void
   p.T = (int)T; p.V = (int)V;
   p.k_steps = (int)((pitch + 127) / 128);
   p.last_mmas = (int)((pitch - (int64_t)(p.k_steps - 1) * 128 + 31) / 32);
-  p.n_vt = (int)n_vt; p.n_tt = (int)n_tt; p.n_tiles = (int)(n_vt * n_tt);
+  p.n_vt = (int)n_vt; p.n_tt = (int)n_tt;
+  p.n_tiles = (int)(n_vt * n_tt);
+  // the last token tile is only as wide as its tokens (in steps of 16, what the MMA takes)
+  p.last_tokens = (int)((T - (n_tt - 1) * bn + 15) / 16 * 16);
   // tokens of a raster group: about 32 MB of codes, a quarter of L2, so that they stay there while W passes
   const int64_t per_tile = (int64_t)bn * pitch;
   int64_t group = ((int64_t)32 << 20) / per_tile;
@@ -214,13 +238,22 @@ difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void
   if (group > n_tt) group = n_tt;
   p.group = (int)group;
   p.pack_pairs = dtype == DIFR_BF16 && ld % 2 == 0 && aligned_to(logits, 4);
+  p.tile_stores = bn == 256 && vector_rows(logits, ld, dtype) && ld <= ((int64_t)1 << 36);
   const int words = format == DIFR_MX8 ? 1 : 2;
-  CUtensorMap tw, th, tsw, tsh;
+  CUtensorMap tw, th, th_last, tsw, tsh;
   if (!codes_tmap(&tw, W_codes, format, V, d, 128) || !codes_tmap(&th, h_codes, format, T, d, bn / 2) ||
+      !codes_tmap(&th_last, h_codes, format, T, d, p.last_tokens / 2) ||
       !scales_tmap(&tsw, W_scales, V, d, words, 1) || !scales_tmap(&tsh, h_scales, T, d, words, bn > 128 ? 2 : 1))
     return DIFR_ERR_CUDA;
-  const int grid = 2 * (p.n_tiles < pairs ? p.n_tiles : pairs);
-  return launch_mx_logits(format, bn, dtype, tw, th, tsw, tsh, p, grid, reinterpret_cast<cudaStream_t>(stream)) ==
+  CUtensorMap tout;
+  memset(&tout, 0, sizeof tout);
+  if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
+  const int n_pairs = p.n_tiles < pairs ? p.n_tiles : pairs;
+  // a pair's token tiles follow each other in steps of n_pairs - shift: prime to their number, all come in turn
+  if (n_pairs > 1)
+    while (p.shift < n_pairs - 1 && common_divisor(n_pairs - p.shift, p.group) != 1) ++p.shift;
+  const int grid = 2 * n_pairs;
+  return launch_mx_logits(format, bn, dtype, tw, th, th_last, tsw, tsh, tout, p, grid, reinterpret_cast<cudaStream_t>(stream)) ==
                  cudaSuccess
              ? DIFR_OK
              : DIFR_ERR_CUDA;

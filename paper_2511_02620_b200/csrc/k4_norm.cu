@@ -5,10 +5,11 @@
 //   h = bf16(y)  and / or  codes, scales = microscaled(y)
 //
 // A row stays in registers between the sum of its squares and the scaling, so every element is read once and every
-// result written once: the kernel is bound by those bytes.  One row belongs to a group of whole warps (a thread holds
-// 8 * VPT elements, 16 bytes of bf16 at a time); short rows share a CTA.  The sum runs in fp32 in a fixed order
-// (per thread, shuffles, warps in order), so results do not depend on the launch.  y is rounded once, whatever asks
-// for it: the microscaled codes are taken from the fp32 value, not from h.
+// result written once: the kernel is bound by those bytes, as long as it spends few instructions per element (elements
+// are kept as they lie in memory, 8 per load, and worked on in pairs).  A row belongs to a group of whole warps; rows
+// off the 16-byte boundaries (odd d, odd strides) are turned through shared memory on their way in and out.  The sum
+// runs in fp32 in an order that only d and T fix (per thread, shuffles, warps in order).  y is rounded once, whatever
+// asks for it: the codes are taken from the fp32 value, not from h.
 #include <cuda_runtime.h>
 
 #include "mx_device.cuh"
@@ -16,129 +17,166 @@
 
 namespace difr {
 
-constexpr int kNormMaxThreads = 1024;
+constexpr int kNormMaxThreads = 512;
 
-// Sum over the threads of a row, the same value in all of them.  `part`: one float per warp of the CTA.
-__device__ __forceinline__ float row_sum(float v, float* part, int first_warp, int warps) {
+// Sum over the threads of a row, the same value in all of them.  A row of more than one warp has the CTA to itself.
+__device__ __forceinline__ float row_sum(float v, float* part, int warps) {
 #pragma unroll
   for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
   if (warps == 1) return v;
-  __syncthreads();  // (the array may still be read for an earlier sum)
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
   __syncthreads();
   float s = 0.f;
-  for (int i = 0; i < warps; ++i) s += part[first_warp + i];
+  for (int i = 0; i < warps; ++i) s += part[i];
   return s;
 }
 
-template <typename X, int VPT>
-__global__ void __launch_bounds__(VPT == 1 ? 512 : kNormMaxThreads) rms_norm(const NormParams p) {
-  __shared__ float part[kNormMaxThreads / 32];
-  const int tpr = p.threads_per_row;
-  const int in_cta = threadIdx.x / tpr;  // (tpr is a multiple of 32: uniform over a warp)
-  const int t = threadIdx.x - in_cta * tpr;
-  const int64_t row = (int64_t)blockIdx.x * p.rows_per_cta + in_cta;
-  const bool live = row < p.T;
-  const X* x = static_cast<const X*>(p.x) + (live ? row * p.ldx : 0);
-  const X* res = static_cast<const X*>(p.residual) + (live && p.residual ? row * p.ld_residual : 0);
+// 1 / sqrt(mean + eps) and a factor to apply first.  Squares of values above 1.8e19 leave fp32's range: such a row is
+// measured again in units of 2^80 by `again` (eps no longer counts).  A row with a NaN is NaN throughout; one with an
+// infinity is NaN there and zero elsewhere, as the formula has it.
+template <typename F>
+__device__ __forceinline__ float2 row_scale(float ss, int d, float eps, F again) {
+  if (ss > 3.0e38f) return make_float2(0x1p-80f, 1.f / sqrtf(again() / (float)d));
+  return make_float2(1.f, 1.f / sqrtf(ss / (float)d + eps));
+}
 
-  float v[VPT][8];
-  float ss = 0.f;
+// Rounded sum of two vectors.
+template <typename X>
+__device__ __forceinline__ void add_rounded(Vec8<X>& a, const Vec8<X>& b) {
 #pragma unroll
-  for (int j = 0; j < VPT; ++j) {
-    const int e0 = (j * tpr + t) * 8;
-    const int d = live ? p.d : 0;
-    load8<X>(x, e0, d, p.vec_x, v[j]);
-  }
-  if (p.residual != nullptr) {
+  for (int i = 0; i < 4; ++i) a.set_pair(i, fadd2(a.pair(i), b.pair(i)));
+}
+
+template <typename X, int VPT, bool RES, int FMT, bool AL>
+__global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(const NormParams p) {
+  __shared__ float part[2][kNormMaxThreads / 32];
+  __shared__ uint4 stage_all[AL ? 1 : kNormMaxThreads * sizeof(X) / 2];  // 256 elements per warp
+  X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : (threadIdx.x >> 5) * 256);
+  const int tpr = p.threads_per_row, warps = tpr >> 5;
+  const int in_cta = p.rows_per_cta == 1 ? 0 : (int)threadIdx.x >> 5;  // short rows: one warp each
+  const int t = p.rows_per_cta == 1 ? (int)threadIdx.x : (int)threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * p.rows_per_cta + in_cta;
+  if (row >= p.T) return;  // only where a row is a warp: no barrier is missed
+
+  Vec8<X> v[VPT];
+  load_row<X, VPT, AL>(v, static_cast<const X*>(p.x) + row * p.ldx, t, tpr, p.d, stage);
+  if (RES) {
+    Vec8<X> r[VPT];
+    load_row<X, VPT, AL>(r, static_cast<const X*>(p.residual) + row * p.ld_residual, t, tpr, p.d, stage);
+    X* to = static_cast<X*>(p.residual_out) + row * p.ld_residual_out;
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
-      const int e0 = (j * tpr + t) * 8;
-      float r[8];
-      load8<X>(res, e0, live ? p.d : 0, p.vec_residual, r);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = to_float<X>(from_float<X>(v[j][i] + r[i]));
-      if (p.residual_out != nullptr && live)
-        store8<X>(static_cast<X*>(p.residual_out) + row * p.ld_residual_out, e0, p.d, p.vec_residual_out, v[j]);
+      add_rounded<X>(v[j], r[j]);
+      if (p.residual_out != nullptr) store_row<X, AL>(v[j], to, j * tpr + t, p.d, stage);
     }
   }
+  float2 acc = make_float2(0.f, 0.f);
 #pragma unroll
   for (int j = 0; j < VPT; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(v[j][i], v[j][i], ss);
-  const int first_warp = in_cta * (tpr >> 5);
-  ss = row_sum(ss, part, first_warp, tpr >> 5);
-  float pre = 1.f, rstd;
-  // Squares of values above 1.8e19 leave fp32's range: such a row is measured again in units of 2^80.  (A row with a NaN
-  // is NaN throughout, one with an infinity is NaN there and zero elsewhere, as the formula has it.)  The vote keeps the barriers of row_sum uniform.
-  const bool over = ss > 3.0e38f;
-  rstd = 1.f / sqrtf(ss / (float)p.d + p.eps);
-  if (__syncthreads_or(over)) {
-    float s2 = 0.f;
+    for (int i = 0; i < 4; ++i) acc = ffma2(v[j].pair(i), v[j].pair(i), acc);
+  const float2 f = row_scale(row_sum(acc.x + acc.y, part[0], warps), p.d, p.eps, [&]() {
+    float2 a = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = v[j][i] * 0x1p-80f;
-        s2 = fmaf(a, a, s2);
+      for (int i = 0; i < 4; ++i) {
+        const float2 s = fmul2(v[j].pair(i), make_float2(0x1p-80f, 0x1p-80f));
+        a = ffma2(s, s, a);
       }
-    s2 = row_sum(s2, part, first_warp, tpr >> 5);
-    if (over) {
-      pre = 0x1p-80f;
-      rstd = 1.f / sqrtf(s2 / (float)p.d);
-    }
-  }
-  if (!live) return;  // whole warps; no barrier follows
+    return row_sum(a.x + a.y, part[1], warps);
+  });
 
-  const X* w = static_cast<const X*>(p.weight);
-  __nv_bfloat16* h = static_cast<__nv_bfloat16*>(p.h);
-  const int64_t words = mx_words(p.d);
-  const int nvec = p.fmt ? (int)mx_blocks(p.d) * 4 : (p.d + 7) / 8;
+  __nv_bfloat16* h = static_cast<__nv_bfloat16*>(p.h) + row * p.ldh;
+  const int nvec_mx = FMT ? (int)mx_blocks(p.d) * 4 : 0;
+  const int64_t words = FMT ? mx_words(p.d) : 0;
+  unsigned char* codes = p.codes + (FMT ? row * mx_pitch_bytes(FMT, p.d) : 0);
+  const bool huge = f.x != 1.f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
-    const int vec = j * tpr + t, e0 = vec * 8;
-    float g[8];
-    load8<X>(w, e0, p.d, p.vec_weight, g);
+    const int i = j * tpr + t;
+    Vec8<X> g[1];
+    load_row<X, 1, AL>(g, static_cast<const X*>(p.weight), i, 0, p.d, stage);
+    float2 y[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * pre * rstd * g[i];
-    if (h != nullptr && e0 < p.d) store8<__nv_bfloat16>(h + row * p.ldh, e0, p.d, p.vec_h, v[j]);
-    if (p.fmt != 0) {
-      // elements past the row must be zeros, not 0 * infinity
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (e0 + i >= p.d) v[j][i] = 0.f;
-      uint32_t c[2];
-      uint32_t word;
-      const bool past = vec >= nvec;
-      if (p.fmt == kMx8) {
-        word = mx_quantize8<kMx8>(v[j], past, c);
-        if (!past) *reinterpret_cast<uint2*>(p.codes + row * mx_pitch_bytes(kMx8, p.d) + e0) = make_uint2(c[0], c[1]);
-      } else {
-        word = mx_quantize8<kMx4>(v[j], past, c);
-        if (!past) *reinterpret_cast<uint32_t*>(p.codes + row * mx_pitch_bytes(kMx4, p.d) + (e0 >> 1)) = c[0];
-      }
-      if ((t & 15) == 0 && vec < nvec)
-        *reinterpret_cast<uint32_t*>(p.scales + mx_scale_offset(row, vec >> 4, words)) = word;
+    for (int k = 0; k < 4; ++k) {
+      float2 a = v[j].pair(k);
+      if (huge) a = fmul2(a, make_float2(f.x, f.x));
+      y[k] = fmul2(fmul2(a, make_float2(f.y, f.y)), g[0].pair(k));
     }
+    if (p.h != nullptr) {
+      Vec8<__nv_bfloat16> o;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o.set_pair(k, y[k]);
+      store_row<__nv_bfloat16, AL>(o, h, i, p.d, reinterpret_cast<__nv_bfloat16*>(stage));
+    }
+    if constexpr (FMT != 0) {
+      const bool past = i >= nvec_mx;
+      // the columns behind the row are zeros, not 0 * infinity
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i * 8 + 2 * k >= p.d) y[k].x = 0.f;
+        if (i * 8 + 2 * k + 1 >= p.d) y[k].y = 0.f;
+      }
+      uint32_t c[2];
+      const uint32_t word = mx_quantize8<FMT>(y, past, c);
+      if (!past) {
+        if (FMT == kMx8)
+          *reinterpret_cast<uint2*>(codes + (int64_t)i * 8) = make_uint2(c[0], c[1]);
+        else
+          *reinterpret_cast<uint32_t*>(codes + (int64_t)i * 4) = c[0];
+        if ((t & 15) == 0) *reinterpret_cast<uint32_t*>(p.scales + mx_scale_offset(row, i >> 4, words)) = word;
+      }
+    }
+  }
+}
+
+template <typename X, int VPT, bool RES, bool AL>
+static void launch_format(const NormParams& p, unsigned grid, int threads, cudaStream_t stream) {
+  if (p.fmt == kMx8)
+    rms_norm<X, VPT, RES, kMx8, AL><<<grid, threads, 0, stream>>>(p);
+  else if (p.fmt == kMx4)
+    rms_norm<X, VPT, RES, kMx4, AL><<<grid, threads, 0, stream>>>(p);
+  else
+    rms_norm<X, VPT, RES, 0, AL><<<grid, threads, 0, stream>>>(p);
+}
+template <typename X, int VPT>
+static void launch_vec(const NormParams& p, unsigned grid, int threads, cudaStream_t stream) {
+  if (p.vec) {
+    if (p.residual != nullptr)
+      launch_format<X, VPT, true, true>(p, grid, threads, stream);
+    else
+      launch_format<X, VPT, false, true>(p, grid, threads, stream);
+  } else {
+    if (p.residual != nullptr)
+      launch_format<X, VPT, true, false>(p, grid, threads, stream);
+    else
+      launch_format<X, VPT, false, false>(p, grid, threads, stream);
   }
 }
 
 template <typename X>
 static cudaError_t launch_typed(NormParams p, cudaStream_t stream) {
-  // threads per row: whole warps that cover the row (to whole blocks of 32 elements) at VPT vectors each
-  const int nvec = (p.d + 31) / 32 * 4;
-  int vpt = nvec <= 512 ? 1 : nvec <= 2048 ? 2 : 4;
+  // Vectors per thread: one where there are fewer rows than CTAs to fill the GPU (four 128-thread CTAs per SM), for the
+  // shortest way through a row; otherwise four (fp32: two, the same registers), for more loads in flight and fewer
+  // barriers per byte: T = 16384, d = 4096 in bf16 took 45.9 us at four, 48.3 at two, 47.3 at eight.  Rows that go
+  // through shared memory need the registers for that: one.
+  const int nvec = (p.d + 127) / 128 * 16;  // to whole scale words
+  int vpt = p.T < 592 || !p.vec ? 1 : sizeof(X) == 4 ? 2 : 4;
+  while (vpt > 1 && nvec <= 32 * vpt / 2) vpt /= 2;
+  while ((nvec + vpt - 1) / vpt > kNormMaxThreads) vpt *= 2;
   p.threads_per_row = ((nvec + vpt - 1) / vpt + 31) / 32 * 32;
-  p.rows_per_cta = p.threads_per_row >= 256 ? 1 : 256 / p.threads_per_row;
-  if (p.T < p.rows_per_cta) p.rows_per_cta = (int)p.T;
-  const int64_t grid = (p.T + p.rows_per_cta - 1) / p.rows_per_cta;
+  p.rows_per_cta = p.threads_per_row == 32 ? 4 : 1;
+  const unsigned grid = (unsigned)((p.T + p.rows_per_cta - 1) / p.rows_per_cta);
   const int threads = p.threads_per_row * p.rows_per_cta;
   if (vpt == 1)
-    rms_norm<X, 1><<<(unsigned)grid, threads, 0, stream>>>(p);
+    launch_vec<X, 1>(p, grid, threads, stream);
   else if (vpt == 2)
-    rms_norm<X, 2><<<(unsigned)grid, threads, 0, stream>>>(p);
+    launch_vec<X, 2>(p, grid, threads, stream);
+  else if (vpt == 4)
+    launch_vec<X, 4>(p, grid, threads, stream);
   else
-    rms_norm<X, 4><<<(unsigned)grid, threads, 0, stream>>>(p);
+    launch_vec<X, 8>(p, grid, threads, stream);
   return cudaGetLastError();
 }
 

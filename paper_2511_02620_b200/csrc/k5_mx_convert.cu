@@ -1,9 +1,10 @@
 // Microscaled formats: values -> codes and scales, and back.
 //
-// Both are bound by their bytes.  A warp takes a part of a row, a lane 8 consecutive values at a time (16 bytes of
-// bf16); the four lanes of a block find its maximum with two shuffles and the sixteen lanes of four blocks put their
-// scale bytes together, so that scales leave as whole 32-bit words.  Four vectors per lane are loaded before the first
-// is used.
+// Both are bound by their bytes, as long as few instructions are spent per value.  A warp takes a part of a row, a lane 8
+// consecutive values at a time (16 bytes of bf16); the four lanes of a block find its maximum with two shuffles and the
+// sixteen lanes of four blocks put their scale bytes together, so that scales leave as whole 32-bit words.  Four
+// vectors per lane are loaded before the first is used.  Rows off the 16-byte boundaries (odd d, odd strides) are
+// turned through shared memory, so that global loads and stores stay contiguous.
 #include <cuda_runtime.h>
 
 #include "mx_device.cuh"
@@ -15,25 +16,29 @@ constexpr int kCvtWarps = 8;    // rows per CTA
 constexpr int kCvtUnroll = 4;   // vectors of 8 values per lane
 constexpr int kCvtElems = 32 * 8 * kCvtUnroll;  // of a row, per CTA
 
-template <typename X, int FMT>
+template <typename X, int FMT, bool AL>
 __global__ void __launch_bounds__(kCvtWarps * 32) mx_quantize(const MxConvertParams p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kCvtWarps + (threadIdx.x >> 5);
+  __shared__ uint4 stage_all[AL ? 1 : kCvtWarps * 32 * sizeof(X) / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : warp * 256);
+  const int64_t row = (int64_t)blockIdx.x * kCvtWarps + warp;
   if (row >= p.rows) return;
-  const X* in = static_cast<const X*>(p.in) + row * p.ld;
   unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d);
   const int64_t words = mx_words(p.d);
   const int nvec = (int)mx_blocks(p.d) * 4;
   const int vec0 = (int)blockIdx.y * (kCvtElems / 8) + lane;
-  float v[kCvtUnroll][8];
-#pragma unroll
-  for (int j = 0; j < kCvtUnroll; ++j) load8<X>(in, (vec0 + j * 32) * 8, p.d, p.vec, v[j]);
+  Vec8<X> raw[kCvtUnroll];
+  load_row<X, kCvtUnroll, AL>(raw, static_cast<const X*>(p.in) + row * p.ld, vec0, 32, p.d, stage);
 #pragma unroll
   for (int j = 0; j < kCvtUnroll; ++j) {
     const int vec = vec0 + j * 32;
+    if (vec - lane >= nvec) break;  // uniform over the warp
     const bool past = vec >= nvec;
+    float2 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = raw[j].pair(i);
     uint32_t c[2];
-    const uint32_t word = mx_quantize8<FMT>(v[j], past, c);
+    const uint32_t word = mx_quantize8<FMT>(v, past, c);
     if (!past) {
       if (FMT == kMx8)
         *reinterpret_cast<uint2*>(codes + (int64_t)vec * 8) = make_uint2(c[0], c[1]);
@@ -44,10 +49,12 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_quantize(const MxConvertPar
   }
 }
 
-template <typename X, int FMT>
+template <typename X, int FMT, bool AL>
 __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertParams p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kCvtWarps + (threadIdx.x >> 5);
+  __shared__ uint4 stage_all[AL ? 1 : kCvtWarps * 32 * sizeof(X) / 2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : warp * 256);
+  const int64_t row = (int64_t)blockIdx.x * kCvtWarps + warp;
   if (row >= p.rows) return;
   X* out = static_cast<X*>(p.out) + row * p.ld;
   const unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d);
@@ -61,7 +68,7 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertP
     const int vec = vec0 + j * 32;
     c[j] = make_uint2(0u, 0u);
     byte[j] = 0u;
-    if (vec < nvec) {
+    if (vec < nvec) {  // (codes run to whole blocks: eight of them are always there)
       if (FMT == kMx8)
         c[j] = *reinterpret_cast<const uint2*>(codes + (int64_t)vec * 8);
       else
@@ -72,9 +79,9 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertP
 #pragma unroll
   for (int j = 0; j < kCvtUnroll; ++j) {
     const int vec = vec0 + j * 32;
-    if (vec >= nvec) break;
+    if (vec - lane >= nvec) break;  // uniform over the warp
     const float s = mx_scale_value(byte[j]);
-    float v[8];
+    Vec8<X> o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float2 two;
@@ -82,10 +89,9 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertP
         two = cvt_e4m3x2_to_float2(((i < 2 ? c[j].x : c[j].y) >> (16 * (i & 1))) & 0xFFFFu);
       else
         two = cvt_e2m1x2_to_float2((c[j].x >> (8 * i)) & 0xFFu);
-      v[2 * i] = two.x * s;
-      v[2 * i + 1] = two.y * s;
+      o.set_pair(i, fmul2(two, make_float2(s, s)));
     }
-    store8<X>(out, vec * 8, p.d, p.vec, v);
+    store_row<X, AL>(o, out, vec, p.d, stage);
   }
 }
 
@@ -93,13 +99,17 @@ static dim3 cvt_grid(const MxConvertParams& p) {
   return dim3((unsigned)((p.rows + kCvtWarps - 1) / kCvtWarps), (unsigned)((p.d + kCvtElems - 1) / kCvtElems));
 }
 
+template <typename X, int FMT>
+static cudaError_t quantize_format(const MxConvertParams& p, cudaStream_t stream) {
+  if (p.vec)
+    mx_quantize<X, FMT, true><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
+  else
+    mx_quantize<X, FMT, false><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
+  return cudaGetLastError();
+}
 template <typename X>
 static cudaError_t quantize_typed(const MxConvertParams& p, cudaStream_t stream) {
-  if (p.fmt == kMx8)
-    mx_quantize<X, kMx8><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
-  else
-    mx_quantize<X, kMx4><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
-  return cudaGetLastError();
+  return p.fmt == kMx8 ? quantize_format<X, kMx8>(p, stream) : quantize_format<X, kMx4>(p, stream);
 }
 
 cudaError_t launch_mx_quantize(const MxConvertParams& p, int dtype, cudaStream_t stream) {
@@ -110,13 +120,17 @@ cudaError_t launch_mx_quantize(const MxConvertParams& p, int dtype, cudaStream_t
   }
 }
 
+template <typename X, int FMT>
+static cudaError_t dequantize_format(const MxConvertParams& p, cudaStream_t stream) {
+  if (p.vec)
+    mx_dequantize<X, FMT, true><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
+  else
+    mx_dequantize<X, FMT, false><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
+  return cudaGetLastError();
+}
 template <typename X>
 static cudaError_t dequantize_typed(const MxConvertParams& p, cudaStream_t stream) {
-  if (p.fmt == kMx8)
-    mx_dequantize<X, kMx8><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
-  else
-    mx_dequantize<X, kMx4><<<cvt_grid(p), kCvtWarps * 32, 0, stream>>>(p);
-  return cudaGetLastError();
+  return p.fmt == kMx8 ? dequantize_format<X, kMx8>(p, stream) : dequantize_format<X, kMx4>(p, stream);
 }
 
 cudaError_t launch_mx_dequantize(const MxConvertParams& p, int dtype, cudaStream_t stream) {

@@ -16,8 +16,10 @@
 // CTA's own 128 ids and, in both CTAs, those of all BN tokens.  tcgen05.cp puts the words into TMEM, where the MMAs
 // read them.
 //
-// TMEM: two accumulators and a few slots of scales.  With BN = 256 two accumulators would take all 512 columns, so
-// they overlap by 64: the epilogue reads the shared columns first, and the next tile's MMAs start as soon as it has.
+// TMEM: two accumulators and each stage's scales.  With BN = 256 two accumulators would take all 512 columns, so they
+// overlap by 64 (e4m3) or 128 (e2m1): the epilogue reads the shared columns first, and the next tile's MMAs start as
+// soon as it has.  (Fewer columns of scales than stages were slower: the MMA warp then had to wait for the readers of a
+// slot, and its own loop, not the tensor pipe, set the pace: 520 clocks a stage where the MMAs take 512.)
 //
 // Warps: 0 TMA, 1 MMA, 2 TMEM allocation, 4..11 epilogue (two per lane quarter, half of the tile's columns each).
 #include <cuda.h>
@@ -49,34 +51,36 @@ struct MxTile {
   static constexpr int load_bytes = a_bytes + b_bytes + sa_bytes + sb_bytes;
   static constexpr int stage_bytes = (load_bytes + 1023) / 1024 * 1024;
   static constexpr int bar_bytes = 512;
-  static constexpr int fit = (227 * 1024 - 1024 - bar_bytes) / stage_bytes;
+  // 256-token tiles leave through shared memory: kOutBuffers pieces in flight for each half of the epilogue
+  static constexpr int out_buffers = BN == 256 ? 3 : 0;
+  static constexpr int out_bytes = 2 * out_buffers * kMxOutBytes;
+  static constexpr int fit = (227 * 1024 - 1024 - bar_bytes - out_bytes) / stage_bytes;
   static constexpr int stages = fit > 12 ? 12 : fit;
-  static constexpr int smem_bytes = stages * stage_bytes + bar_bytes + 1024;  // + slack for 1024-byte alignment
-  // TMEM columns
-  static constexpr bool overlap = BN == 256;
-  static constexpr int acc_stride = overlap ? 192 : BN;
-  static constexpr int shared_cols = overlap ? 64 : 0;
-  static constexpr int sf_col0 = overlap ? 448 : 2 * BN;
+  static constexpr int smem_bytes = stages * stage_bytes + out_bytes + bar_bytes + 1024;  // + slack for 1024-byte alignment
+  // TMEM columns: two accumulators, and a slot of scales per stage
   static constexpr int sa_cols = 4 * words, sb_cols = 4 * words * row_blocks;
   static constexpr int sf_cols = sa_cols + sb_cols;
-  static constexpr int slots_fit = (kMxTmemCols - sf_col0) / sf_cols;
-  static constexpr int slots = slots_fit > stages ? stages : slots_fit;
-  // epilogue: columns per TMEM load, loads per accumulator
+  static constexpr bool overlap = BN == 256;
+  static constexpr int shared_cols = !overlap ? 0 : sf_cols * stages > 64 ? 128 : 64;
+  static constexpr int acc_stride = BN - shared_cols;
+  static constexpr int sf_col0 = 2 * BN - shared_cols;
+  // epilogue: columns per TMEM load, loads per accumulator, loads per half that cover the shared columns
   static constexpr int chunk = BN >= 64 ? 32 : 16;
   static constexpr int chunks = BN / chunk;
-  static_assert(slots >= 2 && stages > slots - 1 && stages >= 2, "scale slots");
-  static_assert(!overlap || shared_cols == 2 * chunk, "each epilogue half drains one shared chunk first");
+  static constexpr int shared_loads = shared_cols / (2 * chunk);
+  static_assert(sf_col0 + stages * sf_cols <= kMxTmemCols, "TMEM columns");
+  static_assert(stages >= 4, "pipeline depth");
 };
 
 // Which chunk of the accumulator the `i`-th load of an epilogue half takes (-1: none).  Overlapping accumulators start
-// with the shared columns: the last 64 of accumulator 0, the first 64 of accumulator 1.
+// with the shared columns: the last ones of accumulator 0, the first ones of accumulator 1.
 template <int FMT, int BN>
 __device__ __forceinline__ int epi_chunk(int i, int half, int acc) {
   using Tl = MxTile<FMT, BN>;
   if (Tl::overlap) {
-    const int shared0 = acc == 0 ? Tl::chunks - 2 : 0;     // the shared chunks
-    const int rest0 = acc == 0 ? 0 : 2;                    // the others
-    return i == 0 ? shared0 + half : rest0 + half * (Tl::chunks / 2 - 1) + i - 1;
+    constexpr int shared = 2 * Tl::shared_loads, rest = Tl::chunks - shared;
+    if (i < Tl::shared_loads) return (acc == 0 ? rest : 0) + half * Tl::shared_loads + i;
+    return (acc == 0 ? 0 : shared) + half * (rest / 2) + i - Tl::shared_loads;
   }
   const int c = i * 2 + half;
   return c < Tl::chunks ? c : -1;
@@ -124,11 +128,75 @@ __device__ __forceinline__ void store_chunk(const MxLogitsParams& p, const uint3
   }
 }
 
+// The staged way out of a 32-token chunk, for the four warps (128 ids) of an epilogue half: through pieces in shared
+// memory that leave by TMA, whole rows of 128 ids at a time.  (Stored from registers, a warp's 32 ids of one token
+// are a request of 128 or 64 bytes each, and the requests, not the bytes, were what the epilogue took its time for.)
+template <typename OUT>
+struct OutPieces {
+  static constexpr int kTokens = mx_out_tokens((int)sizeof(OUT));
+  OUT* buf;        // this half's pieces
+  int next;        // the one to fill
+  uint64_t policy;
+
+  template <int BUFFERS>
+  __device__ __forceinline__ void store(const MxLogitsParams& p, const CUtensorMap* map, const uint32_t (&r)[32], int t0,
+                                        int v_block, int quarter, int lane, int half) {
+    const bool issuer = quarter == 0 && lane == 0;
+#pragma unroll
+    for (int k = 0; k < 32 / kTokens; ++k) {
+      if (t0 + k * kTokens >= p.T) break;  // the same in all four warps
+      if (issuer) bulk_wait_read<BUFFERS - 1>();  // the store that last left from this piece has read it
+      named_barrier(1 + half, 128);
+      OUT* dst = buf + next * (kMxOutBytes / (int)sizeof(OUT));
+#pragma unroll
+      for (int j = 0; j < kTokens; ++j)
+        dst[j * 128 + quarter * 32 + lane] = from_float<OUT>(__uint_as_float(r[k * kTokens + j]));
+      fence_async_shared();
+      named_barrier(1 + half, 128);
+      if (issuer) {
+        if (v_block < p.V) tma_store_2d(map, v_block, t0 + k * kTokens, smem_u32(dst), policy);
+        bulk_commit();
+      }
+      if (++next == BUFFERS) next = 0;
+    }
+  }
+};
+
+// The tiles of one pair.  Tiles are numbered in groups of token tiles (a group's tokens stay in L2 while W passes by),
+// inside a group along the vocabulary, inside that along the group's token tiles, and are dealt out in rounds of one
+// tile per pair: the pairs that run at the same time share a few rows of W.  From round to round the deal shifts by
+// `shift` pairs, chosen so that the narrower last token tiles reach all pairs alike.
+struct TileWalk {
+  const MxLogitsParams& p;
+  const int pair, n_pairs;
+  int round0, turn;  // first tile of the round, pair that is dealt to first
+
+  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n)
+      : p(params), pair(pr), n_pairs(n), round0(0), turn(0) {}
+  __device__ __forceinline__ bool next(int& vt, int& tt) {
+    const int at = pair - turn;
+    const int i = round0 + (at < 0 ? at + n_pairs : at);
+    if (i >= p.n_tiles) return false;
+    round0 += n_pairs;
+    turn += p.shift;
+    if (turn >= n_pairs) turn -= n_pairs;
+    const int per_group = p.group * p.n_vt;
+    const int g = i / per_group;
+    const int rem = i - g * per_group;
+    const int first = g * p.group;
+    const int cnt = min(p.group, p.n_tt - first);
+    vt = rem / cnt;
+    tt = first + rem - vt * cnt;
+    return true;
+  }
+};
+
 template <int FMT, int BN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxThreads, 1)
 mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_h,
-          const __grid_constant__ CUtensorMap tmap_sw, const __grid_constant__ CUtensorMap tmap_sh,
-          const MxLogitsParams p) {
+          const __grid_constant__ CUtensorMap tmap_h_last, const __grid_constant__ CUtensorMap tmap_sw,
+          const __grid_constant__ CUtensorMap tmap_sh, const __grid_constant__ CUtensorMap tmap_out,
+          const __grid_constant__ MxLogitsParams p) {
   using Tl = MxTile<FMT, BN>;
   constexpr int kStages = Tl::stages;
   extern __shared__ uint8_t smem_raw[];
@@ -142,8 +210,9 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   //   acc_full[a] each CTA's own copy: 1 arrival, the commit after a tile's last MMA, delivered to both
   //   acc_free[a] first CTA's copy is used: one arrival per epilogue warp of both CTAs, after its last load of the
   //               accumulator, or, where the accumulators overlap, after its load of shared columns
-  const uint32_t bar0 = smem_base + kStages * Tl::stage_bytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * Tl::stage_bytes);
+  const uint32_t bar0 = smem_base + kStages * Tl::stage_bytes + Tl::out_bytes;
+  uint8_t* out_pieces = smem + kStages * Tl::stage_bytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(out_pieces + Tl::out_bytes);
   auto full_bar = [&](int s) { return bar0 + 8u * (uint32_t)s; };
   auto empty_bar = [&](int s) { return bar0 + 8u * (uint32_t)(kStages + s); };
   auto acc_full_bar = [&](int a) { return bar0 + 8u * (uint32_t)(2 * kStages + a); };
@@ -171,6 +240,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     mbar_fence_init();
     tma_prefetch_desc(&tmap_w);
     tma_prefetch_desc(&tmap_h);
+    tma_prefetch_desc(&tmap_h_last);
     tma_prefetch_desc(&tmap_sw);
     tma_prefetch_desc(&tmap_sh);
   }
@@ -185,17 +255,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  // Tiles in raster order: groups of token tiles, inside a group the vocabulary, inside that the group's token tiles.
-  // The pairs that run at the same time share rows of W, and a group's tokens stay in L2 while W passes by.
-  auto decode = [&](int i, int& vt, int& tt) {
-    const int per_group = p.group * p.n_vt;
-    const int g = i / per_group;
-    const int rem = i - g * per_group;
-    const int first = g * p.group;
-    const int cnt = min(p.group, p.n_tt - first);
-    vt = rem / cnt;
-    tt = first + rem - vt * cnt;
-  };
+  TileWalk walk(p, pair, n_pairs);
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -204,19 +264,22 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int i = pair; i < p.n_tiles && ok; i += n_pairs) {
-      int vt, tt;
-      decode(i, vt, tt);
+    int vt, tt;
+    while (ok && walk.next(vt, tt)) {
+      const bool last = tt == p.n_tt - 1;
+      const int half = last ? p.last_tokens / 2 : BN / 2;
+      const uint32_t bytes = (uint32_t)(Tl::load_bytes - (BN / 2 - half) * kMxSlice);
+      const void* tmap_tokens = last ? &tmap_h_last : &tmap_h;
       const int w_row = vt * kMxPairM + (int)cta * 128;
-      const int h_row = tt * BN + (int)cta * (BN / 2);
+      const int h_row = tt * BN + (int)cta * half;
       for (int k = 0; k < p.k_steps; ++k) {
         if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
         if (elect_one()) {
-          if (cta == 0) mbar_arrive_expect_tx(full_bar(stage), 2u * Tl::load_bytes);
+          if (cta == 0) mbar_arrive_expect_tx(full_bar(stage), 2u * bytes);
           const uint32_t full0 = full0_base + 8u * (uint32_t)stage;
           const uint32_t dst = smem_base + (uint32_t)(stage * Tl::stage_bytes);
           tma_load_2d_pair(dst, &tmap_w, k * kMxSlice, w_row, full0, stream);
-          tma_load_2d_pair(dst + Tl::a_bytes, &tmap_h, k * kMxSlice, h_row, full0, keep);
+          tma_load_2d_pair(dst + Tl::a_bytes, tmap_tokens, k * kMxSlice, h_row, full0, keep);
           tma_load_3d_pair(dst + Tl::a_bytes + Tl::b_bytes, &tmap_sw, 0, k * Tl::words, w_row >> 7, full0, stream);
           tma_load_3d_pair(dst + Tl::a_bytes + Tl::b_bytes + Tl::sa_bytes, &tmap_sh, 0, k * Tl::words,
                            (tt * BN) >> 7, full0, keep);
@@ -228,18 +291,17 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issuer
     if (cta == 0) {
-      constexpr uint32_t idesc = umma_idesc_mx<FMT>(kMxPairM, BN);
       const uint64_t desc0 = umma_desc_k_major_sw128(smem_base);
       const uint32_t desc_hi = (uint32_t)(desc0 >> 32), desc_lo0 = (uint32_t)desc0;
       const uint64_t sdesc0 = umma_desc_scales(smem_base);
       const uint32_t sdesc_hi = (uint32_t)(sdesc0 >> 32), sdesc_lo0 = (uint32_t)sdesc0;
-      int stage = 0, acc = 0, slot = 0;
+      int stage = 0, acc = 0;
       uint32_t phase = 0, n_tile = 0;
-      // the stage whose MMAs last read the scale slot that comes next: `slots` stages ago
-      int old_stage = 0;
-      uint32_t old_phase = 0, n_step = 0;
+      bool full_seen = false;
       bool ok = true;
-      for (int i = pair; i < p.n_tiles && ok; i += n_pairs, ++n_tile) {
+      int vt, tt;
+      for (; ok && walk.next(vt, tt); ++n_tile) {
+        const uint32_t idesc = umma_idesc_mx<FMT>(kMxPairM, tt == p.n_tt - 1 ? p.last_tokens : BN);
         // Separate accumulators: the tile before last has been read.  Overlapping ones: the shared columns of the last
         // tile have been read (every epilogue warp had then finished the tile before it).
         if (Tl::overlap) {
@@ -253,21 +315,20 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * Tl::acc_stride);
         uint32_t accumulate = 0;
         for (int k = 0; k < p.k_steps; ++k) {
-          if (!__all_sync(0xffffffffu, mbar_wait(full_bar(stage), phase, abort_flag))) { ok = false; break; }
-          // the slot's last readers have finished (a copy is only ordered before the MMAs that follow it)
-          // (where there are as many slots as stages, the stage's own reuse says so)
-          if (Tl::slots < kStages && n_step >= (uint32_t)Tl::slots) {
-            if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(old_stage), old_phase, abort_flag))) { ok = false; break; }
-            if (++old_stage == kStages) { old_stage = 0; old_phase ^= 1u; }
+          if (!__all_sync(0xffffffffu, mbar_wait_cta(full_bar(stage), phase, full_seen, abort_flag))) { ok = false; break; }
+          // a look at the next stage: its answer is there by the time it is needed
+          {
+            const bool wrap = stage + 1 == kStages;
+            full_seen = mbar_peek_cta(full_bar(wrap ? 0 : stage + 1), wrap ? phase ^ 1u : phase);
           }
-          ++n_step;
           tc_fence_after();
           const int n_mma = k + 1 < p.k_steps ? kMxSlice / kMxMmaBytes : p.last_mmas;
           const uint32_t at = (uint32_t)(stage * Tl::stage_bytes) >> 4;
           const uint32_t a_lo = desc_lo0 + at, b_lo = a_lo + (Tl::a_bytes >> 4);
           const uint32_t sa_lo = sdesc_lo0 + at + ((Tl::a_bytes + Tl::b_bytes) >> 4);
           const uint32_t sb_lo = sa_lo + (Tl::sa_bytes >> 4);
-          const uint32_t sa = tmem_base + (uint32_t)(Tl::sf_col0 + slot * Tl::sf_cols);
+          // (a stage has its own columns for scales, free again when the stage is)
+          const uint32_t sa = tmem_base + (uint32_t)(Tl::sf_col0 + stage * Tl::sf_cols);
           const uint32_t sb = sa + Tl::sa_cols;
           if (elect_one()) {
 #pragma unroll
@@ -296,7 +357,6 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
           __syncwarp();
           accumulate = 1;
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
-          if (++slot == Tl::slots) slot = 0;
         }
         if (ok && elect_one()) umma_commit_pair(acc_full_bar(acc), 3);
         __syncwarp();
@@ -310,27 +370,39 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
     int acc = 0;
     uint32_t acc_phase = 0;
-    for (int i = pair; i < p.n_tiles; i += n_pairs) {
-      int vt, tt;
-      decode(i, vt, tt);
-      if (!mbar_wait(acc_full_bar(acc), acc_phase, abort_flag)) break;
+    OutPieces<OUT> pieces;
+    pieces.buf = reinterpret_cast<OUT*>(out_pieces + half * (Tl::out_bytes / 2));
+    pieces.next = 0;
+    pieces.policy = l2_policy_evict_first();
+    int vt, tt;
+    while (walk.next(vt, tt)) {
+      bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
+      // (the warps of a half meet at barriers below, so they give up together or not at all)
+      if (BN == 256) ok = named_barrier_and(1 + half, 128, ok);
+      if (!ok) break;
       __syncwarp();
       tc_fence_after();
       const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
       const uint32_t free_bar = map_to_cta(acc_free_bar(acc), 0);
       constexpr int kLoads = (Tl::chunks + 1) / 2;
+      // where the accumulators overlap, the shared columns are read first, all of them before the first store
+      constexpr int kFirst = Tl::overlap ? Tl::shared_loads : 1;
+      uint32_t r[kFirst][Tl::chunk];
 #pragma unroll 1
-      for (int c = 0; c < kLoads; ++c) {
-        const int ch = epi_chunk<FMT, BN>(c, half, acc);
-        uint32_t r[Tl::chunk];
-        if (ch >= 0) {
-          const uint32_t taddr = tmem_base + lane_addr + (uint32_t)(acc * Tl::acc_stride + ch * Tl::chunk);
-          if constexpr (Tl::chunk == 32) {
-            tmem_ld_32x32(taddr, r);
-            tmem_ld_wait32(r);
-          } else {
-            tmem_ld_32x16(taddr, r);
-            tmem_ld_wait(r);
+      for (int c = 0; c < kLoads; c += (c == 0 ? kFirst : 1)) {
+        const int n_here = c == 0 ? kFirst : 1;
+#pragma unroll
+        for (int q = 0; q < kFirst; ++q) {
+          const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
+          if (q < n_here && ch >= 0 && tt * BN + ch * Tl::chunk < p.T) {
+            const uint32_t taddr = tmem_base + lane_addr + (uint32_t)(acc * Tl::acc_stride + ch * Tl::chunk);
+            if constexpr (Tl::chunk == 32) {
+              tmem_ld_32x32(taddr, r[q]);
+              tmem_ld_wait32(r[q]);
+            } else {
+              tmem_ld_32x16(taddr, r[q]);
+              tmem_ld_wait(r[q]);
+            }
           }
         }
         if (c == (Tl::overlap ? 0 : kLoads - 1)) {
@@ -338,13 +410,24 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster_nofence(free_bar);
         }
-        if (ch >= 0) {
+#pragma unroll
+        for (int q = 0; q < kFirst; ++q) {
+          const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
           const int t0 = tt * BN + ch * Tl::chunk;
-          if (t0 < p.T) store_chunk<Tl::chunk>(p, r, t0, v, static_cast<OUT*>(nullptr));
+          if (q < n_here && ch >= 0 && t0 < p.T) {
+            if constexpr (BN == 256) {
+              if (p.tile_stores) {
+                pieces.template store<Tl::out_buffers>(p, &tmap_out, r[q], t0, v - quarter * 32 - lane, quarter, lane, half);
+                continue;
+              }
+            }
+            store_chunk<Tl::chunk>(p, r[q], t0, v, static_cast<OUT*>(nullptr));
+          }
         }
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
+    if (BN == 256 && p.tile_stores) bulk_wait_all();  // the pieces stay until they have left
   }
 
   __syncwarp();
@@ -366,36 +449,36 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
 
 // ------------------------------------------------------------------ launcher
 template <int FMT, int BN, typename OUT>
-static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& sw,
-                               const CUtensorMap& sh, const MxLogitsParams& p, int grid, cudaStream_t stream) {
+static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& hl, const CUtensorMap& sw,
+                               const CUtensorMap& sh, const CUtensorMap& out, const MxLogitsParams& p, int grid, cudaStream_t stream) {
   const cudaError_t e = cudaFuncSetAttribute(mx_logits<FMT, BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              MxTile<FMT, BN>::smem_bytes);
   if (e != cudaSuccess) return e;
-  mx_logits<FMT, BN, OUT><<<grid, kMxThreads, MxTile<FMT, BN>::smem_bytes, stream>>>(w, h, sw, sh, p);
+  mx_logits<FMT, BN, OUT><<<grid, kMxThreads, MxTile<FMT, BN>::smem_bytes, stream>>>(w, h, hl, sw, sh, out, p);
   return cudaGetLastError();
 }
 
 template <int FMT, typename OUT>
-static cudaError_t launch_typed(int bn, const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& sw,
-                                const CUtensorMap& sh, const MxLogitsParams& p, int grid, cudaStream_t stream) {
+static cudaError_t launch_typed(int bn, const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& hl, const CUtensorMap& sw,
+                                const CUtensorMap& sh, const CUtensorMap& out, const MxLogitsParams& p, int grid, cudaStream_t stream) {
   switch (bn) {
-    case 16: return launch_tile<FMT, 16, OUT>(w, h, sw, sh, p, grid, stream);
-    case 32: return launch_tile<FMT, 32, OUT>(w, h, sw, sh, p, grid, stream);
-    case 64: return launch_tile<FMT, 64, OUT>(w, h, sw, sh, p, grid, stream);
-    case 128: return launch_tile<FMT, 128, OUT>(w, h, sw, sh, p, grid, stream);
-    case 256: return launch_tile<FMT, 256, OUT>(w, h, sw, sh, p, grid, stream);
+    case 16: return launch_tile<FMT, 16, OUT>(w, h, hl, sw, sh, out, p, grid, stream);
+    case 32: return launch_tile<FMT, 32, OUT>(w, h, hl, sw, sh, out, p, grid, stream);
+    case 64: return launch_tile<FMT, 64, OUT>(w, h, hl, sw, sh, out, p, grid, stream);
+    case 128: return launch_tile<FMT, 128, OUT>(w, h, hl, sw, sh, out, p, grid, stream);
+    case 256: return launch_tile<FMT, 256, OUT>(w, h, hl, sw, sh, out, p, grid, stream);
   }
   return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
-                             const CUtensorMap& sw, const CUtensorMap& sh, const MxLogitsParams& p, int grid,
+                             const CUtensorMap& hl, const CUtensorMap& sw, const CUtensorMap& sh, const CUtensorMap& out, const MxLogitsParams& p, int grid,
                              cudaStream_t stream) {
   if (fmt == kMx8)
-    return dtype == kBf16 ? launch_typed<kMx8, __nv_bfloat16>(tokens_per_tile, w, h, sw, sh, p, grid, stream)
-                          : launch_typed<kMx8, float>(tokens_per_tile, w, h, sw, sh, p, grid, stream);
-  return dtype == kBf16 ? launch_typed<kMx4, __nv_bfloat16>(tokens_per_tile, w, h, sw, sh, p, grid, stream)
-                        : launch_typed<kMx4, float>(tokens_per_tile, w, h, sw, sh, p, grid, stream);
+    return dtype == kBf16 ? launch_typed<kMx8, __nv_bfloat16>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream)
+                          : launch_typed<kMx8, float>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream);
+  return dtype == kBf16 ? launch_typed<kMx4, __nv_bfloat16>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream)
+                        : launch_typed<kMx4, float>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream);
 }
 
 // Pairs the device keeps resident at once: one CTA per SM, the same for every variant (each takes the whole TMEM).

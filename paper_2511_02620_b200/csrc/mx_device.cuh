@@ -55,7 +55,7 @@ __device__ __forceinline__ uint32_t cvt_e4m3x4(float a0, float a1, float a2, flo
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(hi) : "f"(a2), "f"(a3));
   return (uint32_t)lo | ((uint32_t)hi << 16);
 }
-__device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&a)[8]) {
+__device__ __forceinline__ uint32_t cvt_e2m1x8(const float2 (&a)[4]) {
   uint32_t r;
   asm("{\n"
       ".reg .b8 b0, b1, b2, b3;\n"
@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&a)[8]) {
       "mov.b32 %0, {b0, b1, b2, b3};\n"
       "}\n"
       : "=r"(r)
-      : "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]), "f"(a[4]), "f"(a[5]), "f"(a[6]), "f"(a[7]));
+      : "f"(a[0].x), "f"(a[0].y), "f"(a[1].x), "f"(a[1].y), "f"(a[2].x), "f"(a[2].y), "f"(a[3].x), "f"(a[3].y));
   return r;
 }
 // Codes back to values (exact in fp16: e4m3 and e2m1 are subsets of it).
@@ -90,29 +90,46 @@ __device__ __forceinline__ float2 cvt_e2m1x2_to_float2(uint32_t two_codes) {
   return half2_bits_to_float2(h2);
 }
 
+// max(|a|, |b|, |c|); a NaN among them is what comes out.
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&d);
+}
+
 // Quantises 8 consecutive values held by each lane.  A block of 32 is four neighbouring lanes (lane % 4 == 0 starts
 // one), a scale word (four blocks) sixteen; every lane of the warp takes part, lanes past the row hold zeros.  `codes`
 // receives 8 codes (4 or 8 bytes), the returned word is the four scale bytes of the lane's sixteen.
 template <int FMT>
-__device__ __forceinline__ uint32_t mx_quantize8(const float (&v)[8], bool past_end, uint32_t (&codes)[2]) {
-  // magnitudes compare like their bits, and a NaN's bits are above every number's
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+__device__ __forceinline__ uint32_t mx_quantize8(const float2 (&v)[4], bool past_end, uint32_t (&codes)[2]) {
+  // (magnitudes compare like their bits, and a NaN's bits are above every number's)
+  float f = max3_abs(v[0].x, v[0].y, v[1].x);
+  f = max3_abs(f, v[1].y, v[2].x);
+  f = max3_abs(f, v[2].y, v[3].x);
+  f = max3_abs(f, v[3].y, 0.f);
+  uint32_t m = __float_as_uint(f);
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
   m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
   const uint32_t byte = past_end ? 0u : mx_scale_byte<FMT>(m);
   const float inv = mx_inverse_scale(byte);
-  float q[8];
+  float2 q[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = byte == 255u ? 0.f : v[i] * inv;
+  for (int i = 0; i < 4; ++i) q[i] = fmul2(v[i], make_float2(inv, inv));
   if (FMT == kMx8) {
-    codes[0] = cvt_e4m3x4(q[0], q[1], q[2], q[3]);
-    codes[1] = cvt_e4m3x4(q[4], q[5], q[6], q[7]);
+    codes[0] = cvt_e4m3x4(q[0].x, q[0].y, q[1].x, q[1].y);
+    codes[1] = cvt_e4m3x4(q[2].x, q[2].y, q[3].x, q[3].y);
   } else {
     codes[0] = cvt_e2m1x8(q);
     codes[1] = 0;
   }
+  if (byte == 255u) codes[0] = codes[1] = 0;
   uint32_t word = byte << (((threadIdx.x >> 2) & 3) * 8);
   word |= __shfl_xor_sync(0xffffffffu, word, 4);
   word |= __shfl_xor_sync(0xffffffffu, word, 8);
@@ -137,39 +154,155 @@ __device__ __forceinline__ __half from_float<__half>(float x) { return __float2h
 template <>
 __device__ __forceinline__ float from_float<float>(float x) { return x; }
 
-// Elements e0 .. e0 + 7 of a row of d, zeros past its end.  `vec`: the row starts on a 16-byte boundary.  (Plain loads,
-// not the read-only path: a call may write its result over its input.)
+// Eight consecutive elements as they lie in memory, on a 16-byte boundary.  (Plain loads, not the read-only path: a call
+// may write its result over its input.)
 template <typename X>
-__device__ __forceinline__ void load8(const X* row, int e0, int d, bool vec, float (&v)[8]) {
-  if (vec && e0 + 8 <= d) {
-    __align__(16) X raw[8];
+struct Vec8 {
+  uint4 q[sizeof(X) / 2];
+  __device__ __forceinline__ void load(const X* p) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(X) * 8 / 16; ++i)
-      reinterpret_cast<uint4*>(raw)[i] = reinterpret_cast<const uint4*>(row + e0)[i];
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+  }
+  __device__ __forceinline__ void store(X* p) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_float<X>(raw[i]);
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = q[i];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(X) / 2; ++i) q[i] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ uint32_t word(int i) const {
+    const uint4& a = q[i >> 2];
+    return (i & 3) == 0 ? a.x : (i & 3) == 1 ? a.y : (i & 3) == 2 ? a.z : a.w;
+  }
+  __device__ __forceinline__ void set_word(int i, uint32_t w) {
+    uint4& a = q[i >> 2];
+    if ((i & 3) == 0) a.x = w;
+    else if ((i & 3) == 1) a.y = w;
+    else if ((i & 3) == 2) a.z = w;
+    else a.w = w;
+  }
+  // elements 2 i and 2 i + 1
+  __device__ __forceinline__ float2 pair(int i) const;
+  __device__ __forceinline__ void set_pair(int i, float2 v);
+};
+template <>
+__device__ __forceinline__ float2 Vec8<__nv_bfloat16>::pair(int i) const {
+  const uint32_t w = word(i);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+template <>
+__device__ __forceinline__ float2 Vec8<__half>::pair(int i) const {
+  return half2_bits_to_float2(word(i));
+}
+template <>
+__device__ __forceinline__ float2 Vec8<float>::pair(int i) const {
+  return make_float2(__uint_as_float(word(2 * i)), __uint_as_float(word(2 * i + 1)));
+}
+template <>
+__device__ __forceinline__ void Vec8<__nv_bfloat16>::set_pair(int i, float2 v) {
+  __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
+  set_word(i, *reinterpret_cast<uint32_t*>(&b));
+}
+template <>
+__device__ __forceinline__ void Vec8<__half>::set_pair(int i, float2 v) {
+  __half2 b = __floats2half2_rn(v.x, v.y);
+  set_word(i, *reinterpret_cast<uint32_t*>(&b));
+}
+template <>
+__device__ __forceinline__ void Vec8<float>::set_pair(int i, float2 v) {
+  set_word(2 * i, __float_as_uint(v.x));
+  set_word(2 * i + 1, __float_as_uint(v.y));
+}
+
+// Vectors vec0 + j stride (j < N) of a row of d elements, one per lane, zeros past its end; vec0 - lane is the same in
+// all lanes.  AL: the row starts on a 16-byte boundary and d is a multiple of 8.  Otherwise (odd d, odd strides) the warp
+// reads its 256 elements one per lane, 32 neighbours at a time, and turns them through `stage` (256 elements of its own).
+template <typename X, int N, bool AL>
+__device__ __forceinline__ void load_row(Vec8<X> (&v)[N], const X* row, int vec0, int stride, int d, X* stage) {
+  if constexpr (AL) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = vec0 + j * stride;
+      if (i * 8 < d) v[j].load(row + i * 8); else v[j].zero();
+    }
   } else {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = e0 + i < d ? to_float<X>(row[e0 + i]) : 0.f;
+    for (int j = 0; j < N; ++j) {
+      const int e0 = (vec0 - lane + j * stride) * 8 + lane;
+      X one[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) one[k] = e0 + k * 32 < d ? row[e0 + k * 32] : from_float<X>(0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) stage[k * 32 + lane] = one[k];
+      __syncwarp();
+      v[j].load(stage + lane * 8);
+      __syncwarp();
+    }
   }
 }
-template <typename X>
-__device__ __forceinline__ void store8(X* row, int e0, int d, bool vec, const float (&v)[8]) {
-  if (vec && e0 + 8 <= d) {
-    __align__(16) X raw[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i] = from_float<X>(v[i]);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(X) * 8 / 16; ++i)
-      reinterpret_cast<uint4*>(row + e0)[i] = reinterpret_cast<const uint4*>(raw)[i];
+// The way back for one vector per lane.
+template <typename X, bool AL>
+__device__ __forceinline__ void store_row(const Vec8<X>& v, X* row, int vec, int d, X* stage) {
+  if constexpr (AL) {
+    if (vec * 8 < d) v.store(row + vec * 8);
   } else {
+    const int lane = threadIdx.x & 31;
+    v.store(stage + lane * 8);
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (e0 + i < d) row[e0 + i] = from_float<X>(v[i]);
+    for (int k = 0; k < 8; ++k) {
+      const int e = (vec - lane) * 8 + k * 32 + lane;
+      if (e < d) row[e] = stage[k * 32 + lane];
+    }
+    __syncwarp();
   }
 }
 
 // ------------------------------------------------------- PTX: TMA and tcgen05 of the block-scaled product
+// Waits at CTA scope: for phases that a copy or a commit completes (what they order lies in shared memory and TMEM, and
+// is read by the tensor core).  mbar_peek_cta only looks, mbar_test_cta lets the hardware suspend the thread for a while.
+__device__ __forceinline__ bool mbar_peek_cta(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_test_cta(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// The bounded wait at CTA scope; `seen`: the barrier's phase was already seen to be complete.
+__device__ __forceinline__ bool mbar_wait_cta(uint32_t bar, uint32_t parity, bool seen, volatile int* abort_flag) {
+  if (seen || mbar_test_cta(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (true) {
+    if (mbar_test_cta(bar, parity)) return true;
+    if (*abort_flag) return false;
+    if (clock64() - t0 > kWaitCycles) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+
 // Three-dimensional form of tma_load_2d_pair.
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* tmap, int x, int y, int z,
                                                  uint32_t bar, uint64_t policy) {
@@ -178,6 +311,46 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst_smem, const void* 
       "[%0], [%1, {%2, %3, %4}], [%5], %6;"
       ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar), "l"(policy)
       : "memory");
+}
+
+// Tile store: shared memory (rows of the box one after another) -> global memory; what lies outside the tensor is left out.
+__device__ __forceinline__ void tma_store_2d(const void* tmap, int x, int y, uint32_t src_smem, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%1, %2}], [%3], %4;"
+      ::"l"(tmap), "r"(x), "r"(y), "r"(src_smem), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// At most N of this thread's committed stores still read shared memory.
+template <int N>
+__device__ __forceinline__ void bulk_wait_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// Makes this thread's shared-memory writes visible to the copies that follow.
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// The same, and whether `ok` held for all of its threads.
+__device__ __forceinline__ bool named_barrier_and(int id, int threads, bool ok) {
+  uint32_t all;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.u32 p, %3, 0;\n"
+      "barrier.cta.red.and.pred q, %1, %2, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(all)
+      : "r"(id), "r"(threads), "r"((uint32_t)ok)
+      : "memory");
+  return all != 0;
+}
+__device__ __forceinline__ uint64_t l2_policy_evict_first() {
+  uint64_t pol;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
+  return pol;
 }
 
 // Copies one scale word (32 lanes x 16 bytes, in each CTA of the pair from its own shared memory) to four TMEM

@@ -21,7 +21,7 @@ struct NormParams {
   int d, fmt;
   float eps;
   int threads_per_row, rows_per_cta;
-  bool vec_x, vec_residual, vec_residual_out, vec_h, vec_weight;  // rows start on 16-byte boundaries
+  bool vec;              // all rows start on 16-byte boundaries and d is a multiple of 8
 };
 constexpr int kNormMaxD = 32768;
 cudaError_t launch_rms_norm(const NormParams& p, int dtype, cudaStream_t stream);
@@ -33,7 +33,7 @@ struct MxConvertParams {
   unsigned char* scales;
   int64_t rows, ld;
   int d, fmt;
-  bool vec;              // rows of `in` / `out` start on 16-byte boundaries
+  bool vec;              // the rows of `in` / `out` start on 16-byte boundaries and d is a multiple of 8
 };
 cudaError_t launch_mx_quantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
 cudaError_t launch_mx_dequantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
@@ -47,13 +47,19 @@ struct MxLogitsParams {
   int last_mmas;         // MMAs (32 bytes of codes each) of the last slice
   int n_vt, n_tt;        // vocabulary tiles of 256 ids, token tiles
   int group;             // token tiles per raster group
+  int last_tokens;       // width of the last token tile, a multiple of 16
   int n_tiles;
-  bool pack_pairs;       // bf16 logits: two neighbouring ids leave in one 4-byte store
+  int shift;             // of the deal, per round
+  bool pack_pairs;       // bf16 logits, plain stores: two neighbouring ids leave in one 4-byte store
+  bool tile_stores;      // the rows of the logits start on 16-byte boundaries: tiles leave by TMA (256-token tiles only)
 };
 constexpr int kMxPairM = 256;  // vocabulary ids per tile of a CTA pair
-// `tokens_per_tile`: 16, 32, 64, 128 or 256; maps: codes of W and h, scales of W and h.
+constexpr int kMxOutBytes = 8192;                            // a piece of a tile on its way out: 128 ids x
+constexpr int mx_out_tokens(int elem) { return kMxOutBytes / (128 * elem); }  // 16 (fp32) or 32 (bf16) tokens
+// `tokens_per_tile`: 16, 32, 64, 128 or 256; maps: codes of W, of h, of h for the last token tile, scales of W
+// and of h, logits (used with tile_stores only).
 cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
-                             const CUtensorMap& sw, const CUtensorMap& sh, const MxLogitsParams& p, int grid,
+                             const CUtensorMap& h_last, const CUtensorMap& sw, const CUtensorMap& sh, const CUtensorMap& out, const MxLogitsParams& p, int grid,
                              cudaStream_t stream);
 int mx_logits_max_resident_pairs();
 
