@@ -376,10 +376,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     pieces.policy = l2_policy_evict_first();
     int vt, tt;
     while (walk.next(vt, tt)) {
-      bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
-      // (the warps of a half meet at barriers below, so they give up together or not at all)
-      if (BN == 256) ok = named_barrier_and(1 + half, 128, ok);
-      if (!ok) break;
+      const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
       __syncwarp();
       tc_fence_after();
       const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
@@ -388,28 +385,34 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       // where the accumulators overlap, the shared columns are read first, all of them before the first store
       constexpr int kFirst = Tl::overlap ? Tl::shared_loads : 1;
       uint32_t r[kFirst][Tl::chunk];
-#pragma unroll 1
-      for (int c = 0; c < kLoads; c += (c == 0 ? kFirst : 1)) {
-        const int n_here = c == 0 ? kFirst : 1;
+      auto load = [&](int c, int n) {
 #pragma unroll
         for (int q = 0; q < kFirst; ++q) {
           const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
-          if (q < n_here && ch >= 0 && tt * BN + ch * Tl::chunk < p.T) {
+          if (q < n && ch >= 0 && tt * BN + ch * Tl::chunk < p.T) {
             const uint32_t taddr = tmem_base + lane_addr + (uint32_t)(acc * Tl::acc_stride + ch * Tl::chunk);
-            if constexpr (Tl::chunk == 32) {
-              tmem_ld_32x32(taddr, r[q]);
-              tmem_ld_wait32(r[q]);
-            } else {
-              tmem_ld_32x16(taddr, r[q]);
-              tmem_ld_wait(r[q]);
-            }
+            if constexpr (Tl::chunk == 32) tmem_ld_32x32(taddr, r[q]); else tmem_ld_32x16(taddr, r[q]);
           }
         }
-        if (c == (Tl::overlap ? 0 : kLoads - 1)) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster_nofence(free_bar);
+#pragma unroll
+        for (int q = 0; q < kFirst; ++q) {
+          if constexpr (Tl::chunk == 32) tmem_ld_wait32(r[q]); else tmem_ld_wait(r[q]);
         }
+      };
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster_nofence(free_bar);
+      };
+      if (ok) {
+        load(0, kFirst);
+        if (Tl::overlap || kLoads == 1) release();
+      }
+      // (the warps of a half meet at barriers below, so they give up together or not at all)
+      if (BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !ok) break;
+#pragma unroll 1
+      for (int c = 0; c < kLoads;) {
+        const int n_here = c == 0 ? kFirst : 1;
 #pragma unroll
         for (int q = 0; q < kFirst; ++q) {
           const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
@@ -423,6 +426,11 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
             }
             store_chunk<Tl::chunk>(p, r[q], t0, v, static_cast<OUT*>(nullptr));
           }
+        }
+        c += n_here;
+        if (c < kLoads) {
+          load(c, 1);
+          if (!Tl::overlap && c == kLoads - 1) release();
         }
       }
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
