@@ -381,6 +381,11 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       tc_fence_after();
       const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
       const uint32_t free_bar = map_to_cta(acc_free_bar(acc), 0);
+      // A tile store cuts rows at whole 16 bytes only: where the last ids end inside such a piece, they leave by plain
+      // stores.
+      const int v_block = v - quarter * 32 - lane;
+      const bool by_tile = BN == 256 && p.tile_stores &&
+                           (v_block + 128 <= p.V || p.V % (16 / (int)sizeof(OUT)) == 0);
       constexpr int kLoads = (Tl::chunks + 1) / 2;
       // where the accumulators overlap, the shared columns are read first, all of them before the first store
       constexpr int kFirst = Tl::overlap ? Tl::shared_loads : 1;
@@ -419,8 +424,8 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
           const int t0 = tt * BN + ch * Tl::chunk;
           if (q < n_here && ch >= 0 && t0 < p.T) {
             if constexpr (BN == 256) {
-              if (p.tile_stores) {
-                pieces.template store<Tl::out_buffers>(p, &tmap_out, r[q], t0, v - quarter * 32 - lane, quarter, lane, half);
+              if (by_tile) {
+                pieces.template store<Tl::out_buffers>(p, &tmap_out, r[q], t0, v_block, quarter, lane, half);
                 continue;
               }
             }

@@ -313,3 +313,267 @@ def test_logits(T, d, V, out_dtype, fmt):
     assert int(status.item()) == 0
     exact, bound = logits_bound(hv, Wv, fmt, dt)
     assert torch.all((out.cpu().double() - exact).abs() <= bound)
+
+
+@pytest.mark.parametrize("fmt", [4, 8])
+@pytest.mark.parametrize("out_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,ld", [(3, 300, 300), (140, 520, 528), (300, 1000, 1008), (300, 1001, 1001), (530, 777, 800),
+                                    (257, 130, 131)])
+def test_logits_rows_of_a_wider_matrix(T, V, ld, out_dtype, fmt):
+    """Row strides that do and do not allow tile stores; nothing is written behind a row or behind the last one."""
+    d = 160
+    h, hv = random_mx(T, d, fmt, seed=1)
+    W, Wv = random_mx(V, d, fmt, seed=2)
+    dt = DTYPES[out_dtype]
+    buf = torch.full((T + 2, ld), -7.0, dtype=dt, device="cuda")
+    difr.difr_mx_logits(h, W, buf[:T, :V])
+    exact, bound = logits_bound(hv, Wv, fmt, dt)
+    assert torch.all((buf[:T, :V].cpu().double() - exact).abs() <= bound)
+    assert torch.all(buf[:T, V:] == -7.0) and torch.all(buf[T:] == -7.0)
+
+
+@pytest.mark.parametrize("T", [15, 16, 17, 31, 33, 63, 65, 127, 129, 255, 257, 272, 384, 511, 512, 769])
+def test_logits_at_the_borders_of_token_tiles(T):
+    for fmt in (4, 8):
+        h, hv = random_mx(T, 96, fmt, seed=T)
+        W, Wv = random_mx(1100, 96, fmt, seed=T + 1)
+        out = torch.full((T, 1100), math.nan, device="cuda")
+        difr.difr_mx_logits(h, W, out)
+        exact, bound = logits_bound(hv, Wv, fmt, torch.float32)
+        assert torch.all((out.cpu().double() - exact).abs() <= bound)
+
+
+@pytest.mark.parametrize("fmt", [4, 8])
+@pytest.mark.parametrize("T", [1, 200])
+def test_broken_blocks_make_their_logits_nan(T, fmt):
+    """A NaN or an infinity in a hidden state makes its row NaN, one in the head its column; the rest is untouched."""
+    d, V = 200, 700
+    x, w = randn(T, d, seed=8), randn(V, d, seed=9)
+    w[13, 199], w[600, 0] = math.inf, math.nan
+    if T > 1:
+        x[77, 5] = -math.inf
+    h, W = mx_of(T, d, fmt), mx_of(V, d, fmt)
+    difr.difr_mx_quantize(x.cuda(), h)
+    difr.difr_mx_quantize(w.cuda(), W)
+    out = torch.empty(T, V, device="cuda")
+    difr.difr_mx_logits(h, W, out)
+    nan = torch.zeros(T, V, dtype=torch.bool)
+    nan[:, 13] = nan[:, 600] = True
+    if T > 1:
+        nan[77] = True
+    assert torch.equal(torch.isnan(out).cpu(), nan)
+
+
+def test_extreme_scales_in_the_product():
+    """Scales up to the ends of fp32: products that fit come out to the bound, those beyond as infinities."""
+    for fmt in (4, 8):
+        d = 128
+        c = torch.zeros(4, d, dtype=torch.long)
+        one = int((ref.table(fmt) == 1.0).nonzero())
+        c[:, 0] = one
+        hb = torch.tensor([[127 + 60], [127 - 60], [127 + 100], [127]]).expand(4, 4)
+        wb = torch.tensor([[127 + 60], [127 - 60], [127 + 100], [127]]).expand(4, 4)
+        h = difr.MxTensor(ref.pack(c, fmt).cuda(), ref.tile_scales(hb).cuda(), fmt, 4, d)
+        W = difr.MxTensor(ref.pack(c, fmt).cuda(), ref.tile_scales(wb).cuda(), fmt, 4, d)
+        out = torch.empty(4, 4, device="cuda")
+        difr.difr_mx_logits(h, W, out)
+        e = torch.tensor([60, -60, 100, 0])
+        want = torch.exp2((e.view(-1, 1) + e.view(1, -1)).double()).float()
+        assert torch.equal(out.cpu(), want)
+
+
+def test_outputs_beyond_32_bits():
+    """Logits of more than 2^32 values and a matrix of more than 2^32 elements: the last rows are where they belong."""
+    T, V, d = 33000, 131072 + 6, 32
+    h, hv = random_mx(T, d, 4, seed=3)
+    W, Wv = random_mx(V, d, 4, seed=4)
+    out = torch.empty(T, V, dtype=torch.bfloat16, device="cuda")
+    assert out.numel() > 2 ** 32
+    difr.difr_mx_logits(h, W, out)
+    rows = [0, 1, 16383, 16384, 32767, 32768, T - 1]
+    exact, bound = logits_bound(hv[rows], Wv, 4, torch.bfloat16)
+    assert torch.all((out[rows].cpu().double() - exact).abs() <= bound)
+    del out
+    rows, d = (1 << 20) + 3, 4104
+    x = torch.zeros(rows, d, dtype=torch.bfloat16, device="cuda")
+    assert x.numel() > 2 ** 32
+    tail = randn(3, d, seed=6).bfloat16()
+    x[-3:] = tail.cuda()
+    mx = difr.MxTensor.allocate(rows, d, 8)
+    difr.difr_mx_quantize(x, mx)
+    c, byte = ref.quantize(tail, 8)
+    assert torch.equal(mx.codes[-3:].cpu(), ref.pack(c, 8)) and int(mx.codes[:-3].max()) == 0
+    x.zero_()
+    difr.difr_mx_dequantize(mx, x)
+    assert torch.equal(x[-3:].cpu().double(), ref.values(c, byte, 8, d)) and float(x[:-3].abs().max()) == 0
+    x[:-3] = 0
+    x[-3:] = tail.cuda()
+    difr.difr_rms_norm(x, torch.ones(d, dtype=torch.bfloat16, device="cuda"), 1e-6, difr.NormOut(h=x))
+    _, y = ref.rms_norm(tail, None, torch.ones(d), 1e-6)
+    assert_close_h(x[-3:], y)
+
+
+# ------------------------------------------------------------------ together, and as programs call it
+@pytest.mark.parametrize("fmt", [4, 8])
+def test_a_quantised_head_from_the_residual_stream_to_the_scores(fmt):
+    """Norm -> microscaled h -> logits of the quantised head; the same head dequantised goes through the scoring calls, and
+    both agree: logits with difr_logits, the greedy replay's token with the largest logit."""
+    T, d, V = 300, 512, 4096
+    x, r = randn(T, d, seed=1).bfloat16().cuda(), randn(T, d, seed=2, std=2.0).bfloat16().cuda()
+    w = (1 + 0.1 * randn(d, seed=3)).bfloat16().cuda()
+    Wb = (randn(V, d, seed=4) * d ** -0.5).bfloat16().cuda()
+    W = difr.difr_mx_quantize(Wb, difr.MxTensor.allocate(V, d, fmt))
+    o = difr.NormOut(residual=r, mx=difr.MxTensor.allocate(T, d, fmt))
+    difr.difr_rms_norm(x, w, 1e-6, o, residual=r)
+    logits = difr.difr_mx_logits(o.mx, W, torch.empty(T, V, device="cuda"))
+    h = difr.difr_mx_dequantize(o.mx, torch.empty(T, d, dtype=torch.bfloat16, device="cuda"))
+    Wd = difr.difr_mx_dequantize(W, torch.empty(V, d, dtype=torch.bfloat16, device="cuda"))
+    exact, bound = logits_bound(h.cpu().double(), Wd.cpu().double(), fmt, torch.float32)
+    assert torch.all((logits.cpu().double() - exact).abs() <= bound)
+    plain = difr.difr_logits(h, Wd, torch.empty(T, V, device="cuda"))
+    # (the bf16 product accumulates 16 values a step: twice the steps at most)
+    assert torch.all((logits - plain).abs().cpu() <= 5 * bound)
+    out = difr.DifrOut.allocate(T, d, V, 0.05)
+    top = logits.topk(2, dim=1)
+    tokens = top.indices[:, 0].int().contiguous()
+    difr.difr_score_gm(h, Wd, tokens, torch.arange(T, device="cuda"), torch.arange(T, device="cuda", dtype=torch.int32), 0.0, out)
+    clear = (top.values[:, 0] - top.values[:, 1]).cpu() > 2 * bound.max(dim=1).values
+    assert clear.float().mean() > 0.9
+    assert torch.equal(out.argmax.cpu()[clear], tokens.cpu()[clear])
+    assert torch.all(out.margin.cpu()[clear] >= 0)
+
+
+def test_capture_and_replay():
+    """A captured run of the operators, replayed on other inputs in the same buffers, gives what the calls give."""
+    T, d, V, fmt = 200, 416, 1000, 4
+    x, r = torch.empty(T, d, dtype=torch.bfloat16, device="cuda"), torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    Wb = randn(V, d, seed=1).bfloat16().cuda()
+
+    def make():
+        return (difr.NormOut(h=torch.empty_like(x), residual=torch.empty_like(x), mx=difr.MxTensor.allocate(T, d, fmt)),
+                difr.MxTensor.allocate(V, d, fmt), torch.empty(T, V, device="cuda"), torch.empty_like(x))
+
+    def run(o, W, logits, back):
+        difr.difr_mx_quantize(Wb, W)
+        difr.difr_rms_norm(x, w, 1e-6, o, residual=r)
+        difr.difr_mx_logits(o.mx, W, logits)
+        difr.difr_mx_dequantize(o.mx, back)
+
+    x.copy_(randn(T, d, seed=2)); r.copy_(randn(T, d, seed=3))
+    a, b = make(), make()
+    run(*a)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):  # two graphs of the same work, replayed one after the other
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            run(*a)
+        graphs.append(g)
+    for seed in (5, 6, 7):
+        x.copy_(randn(T, d, seed=seed)); r.copy_(randn(T, d, seed=seed + 10)); Wb.copy_(randn(V, d, seed=seed + 20))
+        for g in graphs:
+            g.replay()
+        run(*b)
+        torch.cuda.synchronize()
+        for p, q in zip((a[0].h, a[0].residual, a[0].mx.codes, a[0].mx.scales, a[2], a[3]),
+                        (b[0].h, b[0].residual, b[0].mx.codes, b[0].mx.scales, b[2], b[3])):
+            assert torch.equal(p, q)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, and on a stream that is not the current one, each with buffers of their own."""
+    T, d, V = 500, 1024, 30000
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    sets = []
+    for k, fmt in enumerate((4, 8)):
+        h, hv = random_mx(T, d, fmt, seed=k)
+        W, Wv = random_mx(V, d, fmt, seed=10 + k)
+        sets.append((h, W, torch.empty(T, V, device="cuda"), difr.difr_mx_logits(h, W, torch.empty(T, V, device="cuda"))))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (h, W, out, _) in zip(streams, sets):
+            difr.difr_mx_logits(h, W, out, stream=s)
+    torch.cuda.synchronize()
+    for _, _, out, want in sets:
+        assert torch.equal(out, want)
+
+
+def test_repeated_calls_give_the_same_bits():
+    for fmt in (4, 8):
+        T, d, V = 700, 1000, 5000
+        x, w = randn(T, d, seed=1).cuda(), torch.ones(d, device="cuda")
+        W = difr.difr_mx_quantize(randn(V, d, seed=2).cuda(), difr.MxTensor.allocate(V, d, fmt))
+        first = None
+        for _ in range(30):
+            o = difr.NormOut(h=torch.empty(T, d, dtype=torch.bfloat16, device="cuda"), mx=difr.MxTensor.allocate(T, d, fmt))
+            difr.difr_rms_norm(x, w, 1e-6, o)
+            out = difr.difr_mx_logits(o.mx, W, torch.empty(T, V, device="cuda"))
+            now = (o.h, o.mx.codes, o.mx.scales, out)
+            first = first or now
+            assert all(torch.equal(p, q) for p, q in zip(now, first))
+
+
+def test_empty_batches():
+    d, V = 64, 300
+    x = torch.empty(0, d, device="cuda")
+    mx = difr.MxTensor.allocate(0, d, 4)
+    difr.difr_mx_quantize(x, mx)
+    difr.difr_mx_dequantize(mx, x)
+    difr.difr_rms_norm(x, torch.ones(d, device="cuda"), 1e-6, difr.NormOut(h=torch.empty(0, d, dtype=torch.bfloat16, device="cuda"), mx=mx))
+    W, _ = random_mx(V, d, 4, seed=1)
+    difr.difr_mx_logits(mx, W, torch.empty(0, V, device="cuda"))
+    torch.cuda.synchronize()
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    d = 64
+    x = torch.zeros(8, d, device="cuda")
+    w = torch.ones(d, device="cuda")
+    h16 = torch.empty(8, d, dtype=torch.bfloat16, device="cuda")
+    mx = difr.MxTensor.allocate(8, d, 4)
+    W = difr.MxTensor.allocate(100, d, 4)
+    logits = torch.empty(8, 100, device="cuda")
+    bad = [
+        lambda: difr.difr_mx_quantize(x.double(), mx),
+        lambda: difr.difr_mx_quantize(x.cpu(), mx),
+        lambda: difr.difr_mx_quantize(x[0], mx),
+        lambda: difr.difr_mx_quantize(x[:4], mx),
+        lambda: difr.difr_mx_quantize(x.t(), difr.MxTensor.allocate(d, 8, 4)),
+        lambda: difr.difr_mx_quantize(x[:1].expand(8, d), mx),
+        lambda: difr.difr_mx_quantize(x, difr.MxTensor(mx.codes, mx.scales, 8, 8, d)),
+        lambda: difr.difr_mx_quantize(x, difr.MxTensor(mx.codes, mx.scales[:-1], 4, 8, d)),
+        lambda: difr.difr_mx_quantize(x, difr.MxTensor(mx.codes.cpu(), mx.scales, 4, 8, d)),
+        lambda: difr.difr_mx_quantize(x, difr.MxTensor(mx.codes, mx.scales, 6, 8, d)),
+        lambda: difr.difr_mx_dequantize(mx, x.half()),
+        lambda: difr.difr_mx_dequantize(mx, x[:, :32]),
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut(h=x)),                       # h is bf16
+        lambda: difr.difr_rms_norm(x, w.bfloat16(), 1e-6, difr.NormOut(h=h16)),
+        lambda: difr.difr_rms_norm(x, w[:32], 1e-6, difr.NormOut(h=h16)),
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut(h=h16), residual=x.bfloat16()),
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut(h=h16), residual=x[:4]),
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut(mx=W)),
+        lambda: difr.difr_mx_logits(mx, difr.MxTensor.allocate(100, d, 8), logits),      # mixed formats
+        lambda: difr.difr_mx_logits(mx, difr.MxTensor.allocate(100, 32, 4), logits),
+        lambda: difr.difr_mx_logits(mx, W, logits.half()),
+        lambda: difr.difr_mx_logits(mx, W, logits[:, :99]),
+    ]
+    for k, call in enumerate(bad):
+        with pytest.raises(TypeError):
+            call()
+            pytest.fail(f"call {k} was accepted")
+    refused = [
+        lambda: difr.difr_rms_norm(x, w, 0.0, difr.NormOut(h=h16)),
+        lambda: difr.difr_rms_norm(x, w, math.nan, difr.NormOut(h=h16)),
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut()),                           # nothing asked for
+        lambda: difr.difr_rms_norm(x, w, 1e-6, difr.NormOut(h=h16, residual=x)),          # a stream without a residual
+        lambda: difr.difr_rms_norm(torch.zeros(1, 32776, device="cuda"), torch.ones(32776, device="cuda"), 1e-6,
+                                   difr.NormOut(h=torch.empty(1, 32776, dtype=torch.bfloat16, device="cuda"))),
+    ]
+    for call in refused:
+        with pytest.raises(difr.DifrError):
+            call()
+    unaligned = torch.empty(8 * 32 + 1, dtype=torch.uint8, device="cuda")[1:].view(8, 32)
+    with pytest.raises(difr.DifrError):
+        difr.difr_mx_quantize(x, difr.MxTensor(unaligned, mx.scales, 4, 8, d))
+    torch.cuda.synchronize()
