@@ -427,6 +427,7 @@ class NormOut:
 
 
 _DTYPES = {}  # torch dtype -> difr_dtype
+_ANY_DTYPE, _WIDE_DTYPE = (DIFR_BF16, DIFR_F16, DIFR_F32), (DIFR_BF16, DIFR_F32)
 
 
 def _dtypes():
@@ -438,30 +439,35 @@ def _dtypes():
 
 
 def _matrix(t, name, dtypes, shape=None, device=None):
-    """A CUDA matrix whose rows are contiguous; returns (C dtype, row stride)."""
-    if getattr(t, "is_cuda", None) is not True or t.dim() != 2:
+    """A CUDA matrix whose rows are contiguous; returns (C dtype, row stride, device index)."""
+    try:
+        index = t.get_device()
+        code = _dtypes().get(t.dtype)
+        rows, cols = t.shape
+        ld, step = t.stride()
+    except (AttributeError, ValueError):
+        raise TypeError(f"{name} must be a CUDA matrix") from None
+    if index < 0:
         raise TypeError(f"{name} must be a CUDA matrix")
-    code = _dtypes().get(t.dtype)
     if code not in dtypes:
         raise TypeError(f"{name}: {t.dtype} is not supported here")
-    if shape is not None and t.shape != shape:
-        raise TypeError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
-    if device is not None and t.device != device:
-        raise TypeError(f"{name} is on {t.device}, not on {device}")
-    rows, cols = t.shape
-    ld, step = t.stride()
+    if shape is not None and (rows, cols) != shape:
+        raise TypeError(f"{name}: expected {tuple(shape)}, got {(rows, cols)}")
+    if device is not None and index != device:
+        raise TypeError(f"{name} is on device {index}, not on {device}")
     if rows <= 1 and ld < cols:
         ld = cols
     if (step != 1 and cols > 1) or ld < cols:
         raise TypeError(f"{name}: the rows must be contiguous and must not overlap")
-    return code, ld
+    return code, ld, index
 
 
 def _check_mx(mx, name, device):
     if not isinstance(mx, MxTensor) or mx.format not in (DIFR_MX8, DIFR_MX4):
         raise TypeError(f"{name} must be an MxTensor of 8 or 4 bits")
-    _check_bytes(mx.codes, mx.rows * ((mx.d + 31) // 32 * 4 * mx.format), name, "codes", device)
-    _check_bytes(mx.scales, (mx.rows + 127) // 128 * ((mx.d + 127) // 128) * 512, name, "scales", device)
+    rows, d = mx.rows, mx.d
+    _check_bytes(mx.codes, rows * ((d + 31) // 32 * 4 * mx.format), name, "codes", device)
+    _check_bytes(mx.scales, (rows + 127) // 128 * ((d + 127) // 128) * 512, name, "scales", device)
 
 
 def _check_bytes(t, n, name, what, device):
@@ -469,23 +475,23 @@ def _check_bytes(t, n, name, what, device):
 
     if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous():
         raise TypeError(f"{name}.{what} must be {n} contiguous bytes (uint8)")
-    if t.device != device:
-        raise TypeError(f"{name}.{what} is on {t.device}, not on {device}")
+    if t.get_device() != device:
+        raise TypeError(f"{name}.{what} is on {t.device}, not on CUDA device {device}")
 
 
 def _call(name, device, stream, *args):
-    """Calls an entry point with `device` current, on the given stream or that device's current one."""
+    """Calls an entry point with device number `device` current, on the given stream or that device's current one."""
     import torch
 
     if stream is None:
         # (the handle alone: building a torch.cuda.Stream costs 2 us a call)
-        raw = torch._C._cuda_getCurrentRawStream(device.index)
-    elif stream.device != device:
-        raise TypeError(f"the stream is on {stream.device}, the tensors on {device}")
+        raw = torch._C._cuda_getCurrentRawStream(device)
+    elif stream.device.index != device:
+        raise TypeError(f"the stream is on {stream.device}, the tensors on CUDA device {device}")
     else:
         raw = stream.cuda_stream
     fn = getattr(_lib or lib(), name)
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device:
         rc = fn(*args, raw)
     else:
         with torch.cuda.device(device):
@@ -496,22 +502,22 @@ def _call(name, device, stream, *args):
 
 def difr_mx_quantize(x, out: MxTensor, stream=None) -> MxTensor:
     """Microscaled codes and scales of a matrix (bf16, fp16 or fp32); see include/difr.h."""
-    dtype, ld = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
-    _check_mx(out, "out", x.device)
+    dtype, ld, device = _matrix(x, "x", _ANY_DTYPE)
+    _check_mx(out, "out", device)
     if (out.rows, out.d) != x.shape:
         raise TypeError(f"out is {out.rows} x {out.d}, x {tuple(x.shape)}")
-    _call("difr_mx_quantize", x.device, stream, x.data_ptr(), dtype, out.rows, out.d, ld, out.format,
+    _call("difr_mx_quantize", device, stream, x.data_ptr(), dtype, out.rows, out.d, ld, out.format,
           out.codes.data_ptr(), out.scales.data_ptr())
     return out
 
 
 def difr_mx_dequantize(mx: MxTensor, out, stream=None):
     """The values of a microscaled tensor, as bf16 (what the scoring calls take) or fp32."""
-    dtype, ld = _matrix(out, "out", (DIFR_BF16, DIFR_F32))
-    _check_mx(mx, "mx", out.device)
+    dtype, ld, device = _matrix(out, "out", _WIDE_DTYPE)
+    _check_mx(mx, "mx", device)
     if (mx.rows, mx.d) != out.shape:
         raise TypeError(f"out is {tuple(out.shape)}, the tensor {mx.rows} x {mx.d}")
-    _call("difr_mx_dequantize", out.device, stream, mx.codes.data_ptr(), mx.scales.data_ptr(), mx.format, mx.rows, mx.d,
+    _call("difr_mx_dequantize", device, stream, mx.codes.data_ptr(), mx.scales.data_ptr(), mx.format, mx.rows, mx.d,
           out.data_ptr(), dtype, ld)
     return out
 
@@ -520,11 +526,11 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     """Final root-mean-square norm of x (+ residual); `out.h` feeds the scoring calls, `out.mx` difr_mx_logits."""
     import torch
 
-    dtype, ldx = _matrix(x, "x", (DIFR_BF16, DIFR_F16, DIFR_F32))
-    shape, device = x.shape, x.device
-    if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.device != device
+    dtype, ldx, device = _matrix(x, "x", _ANY_DTYPE)
+    shape = x.shape
+    if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
             or weight.shape != shape[1:] or not weight.is_contiguous()):
-        raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {device}")
+        raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {x.device}")
     c = _CNormOut()
     ldr = 0
     if residual is not None:
@@ -549,8 +555,7 @@ def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=
     """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format."""
     import torch
 
-    dtype, ld = _matrix(logits, "logits", (DIFR_F32, DIFR_BF16))
-    device = logits.device
+    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
     _check_mx(h, "h", device)
     _check_mx(W, "W", device)
     if h.format != W.format or h.d != W.d:
@@ -559,8 +564,8 @@ def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=
         raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
     if device_status is not None:
         _check(device_status, torch.int32, (1,), "device_status")
-        if device_status.device != device:
-            raise TypeError(f"device_status is on {device_status.device}, not on {device}")
+        if device_status.get_device() != device:
+            raise TypeError(f"device_status is on {device_status.device}, not on CUDA device {device}")
     _call("difr_mx_logits", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
           W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld,
           None if device_status is None else device_status.data_ptr())
