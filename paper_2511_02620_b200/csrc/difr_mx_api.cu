@@ -193,7 +193,7 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
   p.x = x; p.residual = residual; p.weight = weight; p.residual_out = out->residual; p.h = out->h;
   p.codes = static_cast<unsigned char*>(out->codes); p.scales = static_cast<unsigned char*>(out->scales);
   p.T = T; p.ldx = ldx; p.ld_residual = ld_residual; p.ld_residual_out = out->ld_residual; p.ldh = out->ldh;
-  p.d = (int)d; p.fmt = out->mx_format; p.eps = eps;
+  p.d = (int)d; p.fmt = out->mx_format; p.eps = eps; p.inv_d = 1.f / (float)d;
   p.vec = d % 8 == 0 && vector_rows(x, ldx, dtype) && aligned16(weight) &&
           (!residual || vector_rows(residual, ld_residual, dtype)) &&
           (!out->residual || vector_rows(out->residual, out->ld_residual, dtype)) &&

@@ -8,7 +8,7 @@
 // result written once: the kernel is bound by those bytes, as long as it spends few instructions per element (elements
 // are kept as they lie in memory, 8 per load, and worked on in pairs).  A row belongs to a group of whole warps; rows
 // off the 16-byte boundaries (odd d, odd strides) are turned through shared memory on their way in and out.  The sum
-// runs in fp32 in an order that only d and T fix (per thread, shuffles, warps in order).  y is rounded once, whatever
+// runs in an order that only d and T fix (per thread, shuffles, warps in order).  y is rounded once, whatever
 // asks for it: the codes are taken from the fp32 value, not from h.
 #include <cuda_runtime.h>
 
@@ -20,24 +20,27 @@ namespace difr {
 constexpr int kNormMaxThreads = 512;
 
 // Sum over the threads of a row, the same value in all of them.  A row of more than one warp has the CTA to itself.
-__device__ __forceinline__ float row_sum(float v, float* part, int warps) {
+// A thread's own terms are few and go in fp32; their sums are joined in fp64, so that the result is the exact sum
+// rounded once, nearly always: values next to a border of the 4-bit format depend on its last bit.
+__device__ __forceinline__ float row_sum(float own, double* part, int warps) {
+  double v = own;
 #pragma unroll
-  for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
-  if (warps == 1) return v;
+  for (int m = 16; m >= 1; m >>= 1) v += shfl_xor_double(v, m);
+  if (warps == 1) return (float)v;
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
   __syncthreads();
-  float s = 0.f;
+  double s = 0.0;
   for (int i = 0; i < warps; ++i) s += part[i];
-  return s;
+  return (float)s;
 }
 
 // 1 / sqrt(mean + eps) and a factor to apply first.  Squares of values above 1.8e19 leave fp32's range: such a row is
 // measured again in units of 2^80 by `again` (eps no longer counts).  A row with a NaN is NaN throughout; one with an
 // infinity is NaN there and zero elsewhere, as the formula has it.
 template <typename F>
-__device__ __forceinline__ float2 row_scale(float ss, int d, float eps, F again) {
-  if (ss > 3.0e38f) return make_float2(0x1p-80f, 1.f / sqrtf(again() / (float)d));
-  return make_float2(1.f, 1.f / sqrtf(ss / (float)d + eps));
+__device__ __forceinline__ float2 row_scale(float ss, float inv_d, float eps, F again) {
+  if (ss > 3.0e38f) return make_float2(0x1p-80f, rsqrtf(again() * inv_d));
+  return make_float2(1.f, rsqrtf(__fadd_rn(__fmul_rn(ss, inv_d), eps)));  // (the mean is a value of its own: no fma)
 }
 
 // Rounded sum of two vectors.
@@ -49,7 +52,7 @@ __device__ __forceinline__ void add_rounded(Vec8<X>& a, const Vec8<X>& b) {
 
 template <typename X, int VPT, bool RES, int FMT, bool AL>
 __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(const NormParams p) {
-  __shared__ float part[2][kNormMaxThreads / 32];
+  __shared__ double part[2][kNormMaxThreads / 32];
   __shared__ uint4 stage_all[AL ? 1 : kNormMaxThreads * sizeof(X) / 2];  // 256 elements per warp
   X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : (threadIdx.x >> 5) * 256);
   const int tpr = p.threads_per_row, warps = tpr >> 5;
@@ -75,7 +78,7 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
   for (int j = 0; j < VPT; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc = ffma2(v[j].pair(i), v[j].pair(i), acc);
-  const float2 f = row_scale(row_sum(acc.x + acc.y, part[0], warps), p.d, p.eps, [&]() {
+  const float2 f = row_scale(row_sum(acc.x + acc.y, part[0], warps), p.inv_d, p.eps, [&]() {
     float2 a = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < VPT; ++j)

@@ -19,7 +19,7 @@ struct NormParams {
   unsigned char* scales;
   int64_t T, ldx, ld_residual, ld_residual_out, ldh;
   int d, fmt;
-  float eps;
+  float eps, inv_d;
   int threads_per_row, rows_per_cta;
   bool vec;              // all rows start on 16-byte boundaries and d is a multiple of 8
 };

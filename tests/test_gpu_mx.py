@@ -577,3 +577,23 @@ def test_the_binding_refuses_what_does_not_fit():
     with pytest.raises(difr.DifrError):
         difr.difr_mx_quantize(x, difr.MxTensor(unaligned, mx.scales, 4, 8, d))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", [4, 8])
+@pytest.mark.parametrize("out_dtype", ["f32", "bf16"])
+def test_logits_at_every_alignment_of_their_rows(out_dtype, fmt):
+    """First elements at every place inside 16 bytes, strides that move it from row to row, vocabularies that end anywhere
+    inside a block of 128 ids: all values are there and their neighbours are left alone."""
+    dt = DTYPES[out_dtype]
+    T, d = 261, 64
+    h, hv = random_mx(T, d, fmt, seed=1)
+    for k, (V, pad) in enumerate([(256, 0), (257, 0), (383, 1), (385, 2), (130, 3), (255, 5), (512, 7), (640, 1), (769, 0)]):
+        W, Wv = random_mx(V, d, fmt, seed=2 + k)
+        exact, bound = logits_bound(hv, Wv, fmt, dt)
+        for off in (0, 1, 3, 6):
+            flat = torch.full((T * (V + pad) + 64,), -7.0, dtype=dt, device="cuda")
+            out = torch.as_strided(flat, (T, V), (V + pad, 1), off)
+            difr.difr_mx_logits(h, W, out)
+            assert torch.all((out.cpu().double() - exact).abs() <= bound)
+            out.fill_(-7.0)
+            assert torch.all(flat == -7.0)
