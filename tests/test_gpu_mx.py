@@ -382,6 +382,86 @@ def test_extreme_scales_in_the_product():
         assert torch.equal(out.cpu(), want)
 
 
+def test_scales_at_the_ends_of_their_range():
+    """Scale bytes 0 (2^-127) and 254 (2^127) against each other."""
+    for fmt in (4, 8):
+        c = torch.zeros(3, 32, dtype=torch.long)
+        c[:, 5] = int((ref.table(fmt) == 1.0).nonzero())
+        hb, wb = torch.tensor([[0], [254], [127]]), torch.tensor([[254], [0], [127]])
+        h = difr.MxTensor(ref.pack(c, fmt).cuda(), ref.tile_scales(hb).cuda(), fmt, 3, 32)
+        W = difr.MxTensor(ref.pack(c, fmt).cuda(), ref.tile_scales(wb).cuda(), fmt, 3, 32)
+        out = torch.empty(3, 3, device="cuda")
+        difr.difr_mx_logits(h, W, out)
+        assert out[0, 0].item() == 1.0 and out[1, 1].item() == 1.0 and out[2, 2].item() == 1.0
+        assert math.isinf(out[1, 0].item()) and out[2, 0].item() == 2.0 ** 127 and out[1, 2].item() == 2.0 ** 127
+
+
+def test_random_shapes():
+    """Seeded random problems over the operators' ranges, small sizes more often."""
+    import random
+
+    rng = random.Random(2026)
+
+    def size(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    for i in range(60):
+        fmt, dtype = rng.choice((4, 8)), rng.choice(list(DTYPES))
+        T, V, d = size(1, 700), size(1, 3000), size(1, 3000)
+        pad, res = rng.choice((0, 0, 1, 8)), rng.random() < 0.5
+        x = randn(T, d + pad, seed=i).to(DTYPES[dtype])
+        r = randn(T, d, seed=1000 + i, std=4.0).to(DTYPES[dtype]) if res else None
+        w = (1 + 0.3 * randn(d, seed=2000 + i)).to(DTYPES[dtype])
+        o = difr.NormOut(h=torch.empty(T, d, dtype=torch.bfloat16, device="cuda"), mx=mx_of(T, d, fmt),
+                         residual=torch.empty(T, d, dtype=DTYPES[dtype], device="cuda") if res else None)
+        difr.difr_rms_norm(x.cuda()[:, :d], w.cuda(), 1e-5, o, residual=r.cuda() if res else None)
+        stream, y = ref.rms_norm(x[:, :d], r, w, 1e-5)
+        assert_close_h(o.h, y)
+        assert_mx_nearest(o.mx, y, fmt)
+        if res:
+            assert torch.equal(o.residual.cpu(), stream)
+        Wp = (randn(V, d, seed=3000 + i) * d ** -0.5).to(DTYPES[dtype])
+        W = mx_of(V, d, fmt)
+        difr.difr_mx_quantize(Wp.cuda(), W)
+        assert_mx_equal(W, Wp, fmt)
+        out_dtype = rng.choice((torch.float32, torch.bfloat16))
+        out = torch.full((T, V), math.nan, dtype=out_dtype, device="cuda")
+        difr.difr_mx_logits(o.mx, W, out)
+        nb = (d + 31) // 32
+        hv = ref.values(ref.unpack(o.mx.codes.cpu(), fmt), ref.untile_scales(o.mx.scales.cpu(), T, nb), fmt, d)
+        c, byte = ref.quantize(Wp, fmt)
+        exact, bound = logits_bound(hv, ref.values(c, byte, fmt, d), fmt, out_dtype)
+        assert torch.all((out.cpu().double() - exact).abs() <= bound), (i, T, V, d, fmt, dtype)
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """No call before it has loaded a kernel or asked the device anything."""
+    import os
+    import subprocess
+    import sys
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import sys; sys.path.insert(0, %r)
+import torch
+import paper_2511_02620_b200 as difr
+x = torch.randn(40, 96, device="cuda").bfloat16(); w = torch.ones(96, dtype=torch.bfloat16, device="cuda")
+o = difr.NormOut(mx=difr.MxTensor.allocate(40, 96, 4)); W = difr.MxTensor.allocate(300, 96, 4)
+v = torch.randn(300, 96, device="cuda"); out = torch.zeros(40, 300, device="cuda"); back = torch.zeros(300, 96, device="cuda")
+def run():
+    difr.difr_rms_norm(x, w, 1e-6, o); difr.difr_mx_quantize(v, W); difr.difr_mx_logits(o.mx, W, out); difr.difr_mx_dequantize(W, back)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run()
+g.replay(); torch.cuda.synchronize(); a = out.clone(), back.clone(); out.zero_(); back.zero_()
+run(); torch.cuda.synchronize()
+assert torch.equal(a[0], out) and torch.equal(a[1], back) and float(out.abs().max()) > 0
+""" % root
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout + r.stderr
+
+
 def test_outputs_beyond_32_bits():
     """Logits of more than 2^32 values and a matrix of more than 2^32 elements: the last rows are where they belong."""
     T, V, d = 33000, 131072 + 6, 32
