@@ -61,16 +61,23 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
   const int64_t row = (int64_t)blockIdx.x * p.rows_per_cta + in_cta;
   if (row >= p.T) return;  // only where a row is a warp: no barrier is missed
 
+  const X* x = static_cast<const X*>(p.x) + row * p.ldx;
+  const X* res = static_cast<const X*>(p.residual) + row * p.ld_residual;
   Vec8<X> v[VPT];
-  load_row<X, VPT, AL>(v, static_cast<const X*>(p.x) + row * p.ldx, t, tpr, p.d, stage);
-  if (RES) {
-    Vec8<X> r[VPT];
-    load_row<X, VPT, AL>(r, static_cast<const X*>(p.residual) + row * p.ld_residual, t, tpr, p.d, stage);
-    X* to = static_cast<X*>(p.residual_out) + row * p.ld_residual_out;
+  {
+    RowVectors<X, VPT, AL> fx, fr;
+    fetch_row(fx, x, t, tpr, p.d);
+    if (RES) fetch_row(fr, res, t, tpr, p.d);
+    finish_row(v, fx, x, t, tpr, p.d, stage);
+    if (RES) {
+      Vec8<X> r[VPT];
+      finish_row(r, fr, res, t, tpr, p.d, stage);
+      X* to = static_cast<X*>(p.residual_out) + row * p.ld_residual_out;
 #pragma unroll
-    for (int j = 0; j < VPT; ++j) {
-      add_rounded<X>(v[j], r[j]);
-      if (p.residual_out != nullptr) store_row<X, AL>(v[j], to, j * tpr + t, p.d, stage);
+      for (int j = 0; j < VPT; ++j) {
+        add_rounded<X>(v[j], r[j]);
+        if (p.residual_out != nullptr) store_row<X, AL>(v[j], to, j * tpr + t, p.d, stage);
+      }
     }
   }
   float2 acc = make_float2(0.f, 0.f);
@@ -90,6 +97,7 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
     return row_sum(a.x + a.y, part[1], warps);
   });
 
+  const X* w = static_cast<const X*>(p.weight);
   __nv_bfloat16* h = static_cast<__nv_bfloat16*>(p.h) + row * p.ldh;
   const int nvec_mx = FMT ? (int)mx_blocks(p.d) * 4 : 0;
   const int64_t words = FMT ? mx_words(p.d) : 0;
@@ -99,7 +107,9 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
   for (int j = 0; j < VPT; ++j) {
     const int i = j * tpr + t;
     Vec8<X> g[1];
-    load_row<X, 1, AL>(g, static_cast<const X*>(p.weight), i, 0, p.d, stage);
+    RowVectors<X, 1, AL> fg;
+    fetch_row(fg, w, i, 0, p.d);
+    finish_row(g, fg, w, i, 0, p.d, stage);
     float2 y[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {

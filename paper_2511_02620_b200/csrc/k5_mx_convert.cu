@@ -28,7 +28,10 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_quantize(const MxConvertPar
   const int nvec = (int)mx_blocks(p.d) * 4;
   const int vec0 = (int)blockIdx.y * (kCvtElems / 8) + lane;
   Vec8<X> raw[kCvtUnroll];
-  load_row<X, kCvtUnroll, AL>(raw, static_cast<const X*>(p.in) + row * p.ld, vec0, 32, p.d, stage);
+  const X* in = static_cast<const X*>(p.in) + row * p.ld;
+  RowVectors<X, kCvtUnroll, AL> fetched;
+  fetch_row(fetched, in, vec0, 32, p.d);
+  finish_row(raw, fetched, in, vec0, 32, p.d, stage);
 #pragma unroll
   for (int j = 0; j < kCvtUnroll; ++j) {
     const int vec = vec0 + j * 32;

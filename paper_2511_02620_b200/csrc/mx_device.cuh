@@ -8,6 +8,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <string.h>
 
 #include "difr_device.cuh"
 
@@ -215,27 +216,108 @@ __device__ __forceinline__ void Vec8<float>::set_pair(int i, float2 v) {
   set_word(2 * i + 1, __float_as_uint(v.y));
 }
 
+// Rows off the 16-byte boundaries (odd d, odd strides): a warp moves its 256 elements as units that the row's start
+// allows (8, 4 or 2 bytes), neighbouring lanes neighbouring units, and turns them through `stage` (256 elements of its
+// own).  All loads of a thread go out before the first is turned, and only the end of a row is checked element by
+// element (64000 x 4100 in bf16 to 8 bits: 180 us, 212 with one vector and its checks at a time; in place from whole
+// 16-byte pieces by register shifts 209).
+struct RawUnits {
+  uint32_t w[8];  // two, four or eight units of a lane
+};
+template <typename X, typename U>
+__device__ __forceinline__ void fetch_units(RawUnits& raw, const X* from, int lane) {
+  constexpr int kUnits = 8 * (int)sizeof(X) / (int)sizeof(U);
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) {
+    const U one = reinterpret_cast<const U*>(from)[k * 32 + lane];
+    if constexpr (sizeof(U) == 8) {
+      raw.w[2 * k] = one.x;
+      raw.w[2 * k + 1] = one.y;
+    } else if constexpr (sizeof(U) == 4) {
+      raw.w[k] = *reinterpret_cast<const uint32_t*>(&one);
+    } else {
+      raw.w[k] = *reinterpret_cast<const uint16_t*>(&one);
+    }
+  }
+}
+template <typename X, typename U>
+__device__ __forceinline__ void place_units(const RawUnits& raw, X* to, int lane) {
+  constexpr int kUnits = 8 * (int)sizeof(X) / (int)sizeof(U);
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) {
+    if constexpr (sizeof(U) == 8)
+      reinterpret_cast<uint2*>(to)[k * 32 + lane] = make_uint2(raw.w[2 * k], raw.w[2 * k + 1]);
+    else if constexpr (sizeof(U) == 4)
+      reinterpret_cast<uint32_t*>(to)[k * 32 + lane] = raw.w[k];
+    else
+      reinterpret_cast<uint16_t*>(to)[k * 32 + lane] = (uint16_t)raw.w[k];
+  }
+}
+// The units a warp moves its 256 elements e0 .. by: 8, 4 or 2 bytes, 0 for single elements with a check each (the end of
+// a row).  The same in all lanes.
+template <typename X>
+__device__ __forceinline__ int unit_bytes(const X* row, int e0, int d) {
+  if (e0 + 256 > d) return 0;
+  const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(row) & 7u;
+  return at == 0 ? 8 : (at == 4 ? 4 : (int)sizeof(X));
+}
+
 // Vectors vec0 + j stride (j < N) of a row of d elements, one per lane, zeros past its end; vec0 - lane is the same in
-// all lanes.  AL: the row starts on a 16-byte boundary and d is a multiple of 8.  Otherwise (odd d, odd strides) the warp
-// reads its 256 elements one per lane, 32 neighbours at a time, and turns them through `stage` (256 elements of its own).
+// all lanes.  AL: the row starts on a 16-byte boundary and d is a multiple of 8.  In two steps, so that a caller can
+// start more rows before it needs the first: fetch_row, then finish_row.
 template <typename X, int N, bool AL>
-__device__ __forceinline__ void load_row(Vec8<X> (&v)[N], const X* row, int vec0, int stride, int d, X* stage) {
+struct RowVectors {
+  Vec8<X> v[AL ? N : 1];
+  RawUnits raw[AL ? 1 : N];
+};
+template <typename X, int N, bool AL>
+__device__ __forceinline__ void fetch_row(RowVectors<X, N, AL>& f, const X* row, int vec0, int stride, int d) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int i = vec0 + j * stride;
+    if constexpr (AL) {
+      if (i * 8 < d) f.v[j].load(row + i * 8); else f.v[j].zero();
+    } else {
+      const int e0 = (i - lane) * 8;
+      const int bytes = unit_bytes(row, e0, d);
+      if (bytes == 8) {
+        fetch_units<X, uint2>(f.raw[j], row + e0, lane);
+      } else if (bytes == 4) {
+        fetch_units<X, uint32_t>(f.raw[j], row + e0, lane);
+      } else if (sizeof(X) == 2 && bytes == 2) {
+        fetch_units<X, X>(f.raw[j], row + e0, lane);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int e = e0 + k * 32 + lane;
+          const X one = e < d ? row[e] : from_float<X>(0.f);
+          if constexpr (sizeof(X) == 4)
+            f.raw[j].w[k] = *reinterpret_cast<const uint32_t*>(&one);
+          else
+            f.raw[j].w[k] = *reinterpret_cast<const uint16_t*>(&one);
+        }
+      }
+    }
+  }
+}
+template <typename X, int N, bool AL>
+__device__ __forceinline__ void finish_row(Vec8<X> (&v)[N], const RowVectors<X, N, AL>& f, const X* row, int vec0,
+                                           int stride, int d, X* stage) {
   if constexpr (AL) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = vec0 + j * stride;
-      if (i * 8 < d) v[j].load(row + i * 8); else v[j].zero();
-    }
+    for (int j = 0; j < N; ++j) v[j] = f.v[j];
   } else {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int e0 = (vec0 - lane + j * stride) * 8 + lane;
-      X one[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) one[k] = e0 + k * 32 < d ? row[e0 + k * 32] : from_float<X>(0.f);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) stage[k * 32 + lane] = one[k];
+      const int bytes = unit_bytes(row, (vec0 + j * stride - lane) * 8, d);
+      if (bytes == 8)
+        place_units<X, uint2>(f.raw[j], stage, lane);
+      else if (bytes == 4 && sizeof(X) == 2)
+        place_units<X, uint32_t>(f.raw[j], stage, lane);
+      else
+        place_units<X, X>(f.raw[j], stage, lane);  // (fp32: the same units as for 4 bytes)
       __syncwarp();
       v[j].load(stage + lane * 8);
       __syncwarp();
@@ -249,12 +331,23 @@ __device__ __forceinline__ void store_row(const Vec8<X>& v, X* row, int vec, int
     if (vec * 8 < d) v.store(row + vec * 8);
   } else {
     const int lane = threadIdx.x & 31;
+    const int e0 = (vec - lane) * 8;
+    const int bytes = unit_bytes(row, e0, d);
+    RawUnits raw;
     v.store(stage + lane * 8);
     __syncwarp();
+    if (bytes == 8) {
+      fetch_units<X, uint2>(raw, stage, lane);
+      place_units<X, uint2>(raw, row + e0, lane);
+    } else if (bytes == 4) {
+      fetch_units<X, uint32_t>(raw, stage, lane);
+      place_units<X, uint32_t>(raw, row + e0, lane);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int e = (vec - lane) * 8 + k * 32 + lane;
-      if (e < d) row[e] = stage[k * 32 + lane];
+      for (int k = 0; k < 8; ++k) {
+        const int at = k * 32 + lane;
+        if (e0 + at < d) row[e0 + at] = stage[at];
+      }
     }
     __syncwarp();
   }
