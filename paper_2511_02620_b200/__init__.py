@@ -529,25 +529,27 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     dtype, ldx, device = _matrix(x, "x", _ANY_DTYPE)
     shape = x.shape
     if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
-            or weight.shape != shape[1:] or not weight.is_contiguous()):
+            or weight.dim() != 1 or weight.numel() != shape[1] or not weight.is_contiguous()):
         raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {x.device}")
-    c = _CNormOut()
-    ldr = 0
+    residual_p = stream_p = h_p = codes_p = scales_p = None
+    ldr = ld_stream = ldh = fmt = 0
     if residual is not None:
         ldr = _matrix(residual, "residual", (dtype,), shape, device)[1]
+        residual_p = residual.data_ptr()
     if out.residual is not None:
-        c.ld_residual = _matrix(out.residual, "out.residual", (dtype,), shape, device)[1]
-        c.residual = out.residual.data_ptr()
+        ld_stream = _matrix(out.residual, "out.residual", (dtype,), shape, device)[1]
+        stream_p = out.residual.data_ptr()
     if out.h is not None:
-        c.ldh = _matrix(out.h, "out.h", (DIFR_BF16,), shape, device)[1]
-        c.h = out.h.data_ptr()
-    if out.mx is not None:
-        _check_mx(out.mx, "out.mx", device)
-        if (out.mx.rows, out.mx.d) != shape:
-            raise TypeError(f"out.mx is {out.mx.rows} x {out.mx.d}, x {tuple(shape)}")
-        c.mx_format, c.codes, c.scales = out.mx.format, out.mx.codes.data_ptr(), out.mx.scales.data_ptr()
-    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
-          weight.data_ptr(), dtype, shape[0], shape[1], eps, ctypes.byref(c))
+        ldh = _matrix(out.h, "out.h", (DIFR_BF16,), shape, device)[1]
+        h_p = out.h.data_ptr()
+    mx = out.mx
+    if mx is not None:
+        _check_mx(mx, "out.mx", device)
+        if (mx.rows, mx.d) != shape:
+            raise TypeError(f"out.mx is {mx.rows} x {mx.d}, x {tuple(shape)}")
+        fmt, codes_p, scales_p = mx.format, mx.codes.data_ptr(), mx.scales.data_ptr()
+    c = _CNormOut(stream_p, ld_stream, h_p, ldh, fmt, codes_p, scales_p)
+    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, residual_p, ldr, weight.data_ptr(), dtype, shape[0], shape[1], eps, ctypes.byref(c))
     return out
 
 

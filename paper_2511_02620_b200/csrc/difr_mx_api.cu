@@ -237,6 +237,9 @@ difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void
   if (group < 1) group = 1;
   if (group > n_tt) group = n_tt;
   p.group = (int)group;
+  // W is read once where there is one token tile; one that L2 cannot keep for the next call either (96 of its 126 MB) goes
+  // by it (48 tokens, 151936 x 2048 in 8 bits: 51.6 us, 56.5 otherwise; a 65 MB head loses by it, 13.9 us for 11.0)
+  p.w_once = n_tt == 1 && V * pitch > ((int64_t)96 << 20);
   p.pack_pairs = dtype == DIFR_BF16 && ld % 2 == 0 && aligned_to(logits, 4);
   p.tile_stores = bn == 256 && vector_rows(logits, ld, dtype) && ld <= ((int64_t)1 << 36);
   const int words = format == DIFR_MX8 ? 1 : 2;

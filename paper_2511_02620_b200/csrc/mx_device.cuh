@@ -446,6 +446,12 @@ __device__ __forceinline__ uint64_t l2_policy_evict_first() {
   return pol;
 }
 
+// Programmatic launches: a kernel may be made ready while the one before it in the stream still runs; it reads and
+// writes memory only behind grid_wait(), which returns once that kernel has completed.  grid_release() lets the next one
+// be made ready.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Copies one scale word (32 lanes x 16 bytes, in each CTA of the pair from its own shared memory) to four TMEM
 // columns, repeated in all four lane quarters.  Issued by the thread that issues the MMAs; a following MMA sees it.
 __device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t sdesc) {

@@ -51,6 +51,7 @@ struct MxLogitsParams {
   int n_tiles;
   int shift;             // of the deal, per round
   bool pack_pairs;       // bf16 logits, plain stores: two neighbouring ids leave in one 4-byte store
+  bool w_once;           // one token tile, and a W that does not fit L2: its rows need not stay there
   bool tile_stores;      // the rows of the logits start on 16-byte boundaries: tiles leave by TMA (256-token tiles only)
 };
 constexpr int kMxPairM = 256;  // vocabulary ids per tile of a CTA pair
