@@ -23,10 +23,11 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_quantize(const MxConvertPar
   X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : warp * 256);
   const int64_t row = (int64_t)blockIdx.x * kCvtWarps + warp;
   if (row >= p.rows) return;
-  unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d);
-  const int64_t words = mx_words(p.d);
   const int nvec = (int)mx_blocks(p.d) * 4;
   const int vec0 = (int)blockIdx.y * (kCvtElems / 8) + lane;
+  // (a lane's places for its first vector; the others are 32 vectors, two words of scales, further on each time)
+  unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d) + (int64_t)vec0 * FMT;
+  unsigned char* scales = p.scales + mx_scale_offset(row, vec0 >> 4, mx_words(p.d));
   Vec8<X> raw[kCvtUnroll];
   const X* in = static_cast<const X*>(p.in) + row * p.ld;
   RowVectors<X, kCvtUnroll, AL> fetched;
@@ -44,10 +45,10 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_quantize(const MxConvertPar
     const uint32_t word = mx_quantize8<FMT>(v, past, c);
     if (!past) {
       if (FMT == kMx8)
-        *reinterpret_cast<uint2*>(codes + (int64_t)vec * 8) = make_uint2(c[0], c[1]);
+        *reinterpret_cast<uint2*>(codes + j * 32 * FMT) = make_uint2(c[0], c[1]);
       else
-        *reinterpret_cast<uint32_t*>(codes + (int64_t)vec * 4) = c[0];
-      if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(p.scales + mx_scale_offset(row, vec >> 4, words)) = word;
+        *reinterpret_cast<uint32_t*>(codes + j * 32 * FMT) = c[0];
+      if ((lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + j * 2 * kSfWordBytes) = word;
     }
   }
 }
@@ -60,10 +61,10 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertP
   const int64_t row = (int64_t)blockIdx.x * kCvtWarps + warp;
   if (row >= p.rows) return;
   X* out = static_cast<X*>(p.out) + row * p.ld;
-  const unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d);
-  const int64_t words = mx_words(p.d);
   const int nvec = (p.d + 7) / 8;
   const int vec0 = (int)blockIdx.y * (kCvtElems / 8) + lane;
+  const unsigned char* codes = p.codes + row * mx_pitch_bytes(FMT, p.d) + (int64_t)vec0 * FMT;
+  const unsigned char* scales = p.scales + mx_scale_offset(row, vec0 >> 4, mx_words(p.d)) + ((vec0 >> 2) & 3);
   uint2 c[kCvtUnroll];
   uint32_t byte[kCvtUnroll];
 #pragma unroll
@@ -73,10 +74,10 @@ __global__ void __launch_bounds__(kCvtWarps * 32) mx_dequantize(const MxConvertP
     byte[j] = 0u;
     if (vec < nvec) {  // (codes run to whole blocks: eight of them are always there)
       if (FMT == kMx8)
-        c[j] = *reinterpret_cast<const uint2*>(codes + (int64_t)vec * 8);
+        c[j] = *reinterpret_cast<const uint2*>(codes + j * 32 * FMT);
       else
-        c[j].x = *reinterpret_cast<const uint32_t*>(codes + (int64_t)vec * 4);
-      byte[j] = p.scales[mx_scale_offset(row, vec >> 4, words) + ((vec >> 2) & 3)];
+        c[j].x = *reinterpret_cast<const uint32_t*>(codes + j * 32 * FMT);
+      byte[j] = scales[j * 2 * kSfWordBytes];
     }
   }
 #pragma unroll

@@ -43,10 +43,12 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits) {
 __device__ __forceinline__ float mx_inverse_scale(uint32_t byte) {
   return byte == 255u ? 0.f : __uint_as_float((254u - byte) << 23);
 }
-// 2^(byte - 127); NaN for 255.
+// 2^(byte - 127); NaN for 255 (whose bits would be infinity's).
 __device__ __forceinline__ float mx_scale_value(uint32_t byte) {
-  return byte == 255u ? __uint_as_float(0x7FC00000u) : byte == 0u ? __uint_as_float(0x00400000u)
-                                                                 : __uint_as_float(byte << 23);
+  uint32_t bits = byte << 23;
+  if (byte == 0u) bits = 0x00400000u;
+  if (byte == 255u) bits = 0x7FC00000u;
+  return __uint_as_float(bits);
 }
 
 // Rounding to the formats: nearest, ties to even, magnitudes above the largest become the largest.
