@@ -426,23 +426,26 @@ class NormOut:
     mx: MxTensor = None
 
 
-_DTYPES = {}  # torch dtype -> difr_dtype
+_torch = None  # the module, once a call has needed it (an import statement costs each call a quarter of a microsecond)
+_DTYPES = {}   # torch dtype -> difr_dtype
 _ANY_DTYPE, _WIDE_DTYPE = (DIFR_BF16, DIFR_F16, DIFR_F32), (DIFR_BF16, DIFR_F32)
 
 
-def _dtypes():
-    if not _DTYPES:
-        import torch
+def _load_torch():
+    global _torch
+    import torch
 
-        _DTYPES.update({torch.bfloat16: DIFR_BF16, torch.float16: DIFR_F16, torch.float32: DIFR_F32})
-    return _DTYPES
+    _DTYPES.update({torch.bfloat16: DIFR_BF16, torch.float16: DIFR_F16, torch.float32: DIFR_F32})
+    _torch = torch
 
 
 def _matrix(t, name, dtypes, shape=None, device=None):
     """A CUDA matrix whose rows are contiguous; returns (C dtype, row stride, device index)."""
+    if _torch is None:
+        _load_torch()
     try:
         index = t.get_device()
-        code = _dtypes().get(t.dtype)
+        code = _DTYPES.get(t.dtype)
         rows, cols = t.shape
         ld, step = t.stride()
     except (AttributeError, ValueError):
@@ -471,9 +474,7 @@ def _check_mx(mx, name, device):
 
 
 def _check_bytes(t, n, name, what, device):
-    import torch
-
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous():
+    if not isinstance(t, _torch.Tensor) or t.dtype != _torch.uint8 or t.numel() != n or not t.is_contiguous():
         raise TypeError(f"{name}.{what} must be {n} contiguous bytes (uint8)")
     if t.get_device() != device:
         raise TypeError(f"{name}.{what} is on {t.device}, not on CUDA device {device}")
@@ -481,20 +482,18 @@ def _check_bytes(t, n, name, what, device):
 
 def _call(name, device, stream, *args):
     """Calls an entry point with device number `device` current, on the given stream or that device's current one."""
-    import torch
-
     if stream is None:
         # (the handle alone: building a torch.cuda.Stream costs 2 us a call)
-        raw = torch._C._cuda_getCurrentRawStream(device)
+        raw = _torch._C._cuda_getCurrentRawStream(device)
     elif stream.device.index != device:
         raise TypeError(f"the stream is on {stream.device}, the tensors on CUDA device {device}")
     else:
         raw = stream.cuda_stream
     fn = getattr(_lib or lib(), name)
-    if torch._C._cuda_getDevice() == device:
+    if _torch._C._cuda_getDevice() == device:
         rc = fn(*args, raw)
     else:
-        with torch.cuda.device(device):
+        with _torch.cuda.device(device):
             rc = fn(*args, raw)
     if rc != DIFR_OK:
         raise DifrError(rc, name)
@@ -524,11 +523,9 @@ def difr_mx_dequantize(mx: MxTensor, out, stream=None):
 
 def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> NormOut:
     """Final root-mean-square norm of x (+ residual); `out.h` feeds the scoring calls, `out.mx` difr_mx_logits."""
-    import torch
-
     dtype, ldx, device = _matrix(x, "x", _ANY_DTYPE)
     shape = x.shape
-    if (not isinstance(weight, torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
+    if (not isinstance(weight, _torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
             or weight.dim() != 1 or weight.numel() != shape[1] or not weight.is_contiguous()):
         raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {x.device}")
     residual_p = stream_p = h_p = codes_p = scales_p = None
@@ -549,14 +546,13 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
             raise TypeError(f"out.mx is {mx.rows} x {mx.d}, x {tuple(shape)}")
         fmt, codes_p, scales_p = mx.format, mx.codes.data_ptr(), mx.scales.data_ptr()
     c = _CNormOut(stream_p, ld_stream, h_p, ldh, fmt, codes_p, scales_p)
-    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, residual_p, ldr, weight.data_ptr(), dtype, shape[0], shape[1], eps, ctypes.byref(c))
+    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, residual_p, ldr, weight.data_ptr(), dtype, shape[0],
+          shape[1], eps, ctypes.byref(c))
     return out
 
 
 def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=None):
     """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format."""
-    import torch
-
     dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
     _check_mx(h, "h", device)
     _check_mx(W, "W", device)
@@ -565,7 +561,7 @@ def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=
     if logits.shape != (h.rows, W.rows):
         raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
     if device_status is not None:
-        _check(device_status, torch.int32, (1,), "device_status")
+        _check(device_status, _torch.int32, (1,), "device_status")
         if device_status.get_device() != device:
             raise TypeError(f"device_status is on {device_status.device}, not on CUDA device {device}")
     _call("difr_mx_logits", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
