@@ -10,6 +10,8 @@
 // off the 16-byte boundaries (odd d, odd strides) are turned through shared memory on their way in and out.  The sum
 // runs in an order that only d and T fix (per thread, shuffles, warps in order).  y is rounded once, whatever
 // asks for it: the codes are taken from the fp32 value, not from h.
+// Measured in bf16 with residual, stream and h: 65536 x 2048 161 us, 6.7 TB/s of necessary bytes (238 us while an element
+// cost 45 instructions); 8192 x 5120 56 us; to 8 bits without h 54 us.
 #include <cuda_runtime.h>
 
 #include "mx_device.cuh"
