@@ -489,6 +489,8 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
  * Logits of a head held in 8 or 4 bits: logits[t, v] = h[t, :] . W[v, :] of two microscaled tensors of one format,
  * accumulated in fp32 on the block-scaled tensor cores; `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or
  * DIFR_BF16.  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional.
+ *
+ * In all of these calls a row's results are the same bits whatever other rows the batch holds.
  */
 difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
                            int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,

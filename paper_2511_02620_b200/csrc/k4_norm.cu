@@ -8,7 +8,7 @@
 // result written once: the kernel is bound by those bytes, as long as it spends few instructions per element (elements
 // are kept as they lie in memory, 8 per load, and worked on in pairs).  A row belongs to a group of whole warps; rows
 // off the 16-byte boundaries (odd d, odd strides) are turned through shared memory on their way in and out.  The sum
-// runs in an order that only d and T fix (per thread, shuffles, warps in order).  y is rounded once, whatever
+// runs in an order that the row alone fixes (per thread, shuffles, warps in order).  y is rounded once, whatever
 // asks for it: the codes are taken from the fp32 value, not from h.
 // Measured in bf16 with residual, stream and h: 65536 x 2048 161 us, 6.7 TB/s of necessary bytes (238 us while an element
 // cost 45 instructions); 8192 x 5120 56 us; to 8 bits without h 54 us.
@@ -22,10 +22,9 @@ namespace difr {
 constexpr int kNormMaxThreads = 512;
 
 // Sum over the threads of a row, the same value in all of them.  A row of more than one warp has the CTA to itself.
-// A thread's own terms are few and go in fp32; their sums are joined in fp64, so that the result is the exact sum
-// rounded once, nearly always: values next to a border of the 4-bit format depend on its last bit.
-__device__ __forceinline__ float row_sum(float own, double* part, int warps) {
-  double v = own;
+// Eight terms at a time are added in fp32, their sums in fp64, so that the result is the exact sum rounded once, nearly
+// always: values next to a border of the 4-bit format depend on its last bit.
+__device__ __forceinline__ float row_sum(double v, double* part, int warps) {
 #pragma unroll
   for (int m = 16; m >= 1; m >>= 1) v += shfl_xor_double(v, m);
   if (warps == 1) return (float)v;
@@ -82,22 +81,22 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
       }
     }
   }
-  float2 acc = make_float2(0.f, 0.f);
+  auto squares = [&](float unit) {
+    double sum = 0.0;
 #pragma unroll
-  for (int j = 0; j < VPT; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc = ffma2(v[j].pair(i), v[j].pair(i), acc);
-  const float2 f = row_scale(row_sum(acc.x + acc.y, part[0], warps), p.inv_d, p.eps, [&]() {
-    float2 a = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int j = 0; j < VPT; ++j)
+    for (int j = 0; j < VPT; ++j) {
+      float2 a = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 s = fmul2(v[j].pair(i), make_float2(0x1p-80f, 0x1p-80f));
-        a = ffma2(s, s, a);
+        const float2 e = unit == 1.f ? v[j].pair(i) : fmul2(v[j].pair(i), make_float2(unit, unit));
+        a = ffma2(e, e, a);
       }
-    return row_sum(a.x + a.y, part[1], warps);
-  });
+      sum += (double)(a.x + a.y);
+    }
+    return sum;
+  };
+  const float2 f = row_scale(row_sum(squares(1.f), part[0], warps), p.inv_d, p.eps,
+                             [&]() { return row_sum(squares(0x1p-80f), part[1], warps); });
 
   const X* w = static_cast<const X*>(p.weight);
   __nv_bfloat16* h = static_cast<__nv_bfloat16*>(p.h) + row * p.ldh;
@@ -172,12 +171,11 @@ static void launch_vec(const NormParams& p, unsigned grid, int threads, cudaStre
 
 template <typename X>
 static cudaError_t launch_typed(NormParams p, cudaStream_t stream) {
-  // Vectors per thread: one where there are fewer rows than CTAs to fill the GPU (four 128-thread CTAs per SM), for the
-  // shortest way through a row; otherwise four (fp32: two, the same registers), for more loads in flight and fewer
-  // barriers per byte: T = 16384, d = 4096 in bf16 took 45.9 us at four, 48.3 at two, 47.3 at eight.  Rows that go
-  // through shared memory need the registers for that: one.
+  // Vectors per thread, by the row alone, so that a row's result does not depend on the batch it is in: four (fp32: two,
+  // the same registers), for more loads in flight and fewer barriers per byte: T = 16384, d = 4096 in bf16 took 45.9 us
+  // at four, 48.3 at two, 47.3 at eight.  Rows that go through shared memory need the registers for that: one.
   const int nvec = (p.d + 127) / 128 * 16;  // to whole scale words
-  int vpt = p.T < 592 || !p.vec ? 1 : sizeof(X) == 4 ? 2 : 4;
+  int vpt = !p.vec ? 1 : sizeof(X) == 4 ? 2 : 4;
   while (vpt > 1 && nvec <= 32 * vpt / 2) vpt /= 2;
   while ((nvec + vpt - 1) / vpt > kNormMaxThreads) vpt *= 2;
   p.threads_per_row = ((nvec + vpt - 1) / vpt + 31) / 32 * 32;

@@ -7,8 +7,7 @@
 //
 // The vocabulary is the MMA's M side and the tokens its N side: N goes from 16 (a decoding step, bound by the bytes of
 // W) to 256 (re-scoring a batch, bound by the tensor pipe or by the logits' bytes), and a lane of the accumulator is a
-// vocabulary id, so the 32 lanes of a warp store 32 neighbouring logits of one token at a time without a detour
-// through shared memory.
+// vocabulary id, so the 32 lanes of a warp hold 32 neighbouring logits of one token at a time.
 //
 // CTAs run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads its own 128 rows of W
 // and half of the tile's tokens, and the pair's first CTA issues the MMAs.  A stage is a slice of 128 bytes of codes

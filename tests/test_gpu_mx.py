@@ -594,6 +594,25 @@ def test_repeated_calls_give_the_same_bits():
             assert all(torch.equal(p, q) for p, q in zip(now, first))
 
 
+@pytest.mark.parametrize("fmt", [4, 8])
+def test_a_row_does_not_depend_on_its_batch(fmt):
+    """The same rows alone, in small and in large batches: the same bits from the norm and from the product."""
+    d, V = 1504, 3000
+    x, r = randn(2000, d, seed=1).bfloat16().cuda(), randn(2000, d, seed=2, std=2.0).bfloat16().cuda()
+    w = (1 + 0.1 * randn(d, seed=3)).bfloat16().cuda()
+    W = difr.difr_mx_quantize(randn(V, d, seed=4).cuda(), difr.MxTensor.allocate(V, d, fmt))
+
+    def run(T):
+        o = difr.NormOut(h=torch.empty(T, d, dtype=torch.bfloat16, device="cuda"), mx=difr.MxTensor.allocate(T, d, fmt))
+        difr.difr_rms_norm(x[:T], w, 1e-6, o, residual=r[:T])
+        return o.h, o.mx.codes, difr.difr_mx_logits(o.mx, W, torch.empty(T, V, device="cuda"))
+
+    full = run(2000)
+    for T in (1, 2, 17, 33, 65, 129, 300, 700):
+        for part, whole in zip(run(T), full):
+            assert torch.equal(part, whole[:T]), T
+
+
 def test_empty_batches():
     d, V = 64, 300
     x = torch.empty(0, d, device="cuda")
