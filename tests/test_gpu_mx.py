@@ -272,7 +272,8 @@ def logits_bound(h, W, fmt, out_dtype):
 
 @pytest.mark.parametrize("fmt", [4, 8])
 @pytest.mark.parametrize("T,d,V", [(1, 256, 256), (16, 128, 512), (32, 512, 300), (64, 4096, 257), (128, 96, 1000),
-                                   (256, 256, 256), (300, 1749, 515), (513, 640, 2049)])
+                                   (256, 256, 256), (300, 1749, 515), (513, 640, 2049), (300, 1749, 5000), (513, 640, 4200),
+                                   (200, 4096, 9800)])
 def test_logits_of_small_integers_are_exact(T, d, V, fmt):
     """Codes that are small multiples of 1/2 under scales 1/2 .. 2: every partial sum fits fp32, so any error is a
     misplaced code or scale."""
@@ -302,7 +303,7 @@ def test_logits_of_small_integers_are_exact(T, d, V, fmt):
 @pytest.mark.parametrize("fmt", [4, 8])
 @pytest.mark.parametrize("out_dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,d,V", [(1, 1, 1), (1, 32, 31), (2, 4096, 1003), (17, 2080, 777), (40, 64, 256), (100, 992, 3001),
-                                   (129, 1000, 511), (260, 5120, 1025), (1000, 333, 4097)])
+                                   (129, 1000, 511), (260, 5120, 1025), (1000, 333, 4097), (129, 1000, 9731), (260, 2048, 4999)])
 def test_logits(T, d, V, out_dtype, fmt):
     h, hv = random_mx(T, d, fmt, seed=d, exponents=(-6, 3))
     W, Wv = random_mx(V, d, fmt, seed=V, exponents=(-12, -3))
@@ -318,7 +319,7 @@ def test_logits(T, d, V, out_dtype, fmt):
 @pytest.mark.parametrize("fmt", [4, 8])
 @pytest.mark.parametrize("out_dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,V,ld", [(3, 300, 300), (140, 520, 528), (300, 1000, 1008), (300, 1001, 1001), (530, 777, 800),
-                                    (257, 130, 131)])
+                                    (257, 130, 131), (300, 5000, 5008), (300, 5001, 5001), (530, 4097, 4104), (257, 4998, 5000)])
 def test_logits_rows_of_a_wider_matrix(T, V, ld, out_dtype, fmt):
     """Row strides that do and do not allow tile stores; nothing is written behind a row or behind the last one."""
     d = 160
@@ -333,21 +334,22 @@ def test_logits_rows_of_a_wider_matrix(T, V, ld, out_dtype, fmt):
 
 
 @pytest.mark.parametrize("T", [15, 16, 17, 31, 33, 63, 65, 127, 129, 255, 257, 272, 384, 511, 512, 769])
-def test_logits_at_the_borders_of_token_tiles(T):
+@pytest.mark.parametrize("V", [1100, 10000])  # few tiles and many: 128 and 256 tokens per tile
+def test_logits_at_the_borders_of_token_tiles(T, V):
     for fmt in (4, 8):
         h, hv = random_mx(T, 96, fmt, seed=T)
-        W, Wv = random_mx(1100, 96, fmt, seed=T + 1)
-        out = torch.full((T, 1100), math.nan, device="cuda")
+        W, Wv = random_mx(V, 96, fmt, seed=T + 1)
+        out = torch.full((T, V), math.nan, device="cuda")
         difr.difr_mx_logits(h, W, out)
         exact, bound = logits_bound(hv, Wv, fmt, torch.float32)
         assert torch.all((out.cpu().double() - exact).abs() <= bound)
 
 
 @pytest.mark.parametrize("fmt", [4, 8])
-@pytest.mark.parametrize("T", [1, 200])
-def test_broken_blocks_make_their_logits_nan(T, fmt):
+@pytest.mark.parametrize("T,V", [(1, 700), (200, 700), (200, 9800)])
+def test_broken_blocks_make_their_logits_nan(T, V, fmt):
     """A NaN or an infinity in a hidden state makes its row NaN, one in the head its column; the rest is untouched."""
-    d, V = 200, 700
+    d = 200
     x, w = randn(T, d, seed=8), randn(V, d, seed=9)
     w[13, 199], w[600, 0] = math.inf, math.nan
     if T > 1:
@@ -686,7 +688,8 @@ def test_logits_at_every_alignment_of_their_rows(out_dtype, fmt):
     dt = DTYPES[out_dtype]
     T, d = 261, 64
     h, hv = random_mx(T, d, fmt, seed=1)
-    for k, (V, pad) in enumerate([(256, 0), (257, 0), (383, 1), (385, 2), (130, 3), (255, 5), (512, 7), (640, 1), (769, 0)]):
+    for k, (V, pad) in enumerate([(256, 0), (257, 0), (383, 1), (385, 2), (130, 3), (255, 5), (512, 7), (640, 1), (769, 0),
+                                  (5120, 0), (5121, 0), (4991, 1), (4993, 2), (5119, 5), (4866, 6)]):
         W, Wv = random_mx(V, d, fmt, seed=2 + k)
         exact, bound = logits_bound(hv, Wv, fmt, dt)
         for off in (0, 1, 3, 6):
