@@ -762,6 +762,18 @@ def time_variants(difr, h, W, tokens, seeds, pos, temperature, sigma, T, d, V, i
         "score_ipt_filtered_k1000": lambda: difr.difr_score_ipt_filtered(h, W, tokens, seeds, pos, temperature,
                                                                         1000, 1.0, out),
     }
+    # the final norm that makes h, and the same head held in 8 and 4 bits, on up to 4096 rows (their logits are stored)
+    rows = min(T, 4096)
+    x, gain = h[:rows].clone(), torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    stream, logits = torch.zeros_like(x), torch.empty((rows, V), dtype=torch.bfloat16, device="cuda")
+    calls["rms_norm_4096_rows"] = lambda: difr.difr_rms_norm(x, gain, 1e-6, difr.NormOut(h=x, residual=stream),
+                                                             residual=stream)
+    for fmt, bits in ((difr.DIFR_MX8, "8"), (difr.DIFR_MX4, "4")):
+        hq, Wq = difr.MxTensor.allocate(rows, d, fmt), difr.MxTensor.allocate(V, d, fmt)
+        difr.difr_rms_norm(h[:rows], gain, 1e-6, difr.NormOut(mx=hq))
+        calls[f"mx_quantize_head_{bits}_bits"] = lambda Wq=Wq: difr.difr_mx_quantize(W, Wq)
+        calls[f"mx_logits_{bits}_bits_4096_rows"] = lambda hq=hq, Wq=Wq: difr.difr_mx_logits(hq, Wq, logits,
+                                                                                             out.device_status)
     res = {}
     calls["score_gm"]()
     for name, fn in calls.items():
