@@ -398,7 +398,7 @@ def difr_mx_scales_bytes(rows: int, d: int) -> int:
     return int(lib().difr_mx_scales_bytes(rows, d))
 
 
-@dataclass
+@dataclass(slots=True)
 class MxTensor:
     """A microscaled tensor of `rows` x `d` values (layout in include/difr.h)."""
     codes: "object"   # uint8 [rows, pitch bytes]
@@ -418,7 +418,7 @@ class MxTensor:
                         torch.zeros(difr_mx_scales_bytes(rows, d), dtype=torch.uint8, device=device), format, rows, d)
 
 
-@dataclass
+@dataclass(slots=True)
 class NormOut:
     """Output tensors of difr_rms_norm (mirrors `difr_norm_out`); None: not wanted."""
     h: "object" = None         # bf16 [T, d]

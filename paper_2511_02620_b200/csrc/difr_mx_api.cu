@@ -250,9 +250,10 @@ difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void
   const int words = format == DIFR_MX8 ? 1 : 2;
   CUtensorMap tw, th, th_last, tsw, tsh;
   if (!codes_tmap(&tw, W_codes, format, V, d, 128) || !codes_tmap(&th, h_codes, format, T, d, bn / 2) ||
-      !codes_tmap(&th_last, h_codes, format, T, d, p.last_tokens / 2) ||
       !scales_tmap(&tsw, W_scales, V, d, words, 1) || !scales_tmap(&tsh, h_scales, T, d, words, bn > 128 ? 2 : 1))
     return DIFR_ERR_CUDA;
+  th_last = th;
+  if (p.last_tokens != bn && !codes_tmap(&th_last, h_codes, format, T, d, p.last_tokens / 2)) return DIFR_ERR_CUDA;
   CUtensorMap tout;
   memset(&tout, 0, sizeof tout);
   if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
