@@ -29,8 +29,6 @@
 #include <cuda_runtime.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "difr_kernels.h"
 #include "mx_device.cuh"
 #include "mx_kernels.h"

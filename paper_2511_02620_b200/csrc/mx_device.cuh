@@ -141,14 +141,6 @@ __device__ __forceinline__ uint32_t mx_quantize8(const float2 (&v)[4], bool past
 
 // ---------------------------------------------------------------- element types of inputs and outputs
 template <typename X>
-__device__ __forceinline__ float to_float(X x);
-template <>
-__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <>
-__device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
-template <>
-__device__ __forceinline__ float to_float<float>(float x) { return x; }
-template <typename X>
 __device__ __forceinline__ X from_float(float x);
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
