@@ -210,11 +210,10 @@ __device__ __forceinline__ void Vec8<float>::set_pair(int i, float2 v) {
   set_word(2 * i + 1, __float_as_uint(v.y));
 }
 
-// Rows off the 16-byte boundaries (odd d, odd strides): a warp moves its 256 elements as units that the row's start
-// allows (8, 4 or 2 bytes), neighbouring lanes neighbouring units, and turns them through `stage` (256 elements of its
-// own).  All loads of a thread go out before the first is turned, and only the end of a row is checked element by
-// element (64000 x 4100 in bf16 to 8 bits: 180 us, 212 with one vector and its checks at a time; in place from whole
-// 16-byte pieces by register shifts 209).
+// Rows off the 16-byte boundaries (odd d, odd strides).  16-bit rows on 8 or 4 bytes are read and written by lanes that
+// hold eight neighbours each (norm of 20000 x 4100 with all outputs 186 us, 226 by way of shared memory).  Others a warp
+// moves as units that the row's start allows, neighbouring lanes neighbouring units, and turns its 256 elements through
+// `stage`; only the end of a row is checked element by element.  All loads of a thread go out before the first is turned.
 struct RawUnits {
   uint32_t w[8];  // two, four or eight units of a lane
 };
@@ -247,6 +246,47 @@ __device__ __forceinline__ void place_units(const RawUnits& raw, X* to, int lane
       reinterpret_cast<uint16_t*>(to)[k * 32 + lane] = (uint16_t)raw.w[k];
   }
 }
+// 16-bit rows on 8 or 4 bytes need no turning: a lane's eight elements are two or four units of its own.
+template <typename X>
+__device__ __forceinline__ int direct_bytes(const X* row) {  // 0: not such a row
+  const uint32_t at = (uint32_t)reinterpret_cast<uintptr_t>(row) & 7u;
+  return sizeof(X) != 2 ? 0 : at == 0 ? 8 : at == 4 ? 4 : 0;
+}
+template <typename X>
+__device__ __forceinline__ void fetch_direct(RawUnits& raw, const X* from, int n, int bytes) {  // n elements are there
+  if (n >= 8) {
+    if (bytes == 8) {
+      const uint2 a = reinterpret_cast<const uint2*>(from)[0], b = reinterpret_cast<const uint2*>(from)[1];
+      raw.w[0] = a.x; raw.w[1] = a.y; raw.w[2] = b.x; raw.w[3] = b.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw.w[i] = reinterpret_cast<const uint32_t*>(from)[i];
+    }
+  } else {
+    const uint16_t* one = reinterpret_cast<const uint16_t*>(from);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      raw.w[i] = (2 * i < n ? one[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)one[2 * i + 1] << 16 : 0u);
+  }
+}
+template <typename X>
+__device__ __forceinline__ void store_direct(const Vec8<X>& v, X* to, int n, int bytes) {
+  if (n >= 8) {
+    if (bytes == 8) {
+      reinterpret_cast<uint2*>(to)[0] = make_uint2(v.word(0), v.word(1));
+      reinterpret_cast<uint2*>(to)[1] = make_uint2(v.word(2), v.word(3));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(to)[i] = v.word(i);
+    }
+  } else {
+    uint16_t* one = reinterpret_cast<uint16_t*>(to);
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < n) one[i] = (uint16_t)(v.word(i >> 1) >> (16 * (i & 1)));
+  }
+}
+
 // The units a warp moves its 256 elements e0 .. by: 8, 4 or 2 bytes, 0 for single elements with a check each (the end of
 // a row).  The same in all lanes.
 template <typename X>
@@ -274,8 +314,11 @@ __device__ __forceinline__ void fetch_row(RowVectors<X, N, AL>& f, const X* row,
       if (i * 8 < d) f.v[j].load(row + i * 8); else f.v[j].zero();
     } else {
       const int e0 = (i - lane) * 8;
+      const int direct = direct_bytes(row);
       const int bytes = unit_bytes(row, e0, d);
-      if (bytes == 8) {
+      if (sizeof(X) == 2 && direct != 0) {
+        fetch_direct<X>(f.raw[j], row + i * 8, d - i * 8, direct);
+      } else if (bytes == 8) {
         fetch_units<X, uint2>(f.raw[j], row + e0, lane);
       } else if (bytes == 4) {
         fetch_units<X, uint32_t>(f.raw[j], row + e0, lane);
@@ -305,6 +348,11 @@ __device__ __forceinline__ void finish_row(Vec8<X> (&v)[N], const RowVectors<X, 
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
+      if (sizeof(X) == 2 && direct_bytes(row) != 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[j].set_word(k, f.raw[j].w[k]);
+        continue;
+      }
       const int bytes = unit_bytes(row, (vec0 + j * stride - lane) * 8, d);
       if (bytes == 8)
         place_units<X, uint2>(f.raw[j], stage, lane);
@@ -325,6 +373,10 @@ __device__ __forceinline__ void store_row(const Vec8<X>& v, X* row, int vec, int
     if (vec * 8 < d) v.store(row + vec * 8);
   } else {
     const int lane = threadIdx.x & 31;
+    if (sizeof(X) == 2 && direct_bytes(row) != 0) {
+      store_direct<X>(v, row + vec * 8, d - vec * 8, direct_bytes(row));
+      return;
+    }
     const int e0 = (vec - lane) * 8;
     const int bytes = unit_bytes(row, e0, d);
     RawUnits raw;
