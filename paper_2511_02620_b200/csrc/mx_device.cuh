@@ -210,8 +210,8 @@ __device__ __forceinline__ void Vec8<float>::set_pair(int i, float2 v) {
   set_word(2 * i + 1, __float_as_uint(v.y));
 }
 
-// Rows off the 16-byte boundaries (odd d, odd strides).  16-bit rows on 8 or 4 bytes are read and written by lanes that
-// hold eight neighbours each (norm of 20000 x 4100 with all outputs 186 us, 226 by way of shared memory).  Others a warp
+// Rows off the 16-byte boundaries (odd d, odd strides).  16-bit rows on 8 or 4 bytes are read, on 8 bytes written, by lanes
+// that hold eight neighbours each (norm of 20000 x 4100 with all outputs 186 us, 226 by way of shared memory).  Others a warp
 // moves as units that the row's start allows, neighbouring lanes neighbouring units, and turns its 256 elements through
 // `stage`; only the end of a row is checked element by element.  All loads of a thread go out before the first is turned.
 struct RawUnits {
@@ -269,16 +269,13 @@ __device__ __forceinline__ void fetch_direct(RawUnits& raw, const X* from, int n
       raw.w[i] = (2 * i < n ? one[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)one[2 * i + 1] << 16 : 0u);
   }
 }
+// (On 4 bytes four stores a lane, a quarter of every line each, take longer than the turn: 71.6 us against 68.4 for
+// 64000 x 1750 from 8 bits.)
 template <typename X>
-__device__ __forceinline__ void store_direct(const Vec8<X>& v, X* to, int n, int bytes) {
+__device__ __forceinline__ void store_direct(const Vec8<X>& v, X* to, int n) {  // rows on 8 bytes
   if (n >= 8) {
-    if (bytes == 8) {
-      reinterpret_cast<uint2*>(to)[0] = make_uint2(v.word(0), v.word(1));
-      reinterpret_cast<uint2*>(to)[1] = make_uint2(v.word(2), v.word(3));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(to)[i] = v.word(i);
-    }
+    reinterpret_cast<uint2*>(to)[0] = make_uint2(v.word(0), v.word(1));
+    reinterpret_cast<uint2*>(to)[1] = make_uint2(v.word(2), v.word(3));
   } else {
     uint16_t* one = reinterpret_cast<uint16_t*>(to);
 #pragma unroll
@@ -373,8 +370,8 @@ __device__ __forceinline__ void store_row(const Vec8<X>& v, X* row, int vec, int
     if (vec * 8 < d) v.store(row + vec * 8);
   } else {
     const int lane = threadIdx.x & 31;
-    if (sizeof(X) == 2 && direct_bytes(row) != 0) {
-      store_direct<X>(v, row + vec * 8, d - vec * 8, direct_bytes(row));
+    if (sizeof(X) == 2 && direct_bytes(row) == 8) {
+      store_direct<X>(v, row + vec * 8, d - vec * 8);
       return;
     }
     const int e0 = (vec - lane) * 8;

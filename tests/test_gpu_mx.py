@@ -37,7 +37,7 @@ def assert_mx_equal(mx, y, fmt):
 @pytest.mark.parametrize("fmt", [8, 4])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("rows,d", [(1, 1), (1, 32), (3, 31), (5, 33), (2, 100), (129, 128), (130, 1056), (257, 1749),
-                                    (7, 4096), (1, 8192)])
+                                    (9, 70), (20, 1030), (7, 4096), (1, 8192)])
 def test_quantisation_is_bit_exact(rows, d, dtype, fmt):
     x = randn(rows, d, seed=rows + d).to(DTYPES[dtype])
     mx = mx_of(rows, d, fmt)
@@ -102,7 +102,7 @@ def test_extreme_blocks(fmt):
 
 @pytest.mark.parametrize("fmt", [8, 4])
 @pytest.mark.parametrize("out_dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,d,ld", [(1, 1, 1), (3, 31, 40), (129, 256, 256), (70, 1749, 1749), (5, 4096, 4104)])
+@pytest.mark.parametrize("rows,d,ld", [(1, 1, 1), (3, 31, 40), (129, 256, 256), (70, 1749, 1749), (5, 4096, 4104), (9, 70, 70), (20, 1030, 1034)])
 def test_dequantisation_is_exact(rows, d, ld, out_dtype, fmt):
     g = torch.Generator().manual_seed(d)
     nb = (d + 31) // 32
@@ -185,7 +185,7 @@ def assert_mx_nearest(mx, y, fmt):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("fmt", [0, 8, 4])
 @pytest.mark.parametrize("T,d,residual", [(1, 1, False), (1, 4096, True), (3, 100, True), (9, 31, False), (130, 160, True),
-                                          (5, 1749, True), (17, 2048, False), (33, 5120, True), (2, 9001, True),
+                                          (5, 1749, True), (9, 70, True), (7, 1030, True), (17, 2048, False), (33, 5120, True), (2, 9001, True),
                                           (1, 32768, True), (3, 16384, False)])
 def test_norm(T, d, residual, fmt, dtype):
     x = randn(T, d, seed=1).to(DTYPES[dtype])
@@ -208,7 +208,7 @@ def test_norm(T, d, residual, fmt, dtype):
 
 def test_norm_in_place_and_strided():
     """The stream over the residual, h over x; rows of wider matrices, aligned to 16 bytes and not."""
-    for pad, off in ((8, 0), (7, 0), (16, 8), (9, 3)):
+    for pad, off in ((8, 0), (7, 0), (16, 8), (9, 3), (2, 0), (6, 2), (4, 4)):
         T, d = 37, 520
         xb, rb = randn(T, d + pad + off, seed=4).bfloat16(), randn(T, d + pad + off, seed=5).bfloat16()
         w = (1 + 0.1 * randn(d, seed=6)).bfloat16()
