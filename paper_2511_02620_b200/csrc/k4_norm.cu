@@ -36,12 +36,19 @@ __device__ __forceinline__ float row_sum(double v, double* part, int warps) {
 }
 
 // 1 / sqrt(mean + eps) and a factor to apply first.  Squares of values above 1.8e19 leave fp32's range: such a row is
-// measured again in units of 2^80 by `again` (eps no longer counts).  A row with a NaN is NaN throughout; one with an
-// infinity is NaN there and zero elsewhere, as the formula has it.
+// measured again in units of 2^80 by `again`, eps with it (it counts only where it is about as large as such squares).
+// Where eps alone takes the sum out of range, a quarter of both stays inside.  A row with a NaN is NaN throughout; one
+// with an infinity is NaN there and zero elsewhere, as the formula has it.
 template <typename F>
 __device__ __forceinline__ float2 row_scale(float ss, float inv_d, float eps, F again) {
-  if (ss > 3.0e38f) return make_float2(0x1p-80f, rsqrtf(again() * inv_d));
-  return make_float2(1.f, rsqrtf(__fadd_rn(__fmul_rn(ss, inv_d), eps)));  // (the mean is a value of its own: no fma)
+  if (ss > 3.0e38f) {
+    const float unit_eps = eps * 0x1p-80f * 0x1p-80f;
+    return make_float2(0x1p-80f, rsqrtf(__fadd_rn(__fmul_rn(again(), inv_d), unit_eps)));
+  }
+  const float mean = __fmul_rn(ss, inv_d);  // (a value of its own: no fma)
+  const float m = __fadd_rn(mean, eps);
+  if (m > 3.0e38f) return make_float2(1.f, 0.5f * rsqrtf(__fadd_rn(0.25f * mean, 0.25f * eps)));
+  return make_float2(1.f, rsqrtf(m));
 }
 
 // Rounded sum of two vectors.

@@ -699,3 +699,18 @@ def test_logits_at_every_alignment_of_their_rows(out_dtype, fmt):
             assert torch.all((out.cpu().double() - exact).abs() <= bound)
             out.fill_(-7.0)
             assert torch.all(flat == -7.0)
+
+
+# ------------------------------------------------------------------ the ends of fp32's range
+@pytest.mark.parametrize("d", [1, 520, 1001, 32768])
+def test_eps_counts_in_rows_whose_squares_leave_fp32(d):
+    """Any finite eps: as large as squares beyond 3.4e38, and so large that the mean and it leave fp32 together."""
+    scale = torch.tensor([1e-10, 1.0, 1e17, 3e18, 1.7e19, 2e19, 1e21, 1e30, 1e37])
+    x = (0.5 + torch.rand(scale.numel(), d, generator=torch.Generator().manual_seed(d))) * scale.view(-1, 1)
+    x[:, ::2] *= -1
+    w = 1 + 0.2 * randn(d, seed=3)
+    for eps in (1e-6, 1e10, 1e30, 1e34, 1e36, 1e38, 2e38, 3.4e38):
+        h = torch.empty(scale.numel(), d, dtype=torch.bfloat16, device="cuda")
+        difr.difr_rms_norm(x.cuda(), w.cuda(), eps, difr.NormOut(h=h))
+        _, y = ref.rms_norm(x, None, w, eps)
+        assert_close_h(h, y)
