@@ -35,18 +35,19 @@ __device__ __forceinline__ float row_sum(double v, double* part, int warps) {
   return (float)s;
 }
 
-// 1 / sqrt(mean + eps) and a factor to apply first.  Squares of values above 1.8e19 leave fp32's range: such a row is
-// measured again in units of 2^80 by `again`, eps with it (it counts only where it is about as large as such squares).
-// Where eps alone takes the sum out of range, a quarter of both stays inside.  A row with a NaN is NaN throughout; one
-// with an infinity is NaN there and zero elsewhere, as the formula has it.
+// 1 / sqrt(mean + eps) and a factor to apply first.  Squares of values above 1.8e19 leave fp32's range, those of values
+// below 1.1e-19 its normal numbers, which shows where eps is smaller still: such a row is measured by `again` in units of
+// 2^80 or 2^-80, eps with it.  Where eps alone takes the sum out of range, a quarter of both stays inside.  A row with a
+// NaN is NaN throughout; one with an infinity is NaN there and zero elsewhere, as the formula has it.
 template <typename F>
 __device__ __forceinline__ float2 row_scale(float ss, float inv_d, float eps, F again) {
-  if (ss > 3.0e38f) {
-    const float unit_eps = eps * 0x1p-80f * 0x1p-80f;
-    return make_float2(0x1p-80f, rsqrtf(__fadd_rn(__fmul_rn(again(), inv_d), unit_eps)));
-  }
   const float mean = __fmul_rn(ss, inv_d);  // (a value of its own: no fma)
   const float m = __fadd_rn(mean, eps);
+  const bool huge = ss > 3.0e38f;
+  if (huge || m < 0x1p-100f) {
+    const float unit = huge ? 0x1p-80f : 0x1p80f;
+    return make_float2(unit, rsqrtf(__fadd_rn(__fmul_rn(again(unit), inv_d), eps * unit * unit)));
+  }
   if (m > 3.0e38f) return make_float2(1.f, 0.5f * rsqrtf(__fadd_rn(0.25f * mean, 0.25f * eps)));
   return make_float2(1.f, rsqrtf(m));
 }
@@ -103,14 +104,14 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
     return sum;
   };
   const float2 f = row_scale(row_sum(squares(1.f), part[0], warps), p.inv_d, p.eps,
-                             [&]() { return row_sum(squares(0x1p-80f), part[1], warps); });
+                             [&](float unit) { return row_sum(squares(unit), part[1], warps); });
 
   const X* w = static_cast<const X*>(p.weight);
   __nv_bfloat16* h = static_cast<__nv_bfloat16*>(p.h) + row * p.ldh;
   const int nvec_mx = FMT ? (int)mx_blocks(p.d) * 4 : 0;
   unsigned char* scales = p.scales + (FMT ? mx_scale_offset(row, 0, mx_words(p.d)) : 0);
   unsigned char* codes = p.codes + (FMT ? row * mx_pitch_bytes(FMT, p.d) : 0);
-  const bool huge = f.x != 1.f;
+  const bool rescaled = f.x != 1.f;
 #pragma unroll
   for (int j = 0; j < VPT; ++j) {
     const int i = j * tpr + t;
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 8 ? 1 : 2) rms_norm(co
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       float2 a = v[j].pair(k);
-      if (huge) a = fmul2(a, make_float2(f.x, f.x));
+      if (rescaled) a = fmul2(a, make_float2(f.x, f.x));
       y[k] = fmul2(fmul2(a, make_float2(f.y, f.y)), g[0].pair(k));
     }
     if (p.h != nullptr) {

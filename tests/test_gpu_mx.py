@@ -714,3 +714,27 @@ def test_eps_counts_in_rows_whose_squares_leave_fp32(d):
         difr.difr_rms_norm(x.cuda(), w.cuda(), eps, difr.NormOut(h=h))
         _, y = ref.rms_norm(x, None, w, eps)
         assert_close_h(h, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [1, 520, 1001, 9000])
+def test_rows_whose_squares_are_subnormal(d, dtype):
+    """With an eps that is smaller still the formula holds down to the smallest numbers; zero rows stay zero."""
+    scale = torch.tensor([0.0, 1e-44, 1e-40, 1e-30, 1e-24, 1e-22, 1e-21, 1e-20, 1e-19, 1e-15, 1e-10, 1.0])
+    x = (0.5 + torch.rand(scale.numel(), d, generator=torch.Generator().manual_seed(d))) * scale.view(-1, 1)
+    x[:, ::2] *= -1
+    x = x.to(DTYPES[dtype])
+    w = (1 + 0.2 * randn(d, seed=3)).to(DTYPES[dtype])
+    for eps in (1e-45, 1e-42, 1e-40, 1e-36, 1e-31, 1e-29, 1e-6):
+        h = torch.empty(scale.numel(), d, dtype=torch.bfloat16, device="cuda")
+        mx = mx_of(scale.numel(), d, 8)
+        difr.difr_rms_norm(x.cuda(), w.cuda(), eps, difr.NormOut(h=h, mx=mx))
+        _, y = ref.rms_norm(x, None, w, eps)
+        assert_close_h(h, y)
+        assert torch.all(h[0] == 0)
+        keep = y.abs().amax(1) > 1e-30  # (below, y itself is close to fp32's subnormal numbers)
+        got = difr.difr_mx_dequantize(mx, torch.empty(scale.numel(), d, device="cuda")).cpu().double()
+        top = ref.blocks(y).abs().amax(-1, keepdim=True).expand(-1, -1, 32).flatten(1)[:, :d]
+        # e4m3: half a step is 2^-4 of the value, 448 for up to 512 is 2^-3; among its subnormals half a step is 2^-10 of
+        # the scale, which is at most 2^-8 of the block's largest
+        assert torch.all(((got - y).abs() <= (2.0 ** -3 + 2 * Y_ERR) * y.abs() + 2.0 ** -18 * (1 + Y_ERR) * top)[keep])
