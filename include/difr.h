@@ -19,7 +19,7 @@
  *   LM head      difr_rms_norm (the final norm: the h that scoring takes, also in 8 or 4 bits), difr_mx_quantize,
  *                difr_mx_dequantize, difr_mx_logits (a head held in 8 or 4 bits)
  *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes
- *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_debug_plan_override,
+ *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_debug_plan_override,
  *                difr_status_string, difr_version
  *
  * Conventions
@@ -488,7 +488,8 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
 /*
  * Logits of a head held in 8 or 4 bits: logits[t, v] = h[t, :] . W[v, :] of two microscaled tensors of one format,
  * accumulated in fp32 on the block-scaled tensor cores; `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or
- * DIFR_BF16.  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional.
+ * DIFR_BF16.  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional: a wait that
+ * runs out also leaves NaN in the place of every logit that was not computed.
  *
  * In all of these calls a row's results are the same bits whatever other rows the batch holds.
  */
@@ -517,6 +518,17 @@ difr_status difr_philox(const uint32_t* ctr, const uint32_t* key, int64_t n, uin
  * either way and the context stays usable.
  */
 difr_status difr_selftest_wait(int32_t* status2, int64_t limit_cycles, difr_stream_t stream);
+
+/*
+ * Validation aid: difr_mx_logits as it ends when a wait runs out.  Only the first `loaded_tiles` tiles are ever loaded
+ * and waits give up after `limit_cycles` SM clocks (1 .. 1e9): what the loaded tiles hold is computed (as far as the limit
+ * is long enough for it), all other logits are NaN, DIFR_ERR_TIMEOUT is written to device_status, and the context stays
+ * usable.  With as many tiles as there are, or more, and a long limit it is the ordinary call.
+ */
+difr_status difr_selftest_mx_wait(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
+                                  int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype,
+                                  int64_t ld, int64_t loaded_tiles, int64_t limit_cycles, int32_t* device_status,
+                                  difr_stream_t stream);
 
 /*
  * Validation aid: overrides the work planner's choices for every later call of the process (0 = the planner's

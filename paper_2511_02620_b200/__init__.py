@@ -23,7 +23,7 @@ EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_
            "difr_admissible", "difr_exfiltratable_bits", "difr_detect", "difr_expand_seeds", "difr_logits", "difr_philox",
            "difr_mx_codes_bytes", "difr_mx_scales_bytes", "difr_mx_quantize", "difr_mx_dequantize", "difr_rms_norm",
            "difr_mx_logits",
-           "difr_selftest_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
+           "difr_selftest_wait", "difr_selftest_mx_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
 DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
 DIFR_MX8, DIFR_MX4 = 8, 4
@@ -127,6 +127,8 @@ def lib() -> ctypes.CDLL:
         L.difr_rms_norm.argtypes = [v, i64, v, i64, v, i32, i64, i64, ctypes.c_float, ctypes.POINTER(_CNormOut), v]
         L.difr_mx_logits.restype = ctypes.c_int
         L.difr_mx_logits.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, v, v]
+        L.difr_selftest_mx_wait.restype = ctypes.c_int
+        L.difr_selftest_mx_wait.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, i64, i64, v, v]
         _lib = L
     return _lib
 
@@ -551,9 +553,7 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     return out
 
 
-def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=None):
-    """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format."""
-    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
+def _check_product(h, W, logits, device, device_status):
     _check_mx(h, "h", device)
     _check_mx(W, "W", device)
     if h.format != W.format or h.d != W.d:
@@ -564,7 +564,25 @@ def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=
         _check(device_status, _torch.int32, (1,), "device_status")
         if device_status.get_device() != device:
             raise TypeError(f"device_status is on {device_status.device}, not on CUDA device {device}")
+
+
+def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=None):
+    """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format.  A device-side wait that
+    runs out leaves NaN where logits were not computed, and DIFR_ERR_TIMEOUT in `device_status` (int32 [1], optional)."""
+    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
+    _check_product(h, W, logits, device, device_status)
     _call("difr_mx_logits", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
           W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld,
           None if device_status is None else device_status.data_ptr())
+    return logits
+
+
+def difr_selftest_mx_wait(h: MxTensor, W: MxTensor, logits, loaded_tiles: int, limit_cycles: int, device_status=None,
+                          stream=None):
+    """difr_mx_logits that loads `loaded_tiles` tiles only and gives up after `limit_cycles`; see include/difr.h."""
+    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
+    _check_product(h, W, logits, device, device_status)
+    _call("difr_selftest_mx_wait", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
+          W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld, int(loaded_tiles),
+          int(limit_cycles), None if device_status is None else device_status.data_ptr())
     return logits

@@ -169,15 +169,15 @@ struct OutPieces {
 // `shift` pairs, chosen so that the narrower last token tiles reach all pairs alike.
 struct TileWalk {
   const MxLogitsParams& p;
-  const int pair, n_pairs;
+  const int pair, n_pairs, end;
   int round0, turn;  // first tile of the round, pair that is dealt to first
 
-  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n)
-      : p(params), pair(pr), n_pairs(n), round0(0), turn(0) {}
+  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n, int n_tiles)
+      : p(params), pair(pr), n_pairs(n), end(n_tiles), round0(0), turn(0) {}
   __device__ __forceinline__ bool next(int& vt, int& tt) {
     const int at = pair - turn;
     const int i = round0 + (at < 0 ? at + n_pairs : at);
-    if (i >= p.n_tiles) return false;
+    if (i >= end) return false;
     round0 += n_pairs;
     turn += p.shift;
     if (turn >= n_pairs) turn -= n_pairs;
@@ -259,7 +259,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  TileWalk walk(p, pair, n_pairs);
+  TileWalk walk(p, pair, n_pairs, warp == 0 ? p.loaded_tiles : p.n_tiles);
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -277,7 +277,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int w_row = vt * kMxPairM + (int)cta * 128;
       const int h_row = tt * BN + (int)cta * half;
       for (int k = 0; k < p.k_steps; ++k) {
-        if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_cycles))) { ok = false; break; }
         if (elect_one()) {
           if (cta == 0) mbar_arrive_expect_tx(full_bar(stage), 2u * bytes);
           const uint32_t full0 = full0_base + 8u * (uint32_t)stage;
@@ -310,16 +310,19 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         // tile have been read (every epilogue warp had then finished the tile before it).
         if (Tl::overlap) {
           if (n_tile >= 1 && !__all_sync(0xffffffffu, mbar_wait(acc_free_bar(acc ^ 1), ((n_tile - 1) >> 1) & 1u,
-                                                                abort_flag))) { ok = false; break; }
+                                                                abort_flag, p.wait_cycles))) { ok = false; break; }
         } else {
           if (n_tile >= 2 && !__all_sync(0xffffffffu, mbar_wait(acc_free_bar(acc), ((n_tile - 2) >> 1) & 1u,
-                                                                abort_flag))) { ok = false; break; }
+                                                                abort_flag, p.wait_cycles))) { ok = false; break; }
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * Tl::acc_stride);
         uint32_t accumulate = 0;
         for (int k = 0; k < p.k_steps; ++k) {
-          if (!__all_sync(0xffffffffu, mbar_wait_cta(full_bar(stage), phase, full_seen, abort_flag))) { ok = false; break; }
+          if (!__all_sync(0xffffffffu, mbar_wait_cta(full_bar(stage), phase, full_seen, abort_flag, p.wait_cycles))) {
+            ok = false;
+            break;
+          }
           // a look at the next stage: its answer is there by the time it is needed
           {
             const bool wrap = stage + 1 == kStages;
@@ -379,8 +382,9 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     pieces.next = 0;
     pieces.policy = l2_policy_evict_first();
     int vt, tt;
+    bool given_up = false;
     while (walk.next(vt, tt)) {
-      const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
+      const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag, p.wait_cycles);
       __syncwarp();
       tc_fence_after();
       const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
@@ -418,7 +422,8 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         if (Tl::overlap || kLoads == 1) release();
       }
       // (the warps of a half meet at barriers below, so they give up together or not at all)
-      if (BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !ok) break;
+      given_up = BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !__all_sync(0xffffffffu, ok);
+      if (given_up) break;
 #pragma unroll 1
       for (int c = 0; c < kLoads;) {
         const int n_here = c == 0 ? kFirst : 1;
@@ -445,6 +450,23 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (BN == 256 && p.tile_stores) bulk_wait_all();  // the pieces stay until they have left
+    // After a wait that ran out the warp's part of this tile and of the pair's next ones becomes NaN: no caller takes
+    // what the buffer held before for logits.
+    if (given_up) {
+      const OUT nan = from_float<OUT>(__int_as_float(0x7FC00000));
+      do {
+        const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
+#pragma unroll 1
+        for (int i = 0; i < (Tl::chunks + 1) / 2; ++i) {
+          const int ch = epi_chunk<FMT, BN>(i, half, acc);
+          const int t0 = tt * BN + ch * Tl::chunk;
+          if (ch < 0 || v >= p.V) continue;
+#pragma unroll 1
+          for (int t = t0; t < t0 + Tl::chunk && t < p.T; ++t) static_cast<OUT*>(p.logits)[(int64_t)t * p.ld + v] = nan;
+        }
+        acc ^= 1;
+      } while (walk.next(vt, tt));
+    }
   }
 
   __syncwarp();

@@ -426,13 +426,14 @@ __device__ __forceinline__ bool mbar_test_cta(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 // The bounded wait at CTA scope; `seen`: the barrier's phase was already seen to be complete.
-__device__ __forceinline__ bool mbar_wait_cta(uint32_t bar, uint32_t parity, bool seen, volatile int* abort_flag) {
+__device__ __forceinline__ bool mbar_wait_cta(uint32_t bar, uint32_t parity, bool seen, volatile int* abort_flag,
+                                              long long limit_cycles) {
   if (seen || mbar_test_cta(bar, parity)) return true;
   const long long t0 = clock64();
   while (true) {
     if (mbar_test_cta(bar, parity)) return true;
     if (*abort_flag) return false;
-    if (clock64() - t0 > kWaitCycles) {
+    if (clock64() - t0 > limit_cycles) {
       *abort_flag = 1;
       return false;
     }

@@ -49,6 +49,8 @@ struct MxLogitsParams {
   int group;             // token tiles per raster group
   int last_tokens;       // width of the last token tile, a multiple of 16
   int n_tiles;
+  int loaded_tiles;      // n_tiles; fewer (a test of the waits): the tiles from here on are never loaded
+  long long wait_cycles; // after which a wait gives up
   int shift;             // of the deal, per round
   bool pack_pairs;       // bf16 logits, plain stores: two neighbouring ids leave in one 4-byte store
   bool w_once;           // one token tile, and a W that does not fit L2: its rows need not stay there

@@ -738,3 +738,35 @@ def test_rows_whose_squares_are_subnormal(d, dtype):
         # e4m3: half a step is 2^-4 of the value, 448 for up to 512 is 2^-3; among its subnormals half a step is 2^-10 of
         # the scale, which is at most 2^-8 of the block's largest
         assert torch.all(((got - y).abs() <= (2.0 ** -3 + 2 * Y_ERR) * y.abs() + 2.0 ** -18 * (1 + Y_ERR) * top)[keep])
+
+
+# ------------------------------------------------------------------ waits that run out
+@pytest.mark.parametrize("fmt", [4, 8])
+@pytest.mark.parametrize("T,V,ld,out_dtype", [(600, 9800, 9800, "bf16"), (600, 9801, 9801, "f32"), (300, 1100, 1104, "f32"),
+                                              (40, 9800, 9803, "bf16"), (7, 30000, 30000, "f32")])
+def test_logits_that_a_wait_kept_from_being_computed_are_nan(T, V, ld, out_dtype, fmt):
+    """Tiles that are never loaded: their waits give up, their logits are NaN, all others what they should be, the status
+    word says so, and the next call is as good as ever."""
+    d = 160
+    h, _ = random_mx(T, d, fmt, seed=1)
+    W, _ = random_mx(V, d, fmt, seed=2)
+    dt = DTYPES[out_dtype]
+    want = difr.difr_mx_logits(h, W, torch.empty(T, V, dtype=dt, device="cuda"))
+    width = 256 if T > 128 else 16 if T <= 16 else 64
+    if (V + 255) // 256 * ((T + 255) // 256) <= 37 and T > 128:
+        width = 128
+    n_tt = (T + width - 1) // width
+    n = (V + 255) // 256 * n_tt
+    tile = (torch.arange(V, device="cuda") // 256 * n_tt).view(1, -1) + (torch.arange(T, device="cuda") // width).view(-1, 1)
+    for loaded in (0, 1, 5, n - 1, n, n + 7):
+        buf = torch.full((T + 1, ld), -7.0, dtype=dt, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        difr.difr_selftest_mx_wait(h, W, buf[:T, :V], loaded, 2_000_000, status)
+        assert int(status.item()) == (0 if loaded >= n else -7)
+        lost = tile >= loaded
+        assert torch.isnan(buf[:T, :V][lost]).all()
+        assert torch.equal(buf[:T, :V][~lost], want[~lost])
+        assert torch.all(buf[:T, V:] == -7.0) and torch.all(buf[T:] == -7.0)
+        difr.difr_selftest_mx_wait(h, W, buf[:T, :V], loaded, 2_000_000)  # no status word: the logits tell
+        assert torch.equal(torch.isnan(buf[:T, :V]), lost)
+    assert torch.equal(difr.difr_mx_logits(h, W, torch.empty(T, V, dtype=dt, device="cuda")), want)

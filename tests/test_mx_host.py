@@ -85,6 +85,20 @@ def test_refusals_on_the_host():
     assert logits(T=0, hc=None, hs=None) == OK
 
 
+def test_refusals_of_the_wait_self_test():
+    if torch.cuda.is_available():
+        pytest.skip("host-only check")
+    L, p = difr.lib(), 0x10000
+
+    def call(loaded=0, limit=1000, fmt=4, ld=100, hc=p):
+        return L.difr_selftest_mx_wait(hc, p, p, p, fmt, 8, 64, 100, p, 2, ld, loaded, limit, None, None)
+
+    for limit in (0, -1, 1_000_000_001):
+        assert call(limit=limit) == INVALID
+    assert call(loaded=-1) == INVALID
+    assert call(fmt=1) == INVALID and call(ld=99) == INVALID and call(hc=None) == INVALID  # the product's own checks
+
+
 def test_a_well_formed_call_without_a_device_reports_a_cuda_error():
     if torch.cuda.is_available():
         pytest.skip("host-only check")
