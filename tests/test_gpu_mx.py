@@ -770,3 +770,76 @@ def test_logits_that_a_wait_kept_from_being_computed_are_nan(T, V, ld, out_dtype
         difr.difr_selftest_mx_wait(h, W, buf[:T, :V], loaded, 2_000_000)  # no status word: the logits tell
         assert torch.equal(torch.isnan(buf[:T, :V]), lost)
     assert torch.equal(difr.difr_mx_logits(h, W, torch.empty(T, V, dtype=dt, device="cuda")), want)
+
+
+# ------------------------------------------------------------------ long rows, several raster groups, heads beyond L2
+def exact_mx(rows, d, fmt, seed):
+    """Values of the 4-bit format under scales 1/2 .. 2, made on the GPU: (MxTensor, the values it holds exactly)."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c = torch.randint(0, 16, (rows, d), generator=g, device="cuda", dtype=torch.uint8)
+    v = ref.table(4).float().cuda()[(c & 7).int()] * (1 - 2 * (c >> 3).float())
+    e = torch.randint(-1, 2, (rows, (d + 31) // 32), generator=g, device="cuda").float()
+    v *= torch.exp2(e).repeat_interleave(32, 1)[:, :d]
+    mx = difr.difr_mx_quantize(v, difr.MxTensor.allocate(rows, d, fmt))
+    assert torch.equal(difr.difr_mx_dequantize(mx, torch.empty_like(v)), v)
+    return mx, v
+
+
+@pytest.mark.parametrize("T,d,V,fmt", [
+    (1300, 131072, 2500, 4),   # 6 token tiles in groups of 2
+    (1100, 131072, 2500, 4),   # 5: the last group has one
+    (1300, 65536, 2500, 8),
+    (1100, 65537, 2500, 8),
+    (600, 262177, 4100, 4),    # groups of one tile
+    (300, 1 << 20, 700, 4),    # the longest rows, tiles of 128 tokens
+    (300, 1 << 20, 700, 8),
+    (48, 1024, 110000, 8),     # one token tile, heads that L2 does not hold
+    (5, 2048, 120007, 4),
+    (48, 2048, 110001, 8),
+])
+def test_logits_of_long_rows_and_large_heads_are_exact(T, d, V, fmt):
+    """Every product is a multiple of 1/16 and a row's sums stay far below 2^20 (the products' deviation is below 24, and
+    2^20 terms make 2.5e4): each partial sum fits fp32, so any error is a misplaced tile, code or scale."""
+    h, hv = exact_mx(T, d, fmt, seed=1)
+    W, Wv = exact_mx(V, d, fmt, seed=2)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = difr.difr_mx_logits(h, W, torch.full((T, V), math.nan, device="cuda"), status)
+    assert int(status.item()) == 0
+    want = torch.zeros(T, V, dtype=torch.float64, device="cuda")
+    for k in range(0, d, 65536):
+        want += hv[:, k:k + 65536].double() @ Wv[:, k:k + 65536].double().T
+    assert float(want.abs().max()) < 2.0 ** 20
+    assert torch.equal(out.double(), want)
+
+
+# ------------------------------------------------------------------ the norm's steps
+# Relative error of y: a group of eight squares passes four roundings along two chains and one where they meet, the
+# groups are joined in 64 bits; the cast, 1 / d, the mean and + eps make four more; the root halves the nine.  rsqrtf is
+# within 2 units in the last place (four of 2^-24), two products follow: 10.5 of 2^-24, and 0.5 for terms of second order.
+Y_STEPS = 11 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("fmt", [4, 8])
+@pytest.mark.parametrize("T,d,dtype", [(400, 5120, "bf16"), (300, 8192, "f32"), (900, 1749, "f32"), (60, 32768, "bf16")])
+def test_codes_differ_from_the_exact_rows_next_to_a_border_only(T, d, dtype, fmt):
+    """Codes lie between those of y (1 - Y_STEPS) and y (1 + Y_STEPS); rows of one large and many small squares, each
+    lost beside the large one in 32 bits, among them."""
+    x = randn(T, d, seed=1)
+    x[::3] = 2.0 ** -12 * (1 + 0.25 * torch.rand(x[::3].shape, generator=torch.Generator().manual_seed(2)))
+    x[::3, 0] = 1.0
+    x = x.to(DTYPES[dtype])
+    w = (1 + 0.2 * randn(d, seed=3)).to(DTYPES[dtype])
+    mx = mx_of(T, d, fmt)
+    difr.difr_rms_norm(x.cuda(), w.cuda(), 1e-6, difr.NormOut(mx=mx))
+    _, y = ref.rms_norm(x, None, w, 1e-6)
+    nb = (d + 31) // 32
+    byte = ref.untile_scales(mx.scales.cpu(), T, nb)
+    low, high = (ref.quantize(y * f, fmt) for f in (1 - Y_STEPS, 1 + Y_STEPS))
+    assert torch.all((byte == low[1]) | (byte == high[1]))
+    sure = (low[1] == high[1]).unsqueeze(-1).expand(-1, -1, 32).flatten(1)  # (two scales: codes of two grids)
+    assert sure.double().mean() > 0.999
+    mag = 2 ** (fmt - 1) - 1
+    c = ref.unpack(mx.codes.cpu(), fmt)
+    assert torch.equal((c >> (fmt - 1))[sure], (low[0] >> (fmt - 1))[sure])
+    assert torch.all((((c & mag) >= (low[0] & mag)) & ((c & mag) <= (high[0] & mag)))[sure])
+    assert ((low[0] != high[0]) & sure).sum() <= 1e-4 * c.numel()
