@@ -128,7 +128,7 @@ def lib() -> ctypes.CDLL:
         L.difr_mx_logits.restype = ctypes.c_int
         L.difr_mx_logits.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, v, v]
         L.difr_selftest_mx_wait.restype = ctypes.c_int
-        L.difr_selftest_mx_wait.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, i64, i64, v, v]
+        L.difr_selftest_mx_wait.argtypes = [i32, i64, i64, i64, v, i32, i64, i32, i64, v, v]
         _lib = L
     return _lib
 
@@ -553,36 +553,35 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     return out
 
 
-def _check_product(h, W, logits, device, device_status):
-    _check_mx(h, "h", device)
-    _check_mx(W, "W", device)
-    if h.format != W.format or h.d != W.d:
-        raise TypeError(f"h has {h.d} values of {h.format} bits per row, W {W.d} of {W.format}")
-    if logits.shape != (h.rows, W.rows):
-        raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
-    if device_status is not None:
-        _check(device_status, _torch.int32, (1,), "device_status")
-        if device_status.get_device() != device:
-            raise TypeError(f"device_status is on {device_status.device}, not on CUDA device {device}")
+def _check_status_word(t, device):
+    if t is not None:
+        _check(t, _torch.int32, (1,), "device_status")
+        if t.get_device() != device:
+            raise TypeError(f"device_status is on {t.device}, not on CUDA device {device}")
 
 
 def difr_mx_logits(h: MxTensor, W: MxTensor, logits, device_status=None, stream=None):
     """Logits [T, V] (fp32 or bf16) of microscaled hidden states and LM head, both of one format.  A device-side wait that
     runs out leaves NaN where logits were not computed, and DIFR_ERR_TIMEOUT in `device_status` (int32 [1], optional)."""
     dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
-    _check_product(h, W, logits, device, device_status)
+    _check_mx(h, "h", device)
+    _check_mx(W, "W", device)
+    if h.format != W.format or h.d != W.d:
+        raise TypeError(f"h has {h.d} values of {h.format} bits per row, W {W.d} of {W.format}")
+    if logits.shape != (h.rows, W.rows):
+        raise TypeError(f"logits: expected {(h.rows, W.rows)}, got {tuple(logits.shape)}")
+    _check_status_word(device_status, device)
     _call("difr_mx_logits", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
           W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld,
           None if device_status is None else device_status.data_ptr())
     return logits
 
 
-def difr_selftest_mx_wait(h: MxTensor, W: MxTensor, logits, loaded_tiles: int, limit_cycles: int, device_status=None,
-                          stream=None):
-    """difr_mx_logits that loads `loaded_tiles` tiles only and gives up after `limit_cycles`; see include/difr.h."""
+def difr_selftest_mx_wait(format: int, d: int, logits, done_tiles: int, limit_cycles: int, device_status=None, stream=None):
+    """How difr_mx_logits ends where a wait runs out: NaN beyond the first `done_tiles` tiles of every pair of CTAs and
+    DIFR_ERR_TIMEOUT in `device_status`; see include/difr.h."""
     dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
-    _check_product(h, W, logits, device, device_status)
-    _call("difr_selftest_mx_wait", device, stream, h.codes.data_ptr(), h.scales.data_ptr(), W.codes.data_ptr(),
-          W.scales.data_ptr(), h.format, h.rows, h.d, W.rows, logits.data_ptr(), dtype, ld, int(loaded_tiles),
-          int(limit_cycles), None if device_status is None else device_status.data_ptr())
+    _check_status_word(device_status, device)
+    _call("difr_selftest_mx_wait", device, stream, format, logits.shape[0], d, logits.shape[1], logits.data_ptr(), dtype,
+          ld, done_tiles, limit_cycles, None if device_status is None else device_status.data_ptr())
     return logits

@@ -117,18 +117,16 @@ difr_status convert_checks(const void* codes, const void* scales, int32_t format
   return DIFR_OK;
 }
 
-// The product: difr_mx_logits loads all of its tiles and waits kWaitCycles, the self-test of its waits fewer and shorter.
-difr_status mx_logits_call(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
-                           int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
-                           int32_t* device_status, int64_t loaded_tiles, int64_t wait_cycles, difr_stream_t stream) {
+difr_status product_checks(int32_t format, int64_t T, int64_t d, int64_t V, int32_t dtype, int64_t ld) {
   if (!known_format(format) || (dtype != DIFR_F32 && dtype != DIFR_BF16)) return DIFR_ERR_INVALID_ARG;
   if (T < 0 || d <= 0 || V <= 0 || ld < V) return DIFR_ERR_INVALID_ARG;
   if (!mx_supported(T, d) || V > kMaxRows || ld > kMaxLd) return DIFR_ERR_SHAPE;
-  if (T == 0) return DIFR_OK;
-  if (!h_codes || !h_scales || !W_codes || !W_scales || !logits) return DIFR_ERR_INVALID_ARG;
-  if (!aligned16(h_codes) || !aligned16(h_scales) || !aligned16(W_codes) || !aligned16(W_scales) ||
-      !aligned_to(logits, elem_bytes(dtype)))
-    return DIFR_ERR_ALIGN;
+  return DIFR_OK;
+}
+
+// How a product of T >= 1 tokens is cut into tiles: the kernel's parameters, tokens per tile, grid.
+difr_status mx_plan(int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
+                    int32_t* device_status, MxLogitsParams* out, int* tokens_per_tile, int* grid) {
   // tokens per tile: the smallest width that holds all tokens, tiles of 256 beyond 128
   int bn = 16;
   while (bn < 256 && bn < T) bn *= 2;
@@ -151,8 +149,6 @@ difr_status mx_logits_call(const void* h_codes, const void* h_scales, const void
   p.last_mmas = (int)((pitch - (int64_t)(p.k_steps - 1) * 128 + 31) / 32);
   p.n_vt = (int)n_vt; p.n_tt = (int)n_tt;
   p.n_tiles = (int)(n_vt * n_tt);
-  p.loaded_tiles = loaded_tiles < p.n_tiles ? (int)loaded_tiles : p.n_tiles;
-  p.wait_cycles = (long long)wait_cycles;
   // the last token tile is only as wide as its tokens (in steps of 16, what the MMA takes)
   p.last_tokens = (int)((T - (n_tt - 1) * bn + 15) / 16 * 16);
   // tokens of a raster group: about 32 MB of codes, a quarter of L2, so that they stay there while W passes
@@ -166,25 +162,14 @@ difr_status mx_logits_call(const void* h_codes, const void* h_scales, const void
   p.w_once = n_tt == 1 && V * pitch > ((int64_t)96 << 20);
   p.pack_pairs = dtype == DIFR_BF16 && ld % 2 == 0 && aligned_to(logits, 4);
   p.tile_stores = bn == 256 && vector_rows(logits, ld, dtype) && ld <= ((int64_t)1 << 36);
-  const int words = format == DIFR_MX8 ? 1 : 2;
-  CUtensorMap tw, th, th_last, tsw, tsh;
-  if (!codes_tmap(&tw, W_codes, format, V, d, 128) || !codes_tmap(&th, h_codes, format, T, d, bn / 2) ||
-      !scales_tmap(&tsw, W_scales, V, d, words, 1) || !scales_tmap(&tsh, h_scales, T, d, words, bn > 128 ? 2 : 1))
-    return DIFR_ERR_CUDA;
-  th_last = th;
-  if (p.last_tokens != bn && !codes_tmap(&th_last, h_codes, format, T, d, p.last_tokens / 2)) return DIFR_ERR_CUDA;
-  CUtensorMap tout;
-  memset(&tout, 0, sizeof tout);
-  if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
   const int n_pairs = p.n_tiles < pairs ? p.n_tiles : pairs;
   // a pair's token tiles follow each other in steps of n_pairs - shift: prime to their number, all come in turn
   if (n_pairs > 1)
     while (p.shift < n_pairs - 1 && common_divisor(n_pairs - p.shift, p.group) != 1) ++p.shift;
-  const int grid = 2 * n_pairs;
-  return launch_mx_logits(format, bn, dtype, tw, th, th_last, tsw, tsh, tout, p, grid, reinterpret_cast<cudaStream_t>(stream)) ==
-                 cudaSuccess
-             ? DIFR_OK
-             : DIFR_ERR_CUDA;
+  *out = p;
+  *tokens_per_tile = bn;
+  *grid = 2 * n_pairs;
+  return DIFR_OK;
 }
 
 }  // namespace
@@ -274,17 +259,48 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
 difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
                            int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
                            int32_t* device_status, difr_stream_t stream) {
-  return mx_logits_call(h_codes, h_scales, W_codes, W_scales, format, T, d, V, logits, dtype, ld, device_status,
-                        INT64_MAX, kWaitCycles, stream);
+  const difr_status st = product_checks(format, T, d, V, dtype, ld);
+  if (st != DIFR_OK || T == 0) return st;
+  if (!h_codes || !h_scales || !W_codes || !W_scales || !logits) return DIFR_ERR_INVALID_ARG;
+  if (!aligned16(h_codes) || !aligned16(h_scales) || !aligned16(W_codes) || !aligned16(W_scales) ||
+      !aligned_to(logits, elem_bytes(dtype)))
+    return DIFR_ERR_ALIGN;
+  MxLogitsParams p;
+  int bn = 0, grid = 0;
+  const difr_status plan = mx_plan(format, T, d, V, logits, dtype, ld, device_status, &p, &bn, &grid);
+  if (plan != DIFR_OK) return plan;
+  const int words = format == DIFR_MX8 ? 1 : 2;
+  CUtensorMap tw, th, th_last, tsw, tsh;
+  if (!codes_tmap(&tw, W_codes, format, V, d, 128) || !codes_tmap(&th, h_codes, format, T, d, bn / 2) ||
+      !scales_tmap(&tsw, W_scales, V, d, words, 1) || !scales_tmap(&tsh, h_scales, T, d, words, bn > 128 ? 2 : 1))
+    return DIFR_ERR_CUDA;
+  th_last = th;
+  if (p.last_tokens != bn && !codes_tmap(&th_last, h_codes, format, T, d, p.last_tokens / 2)) return DIFR_ERR_CUDA;
+  CUtensorMap tout;
+  memset(&tout, 0, sizeof tout);
+  if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
+  return launch_mx_logits(format, bn, dtype, tw, th, th_last, tsw, tsh, tout, p, grid, reinterpret_cast<cudaStream_t>(stream)) ==
+                 cudaSuccess
+             ? DIFR_OK
+             : DIFR_ERR_CUDA;
 }
 
-difr_status difr_selftest_mx_wait(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
-                                  int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype,
-                                  int64_t ld, int64_t loaded_tiles, int64_t limit_cycles, int32_t* device_status,
+difr_status difr_selftest_mx_wait(int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
+                                  int32_t done_tiles, int64_t limit_cycles, int32_t* device_status,
                                   difr_stream_t stream) {
-  if (loaded_tiles < 0 || limit_cycles < 1 || limit_cycles > 1000000000LL) return DIFR_ERR_INVALID_ARG;
-  return mx_logits_call(h_codes, h_scales, W_codes, W_scales, format, T, d, V, logits, dtype, ld, device_status,
-                        loaded_tiles, limit_cycles, stream);
+  if (done_tiles < 0 || limit_cycles < 1 || limit_cycles > 1000000000LL) return DIFR_ERR_INVALID_ARG;
+  const difr_status st = product_checks(format, T, d, V, dtype, ld);
+  if (st != DIFR_OK || T == 0) return st;
+  if (!logits) return DIFR_ERR_INVALID_ARG;
+  if (!aligned_to(logits, elem_bytes(dtype))) return DIFR_ERR_ALIGN;
+  MxLogitsParams p;
+  int bn = 0, grid = 0;
+  const difr_status plan = mx_plan(format, T, d, V, logits, dtype, ld, device_status, &p, &bn, &grid);
+  if (plan != DIFR_OK) return plan;
+  return launch_mx_wait_selftest(format, bn, dtype, p, done_tiles, (long long)limit_cycles, grid,
+                                 reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? DIFR_OK
+             : DIFR_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -169,15 +169,15 @@ struct OutPieces {
 // `shift` pairs, chosen so that the narrower last token tiles reach all pairs alike.
 struct TileWalk {
   const MxLogitsParams& p;
-  const int pair, n_pairs, end;
+  const int pair, n_pairs;
   int round0, turn;  // first tile of the round, pair that is dealt to first
 
-  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n, int n_tiles)
-      : p(params), pair(pr), n_pairs(n), end(n_tiles), round0(0), turn(0) {}
+  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n)
+      : p(params), pair(pr), n_pairs(n), round0(0), turn(0) {}
   __device__ __forceinline__ bool next(int& vt, int& tt) {
     const int at = pair - turn;
     const int i = round0 + (at < 0 ? at + n_pairs : at);
-    if (i >= end) return false;
+    if (i >= p.n_tiles) return false;
     round0 += n_pairs;
     turn += p.shift;
     if (turn >= n_pairs) turn -= n_pairs;
@@ -191,6 +191,27 @@ struct TileWalk {
     return true;
   }
 };
+
+// After a wait that ran out: the warp's part of tile (vt, tt) and of the pair's next ones becomes NaN, so that no caller
+// takes what the buffer held before for logits.  `lane_id`: this lane's id inside a vocabulary tile.
+template <int FMT, int BN, typename OUT>
+__device__ __forceinline__ void fill_given_up(const MxLogitsParams& p, TileWalk& walk, int vt, int tt, int acc, int half,
+                                              int lane_id) {
+  using Tl = MxTile<FMT, BN>;
+  const OUT nan = from_float<OUT>(__int_as_float(0x7FC00000));
+  do {
+    const int v = vt * kMxPairM + lane_id;
+#pragma unroll 1
+    for (int i = 0; i < (Tl::chunks + 1) / 2; ++i) {
+      const int ch = epi_chunk<FMT, BN>(i, half, acc);
+      const int t0 = tt * BN + ch * Tl::chunk;
+      if (ch < 0 || v >= p.V) continue;
+#pragma unroll 1
+      for (int t = t0; t < t0 + Tl::chunk && t < p.T; ++t) static_cast<OUT*>(p.logits)[(int64_t)t * p.ld + v] = nan;
+    }
+    acc ^= 1;
+  } while (walk.next(vt, tt));
+}
 
 template <int FMT, int BN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxThreads, 1)
@@ -259,7 +280,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
-  TileWalk walk(p, pair, n_pairs, warp == 0 ? p.loaded_tiles : p.n_tiles);
+  TileWalk walk(p, pair, n_pairs);
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -277,7 +298,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int w_row = vt * kMxPairM + (int)cta * 128;
       const int h_row = tt * BN + (int)cta * half;
       for (int k = 0; k < p.k_steps; ++k) {
-        if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag, p.wait_cycles))) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
         if (elect_one()) {
           if (cta == 0) mbar_arrive_expect_tx(full_bar(stage), 2u * bytes);
           const uint32_t full0 = full0_base + 8u * (uint32_t)stage;
@@ -310,19 +331,16 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         // tile have been read (every epilogue warp had then finished the tile before it).
         if (Tl::overlap) {
           if (n_tile >= 1 && !__all_sync(0xffffffffu, mbar_wait(acc_free_bar(acc ^ 1), ((n_tile - 1) >> 1) & 1u,
-                                                                abort_flag, p.wait_cycles))) { ok = false; break; }
+                                                                abort_flag))) { ok = false; break; }
         } else {
           if (n_tile >= 2 && !__all_sync(0xffffffffu, mbar_wait(acc_free_bar(acc), ((n_tile - 2) >> 1) & 1u,
-                                                                abort_flag, p.wait_cycles))) { ok = false; break; }
+                                                                abort_flag))) { ok = false; break; }
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * Tl::acc_stride);
         uint32_t accumulate = 0;
         for (int k = 0; k < p.k_steps; ++k) {
-          if (!__all_sync(0xffffffffu, mbar_wait_cta(full_bar(stage), phase, full_seen, abort_flag, p.wait_cycles))) {
-            ok = false;
-            break;
-          }
+          if (!__all_sync(0xffffffffu, mbar_wait_cta(full_bar(stage), phase, full_seen, abort_flag))) { ok = false; break; }
           // a look at the next stage: its answer is there by the time it is needed
           {
             const bool wrap = stage + 1 == kStages;
@@ -384,7 +402,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     int vt, tt;
     bool given_up = false;
     while (walk.next(vt, tt)) {
-      const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag, p.wait_cycles);
+      const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
       __syncwarp();
       tc_fence_after();
       const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
@@ -450,23 +468,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (BN == 256 && p.tile_stores) bulk_wait_all();  // the pieces stay until they have left
-    // After a wait that ran out the warp's part of this tile and of the pair's next ones becomes NaN: no caller takes
-    // what the buffer held before for logits.
-    if (given_up) {
-      const OUT nan = from_float<OUT>(__int_as_float(0x7FC00000));
-      do {
-        const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
-#pragma unroll 1
-        for (int i = 0; i < (Tl::chunks + 1) / 2; ++i) {
-          const int ch = epi_chunk<FMT, BN>(i, half, acc);
-          const int t0 = tt * BN + ch * Tl::chunk;
-          if (ch < 0 || v >= p.V) continue;
-#pragma unroll 1
-          for (int t = t0; t < t0 + Tl::chunk && t < p.T; ++t) static_cast<OUT*>(p.logits)[(int64_t)t * p.ld + v] = nan;
-        }
-        acc ^= 1;
-      } while (walk.next(vt, tt));
-    }
+    if (given_up) fill_given_up<FMT, BN, OUT>(p, walk, vt, tt, acc, half, (int)cta * 128 + quarter * 32 + lane);
   }
 
   __syncwarp();
@@ -483,6 +485,38 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, kMxTmemCols);
   }
+  if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
+}
+
+// The way out of the epilogue after waits that ran out, without a product: a CTA is the eight epilogue warps, its first
+// `done_tiles` tiles count as finished, and the barrier of the next one is never arrived at.  With tiles of 256 tokens one
+// warp of each half sees its barrier complete, so that it is the others that make it give up.
+template <int FMT, int BN, typename OUT>
+__global__ void __launch_bounds__(32 * kMxEpiWarps)
+mx_wait_selftest(const __grid_constant__ MxLogitsParams p, int done_tiles, long long limit_cycles) {
+  __shared__ uint64_t bars[2];  // never complete, complete
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bars[0]), 1);
+    mbar_init(smem_u32(&bars[1]), 1);
+    abort_word = 0;
+    mbar_fence_init();
+    mbar_arrive(smem_u32(&bars[1]));
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int half = warp >> 2, quarter = warp & 3;
+  TileWalk walk(p, blockIdx.x >> 1, gridDim.x >> 1);
+  int vt, tt;
+  for (int k = 0; k <= done_tiles; ++k)
+    if (!walk.next(vt, tt)) return;  // all tiles of the pair are finished, in all of its threads
+  const bool ok = mbar_wait_cta(smem_u32(&bars[BN == 256 && quarter == 1 ? 1 : 0]), 0, false, abort_flag, limit_cycles);
+  __syncwarp();
+  const bool given_up = BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !__all_sync(0xffffffffu, ok);
+  if (given_up)
+    fill_given_up<FMT, BN, OUT>(p, walk, vt, tt, done_tiles & 1, half, (int)(blockIdx.x & 1) * 128 + quarter * 32 + lane);
+  __syncthreads();
   if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
 }
 
@@ -531,6 +565,28 @@ cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUte
                           : launch_typed<kMx8, float>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream);
   return dtype == kBf16 ? launch_typed<kMx4, __nv_bfloat16>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream)
                         : launch_typed<kMx4, float>(tokens_per_tile, w, h, hl, sw, sh, out, p, grid, stream);
+}
+
+template <int FMT, typename OUT>
+static cudaError_t launch_selftest(int bn, const MxLogitsParams& p, int done, long long limit, int grid, cudaStream_t stream) {
+  constexpr int threads = 32 * kMxEpiWarps;
+  switch (bn) {
+    case 16: mx_wait_selftest<FMT, 16, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+    case 32: mx_wait_selftest<FMT, 32, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+    case 64: mx_wait_selftest<FMT, 64, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+    case 128: mx_wait_selftest<FMT, 128, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+    default: mx_wait_selftest<FMT, 256, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_mx_wait_selftest(int fmt, int tokens_per_tile, int dtype, const MxLogitsParams& p, int done_tiles,
+                                    long long limit_cycles, int grid, cudaStream_t stream) {
+  if (fmt == kMx8)
+    return dtype == kBf16 ? launch_selftest<kMx8, __nv_bfloat16>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream)
+                          : launch_selftest<kMx8, float>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream);
+  return dtype == kBf16 ? launch_selftest<kMx4, __nv_bfloat16>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream)
+                        : launch_selftest<kMx4, float>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream);
 }
 
 // Pairs the device keeps resident at once: one CTA per SM, the same for every variant (each takes the whole TMEM).

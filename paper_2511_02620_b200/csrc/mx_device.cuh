@@ -427,7 +427,7 @@ __device__ __forceinline__ bool mbar_test_cta(uint32_t bar, uint32_t parity) {
 }
 // The bounded wait at CTA scope; `seen`: the barrier's phase was already seen to be complete.
 __device__ __forceinline__ bool mbar_wait_cta(uint32_t bar, uint32_t parity, bool seen, volatile int* abort_flag,
-                                              long long limit_cycles) {
+                                              long long limit_cycles = kWaitCycles) {
   if (seen || mbar_test_cta(bar, parity)) return true;
   const long long t0 = clock64();
   while (true) {

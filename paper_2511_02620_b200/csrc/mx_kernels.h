@@ -49,8 +49,6 @@ struct MxLogitsParams {
   int group;             // token tiles per raster group
   int last_tokens;       // width of the last token tile, a multiple of 16
   int n_tiles;
-  int loaded_tiles;      // n_tiles; fewer (a test of the waits): the tiles from here on are never loaded
-  long long wait_cycles; // after which a wait gives up
   int shift;             // of the deal, per round
   bool pack_pairs;       // bf16 logits, plain stores: two neighbouring ids leave in one 4-byte store
   bool w_once;           // one token tile, and a W that does not fit L2: its rows need not stay there
@@ -64,6 +62,9 @@ constexpr int mx_out_tokens(int elem) { return kMxOutBytes / (128 * elem); }  //
 cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
                              const CUtensorMap& h_last, const CUtensorMap& sw, const CUtensorMap& sh, const CUtensorMap& out, const MxLogitsParams& p, int grid,
                              cudaStream_t stream);
+// The end of the product after waits that ran out, with nothing computed: see difr_selftest_mx_wait.
+cudaError_t launch_mx_wait_selftest(int fmt, int tokens_per_tile, int dtype, const MxLogitsParams& p, int done_tiles,
+                                    long long limit_cycles, int grid, cudaStream_t stream);
 int mx_logits_max_resident_pairs();
 
 }  // namespace difr

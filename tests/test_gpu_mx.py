@@ -742,34 +742,43 @@ def test_rows_whose_squares_are_subnormal(d, dtype):
 
 # ------------------------------------------------------------------ waits that run out
 @pytest.mark.parametrize("fmt", [4, 8])
-@pytest.mark.parametrize("T,V,ld,out_dtype", [(600, 9800, 9800, "bf16"), (600, 9801, 9801, "f32"), (300, 1100, 1104, "f32"),
-                                              (40, 9800, 9803, "bf16"), (7, 30000, 30000, "f32")])
-def test_logits_that_a_wait_kept_from_being_computed_are_nan(T, V, ld, out_dtype, fmt):
-    """Tiles that are never loaded: their waits give up, their logits are NaN, all others what they should be, the status
-    word says so, and the next call is as good as ever."""
-    d = 160
-    h, _ = random_mx(T, d, fmt, seed=1)
-    W, _ = random_mx(V, d, fmt, seed=2)
-    dt = DTYPES[out_dtype]
-    want = difr.difr_mx_logits(h, W, torch.empty(T, V, dtype=dt, device="cuda"))
-    width = 256 if T > 128 else 16 if T <= 16 else 64
-    if (V + 255) // 256 * ((T + 255) // 256) <= 37 and T > 128:
-        width = 128
-    n_tt = (T + width - 1) // width
-    n = (V + 255) // 256 * n_tt
-    tile = (torch.arange(V, device="cuda") // 256 * n_tt).view(1, -1) + (torch.arange(T, device="cuda") // width).view(-1, 1)
-    for loaded in (0, 1, 5, n - 1, n, n + 7):
-        buf = torch.full((T + 1, ld), -7.0, dtype=dt, device="cuda")
+@pytest.mark.parametrize("T,V,d,ld,out_dtype", [
+    (600, 9800, 160, 9800, "bf16"), (600, 9801, 160, 9801, "f32"), (300, 1100, 160, 1104, "f32"), (40, 9800, 96, 9803, "bf16"),
+    (20, 50000, 96, 50000, "bf16"), (7, 30000, 96, 30000, "f32"), (2700, 9800, 1 << 20, 9800, "bf16")])
+def test_logits_that_a_wait_keeps_from_being_computed_are_nan(T, V, d, ld, out_dtype, fmt):
+    """The way out of the product's epilogue after waits that ran out, at every tile width: the warps of a half give up
+    together, all logits but those of the finished tiles are NaN, the status word says so, and the next call is as good
+    as ever."""
+    buf = torch.full((T + 1, ld), -7.0, dtype=DTYPES[out_dtype], device="cuda")
+    part = buf[:T, :V]
+    left = []
+    for done in (0, 1, 2, 3, 1000):
+        buf.fill_(-7.0)
         status = torch.zeros(1, dtype=torch.int32, device="cuda")
-        difr.difr_selftest_mx_wait(h, W, buf[:T, :V], loaded, 2_000_000, status)
-        assert int(status.item()) == (0 if loaded >= n else -7)
-        lost = tile >= loaded
-        assert torch.isnan(buf[:T, :V][lost]).all()
-        assert torch.equal(buf[:T, :V][~lost], want[~lost])
+        difr.difr_selftest_mx_wait(fmt, d, part, done, 1_000_000, status)
+        nan = torch.isnan(part)
+        assert int(status.item()) == (0 if done == 1000 else -7 if bool(nan.any()) else 0)
+        assert torch.all(part[~nan] == -7.0)
         assert torch.all(buf[:T, V:] == -7.0) and torch.all(buf[T:] == -7.0)
-        difr.difr_selftest_mx_wait(h, W, buf[:T, :V], loaded, 2_000_000)  # no status word: the logits tell
-        assert torch.equal(torch.isnan(buf[:T, :V]), lost)
-    assert torch.equal(difr.difr_mx_logits(h, W, torch.empty(T, V, dtype=dt, device="cuda")), want)
+        left.append(~nan)
+        buf.fill_(-7.0)
+        difr.difr_selftest_mx_wait(fmt, d, part, done, 1_000_000)  # no status word: the logits tell
+        assert torch.equal(torch.isnan(part), nan)
+    assert not left[0].any() and left[-1].all()
+    width = 256 if T > 128 and (V + 255) // 256 * ((T + 255) // 256) > 37 else 128 if T > 64 else 64 if T > 32 else 32 if T > 16 else 16
+    for less, more in zip(left, left[1:]):
+        new = more & ~less
+        assert not (less & ~more).any()
+        # whole tiles, at most one for every pair of the 74
+        rows = torch.nn.functional.pad(new, (0, -V % 256, 0, -T % width)).view(-1, width, (V + 255) // 256, 256)
+        tiles = rows.any(3).any(1)
+        assert more.all() or int(tiles.sum()) <= 74
+        inside = torch.nn.functional.pad(torch.ones_like(new), (0, -V % 256, 0, -T % width)).view_as(rows)
+        assert torch.equal(rows, inside & tiles.view(-1, 1, tiles.shape[1], 1))
+    h, _ = random_mx(70, 96, fmt, seed=1)
+    W, _ = random_mx(1000, 96, fmt, seed=2)
+    want = difr.difr_mx_logits(h, W, torch.empty(70, 1000, device="cuda"))
+    assert not torch.isnan(want).any()
 
 
 # ------------------------------------------------------------------ long rows, several raster groups, heads beyond L2

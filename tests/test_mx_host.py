@@ -90,13 +90,14 @@ def test_refusals_of_the_wait_self_test():
         pytest.skip("host-only check")
     L, p = difr.lib(), 0x10000
 
-    def call(loaded=0, limit=1000, fmt=4, ld=100, hc=p):
-        return L.difr_selftest_mx_wait(hc, p, p, p, fmt, 8, 64, 100, p, 2, ld, loaded, limit, None, None)
+    def call(done=0, limit=1000, fmt=4, T=8, ld=100, out=p):
+        return L.difr_selftest_mx_wait(fmt, T, 64, 100, out, 2, ld, done, limit, None, None)
 
     for limit in (0, -1, 1_000_000_001):
         assert call(limit=limit) == INVALID
-    assert call(loaded=-1) == INVALID
-    assert call(fmt=1) == INVALID and call(ld=99) == INVALID and call(hc=None) == INVALID  # the product's own checks
+    assert call(done=-1) == INVALID
+    assert call(fmt=1) == INVALID and call(ld=99) == INVALID and call(out=None) == INVALID and call(out=p + 2) == ALIGN
+    assert call(T=0, out=None) == OK
 
 
 def test_a_well_formed_call_without_a_device_reports_a_cuda_error():
