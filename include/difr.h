@@ -451,8 +451,9 @@ difr_status difr_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
 
 /*
  * codes, scales -> out [rows, d] (row stride ldo >= d elements), DIFR_BF16 or DIFR_F32.  Exact in both, except that
- * bf16 rounds magnitudes below 2^-133.  With W and h dequantised to bf16 every scoring call replays a server whose head
- * is held in the format.
+ * bf16 rounds magnitudes below 2^-133, and that values from 2^128 on (large codes under scale bytes above 246, which
+ * difr_mx_quantize does not write) become infinities.  With W and h dequantised to bf16 every scoring call replays a
+ * server whose head is held in the format.
  */
 difr_status difr_mx_dequantize(const void* codes, const void* scales, int32_t format, int64_t rows, int64_t d,
                                void* out, int32_t dtype, int64_t ldo, difr_stream_t stream);
@@ -476,8 +477,10 @@ typedef struct {
  *   h = bf16(y), codes / scales = microscaled(y)
  *
  * x, residual and weight [d] have the type `dtype`; row strides ldx and ld_residual in elements.  y is rounded once: the
- * microscaled output is taken from the fp32 value, not from h.  Rows whose squares leave fp32's range are handled.  A
- * row with a NaN is NaN throughout; one with an infinity is NaN there and zero elsewhere.
+ * microscaled output is taken from the fp32 value, not from h.  (Some servers round r / sqrt(..) to the activations' type
+ * before they multiply by the weight: their h differs from this one in last bits.)  Rows whose squares leave fp32's range
+ * at either end are handled, with any positive finite eps.  A row with a NaN is NaN throughout; one with an infinity is NaN
+ * there and zero elsewhere.
  * out->residual may be x's or residual's own buffer, and out->h that of a bf16 x or residual, at the same stride;
  * buffers that overlap in another way give undefined results.  d <= 32768; eps > 0.
  */
@@ -488,10 +491,13 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
 /*
  * Logits of a head held in 8 or 4 bits: logits[t, v] = h[t, :] . W[v, :] of two microscaled tensors of one format,
  * accumulated in fp32 on the block-scaled tensor cores; `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or
- * DIFR_BF16.  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional: a wait that
+ * DIFR_BF16.  The cores add 32 (8 bits) or 64 (4 bits) exact products per step and may drop low bits there: the tests hold
+ * the fp32 sums within (2 steps + 2) 2^-23 sum |h W| of the exact ones; their size is 3e-7 of the logits' at d = 5120 in
+ * 8 bits (a plain fp32 product: 1e-7).  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional: a wait that
  * runs out also leaves NaN in the place of every logit that was not computed.
  *
- * In all of these calls a row's results are the same bits whatever other rows the batch holds.
+ * In all of these calls a row's results are the same bits whatever other rows the batch holds, given the same types, strides
+ * and alignment (the norm adds squares in another order where a matrix has rows off the 16-byte boundaries).
  */
 difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
                            int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,

@@ -158,7 +158,8 @@ difr_status mx_plan(int32_t format, int64_t T, int64_t d, int64_t V, void* logit
   if (group > n_tt) group = n_tt;
   p.group = (int)group;
   // W is read once where there is one token tile; one that L2 cannot keep for the next call either (96 of its 126 MB) goes
-  // by it (48 tokens, 151936 x 2048 in 8 bits: 51.6 us, 56.5 otherwise; a 65 MB head loses by it, 13.9 us for 11.0)
+  // by it.  Codes of d = 2048 in 8 bits, read again in every call, 48 tokens: 260 MB 51.9 us by it, 53.4 otherwise; 112 MB
+  // 27.2 and 27.9; 80 MB 16.6 and 17.3, but there it also puts out what other kernels keep in L2.  One token: 0 to 4 %.
   p.w_once = n_tt == 1 && V * pitch > ((int64_t)96 << 20);
   p.pack_pairs = dtype == DIFR_BF16 && ld % 2 == 0 && aligned_to(logits, 4);
   p.tile_stores = bn == 256 && vector_rows(logits, ld, dtype) && ld <= ((int64_t)1 << 36);

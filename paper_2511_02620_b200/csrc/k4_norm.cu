@@ -6,10 +6,11 @@
 //
 // A row stays in registers between the sum of its squares and the scaling, so every element is read once and every
 // result written once: the kernel is bound by those bytes, as long as it spends few instructions per element (elements
-// are kept as they lie in memory, 8 per load, and worked on in pairs).  A row belongs to a group of whole warps; rows
-// off the 16-byte boundaries (odd d, odd strides) are turned through shared memory on their way in and out.  The sum
-// runs in an order that the row alone fixes (per thread, shuffles, warps in order).  y is rounded once, whatever
-// asks for it: the codes are taken from the fp32 value, not from h.
+// are kept as they lie in memory, 8 per load, and worked on in pairs).  A row belongs to a group of whole warps.  Of the
+// rows off the 16-byte boundaries (odd d, odd strides) 16-bit ones on 8 or 4 bytes are read, on 8 bytes written, directly in
+// such pieces; the others are turned through shared memory.  The sum runs in a fixed order (per thread, shuffles, warps
+// in order) that d, the type and whether all rows lie on 16-byte boundaries fix, not the batch.  y is rounded once,
+// whatever asks for it: the codes are taken from the fp32 value, not from h.
 // Measured in bf16 with residual, stream and h: 65536 x 2048 161 us, 6.7 TB/s of necessary bytes (238 us while an element
 // cost 45 instructions); 8192 x 5120 56 us; to 8 bits without h 52 us.
 #include <cuda_runtime.h>
@@ -22,8 +23,8 @@ namespace difr {
 constexpr int kNormMaxThreads = 512;
 
 // Sum over the threads of a row, the same value in all of them.  A row of more than one warp has the CTA to itself.
-// Eight terms at a time are added in fp32, their sums in fp64, so that the result is the exact sum rounded once, nearly
-// always: values next to a border of the 4-bit format depend on its last bit.
+// Eight terms at a time are added in fp32 (five roundings at most), their sums in fp64, where nothing more is lost: values
+// next to a border of the 4-bit format depend on the sum's last bits.
 __device__ __forceinline__ float row_sum(double v, double* part, int warps) {
 #pragma unroll
   for (int m = 16; m >= 1; m >>= 1) v += shfl_xor_double(v, m);
@@ -178,9 +179,9 @@ static void launch_vec(const NormParams& p, unsigned grid, int threads, cudaStre
 
 template <typename X>
 static cudaError_t launch_typed(NormParams p, cudaStream_t stream) {
-  // Vectors per thread, by the row alone, so that a row's result does not depend on the batch it is in: four (fp32: two,
+  // Vectors per thread, whatever the number of rows, so that a row's result does not depend on its batch: four (fp32: two,
   // the same registers), for more loads in flight and fewer barriers per byte: T = 16384, d = 4096 in bf16 took 45.9 us
-  // at four, 48.3 at two, 47.3 at eight.  Rows that go through shared memory need the registers for that: one.
+  // at four, 48.3 at two, 47.3 at eight.  Rows off the 16-byte boundaries need the registers for their pieces: one.
   const int nvec = (p.d + 127) / 128 * 16;  // to whole scale words
   int vpt = !p.vec ? 1 : sizeof(X) == 4 ? 2 : 4;
   while (vpt > 1 && nvec <= 32 * vpt / 2) vpt /= 2;

@@ -21,8 +21,8 @@
 // slot, and its own loop, not the tensor pipe, set the pace: 520 clocks a stage where the MMAs take 512.)
 //
 // Measured: one token x 128256 x 4096 in 4 bits 46 us (6.1 TB/s); 4096 tokens 848 to 892 us in bf16, 4.8 to 5.1 PFLOP/s at the
-// power cap (1.2 to 1.4 GHz, tensor pipe 83 % active); 4096 x 152064 x 5120 in 8 bits 2400 to 2510 us, 2.5 to 2.66 PFLOP/s
-// (95 % active).  Tiles go in rounds over all pairs, not in stretches per pair: the latter's W slabs leave L2, 3604 us.
+// power cap (1.2 to 1.4 GHz, tensor pipe 83 % active); 4096 x 152064 x 5120 in 8 bits 2400 to 2510 us with bf16 logits, 2.5 to
+// 2.66 PFLOP/s (95 % active), 2610 to 2710 us with fp32 ones.  Tiles go in rounds over all pairs, not in stretches per pair: the latter's W slabs leave L2, 3604 us.
 //
 // Warps: 0 TMA, 1 MMA, 2 TMEM allocation, 4..11 epilogue (two per lane quarter, half of the tile's columns each).
 #include <cuda.h>
@@ -52,7 +52,7 @@ struct MxTile {
   static constexpr int load_bytes = a_bytes + b_bytes + sa_bytes + sb_bytes;
   static constexpr int stage_bytes = (load_bytes + 1023) / 1024 * 1024;
   static constexpr int bar_bytes = 512;
-  // 256-token tiles leave through shared memory: kOutBuffers pieces in flight for each half of the epilogue
+  // 256-token tiles leave through shared memory: out_buffers pieces in flight for each half of the epilogue
   static constexpr int out_buffers = BN == 256 ? 3 : 0;
   static constexpr int out_bytes = 2 * out_buffers * kMxOutBytes;
   static constexpr int fit = (227 * 1024 - 1024 - bar_bytes - out_bytes) / stage_bytes;
@@ -527,8 +527,8 @@ static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const
   const cudaError_t e = cudaFuncSetAttribute(mx_logits<FMT, BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              MxTile<FMT, BN>::smem_bytes);
   if (e != cudaSuccess) return e;
-  // (a programmatic launch: a CTA is set up while the kernel before it ends; a decoding step of 128256 x 4096 in 4 bits
-  // takes 46 us instead of 49 for it)
+  // (a programmatic launch: a CTA is set up while the kernel before it ends; with the policy of a head that is read once a
+  // decoding step of 128256 x 4096 in 4 bits takes 46 us instead of 49 for it)
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3((unsigned)grid, 1, 1);
