@@ -493,8 +493,8 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
  * accumulated in fp32 on the block-scaled tensor cores; `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or
  * DIFR_BF16.  The cores add 32 (8 bits) or 64 (4 bits) exact products per step and may drop low bits there: the tests hold
  * the fp32 sums within (2 steps + 2) 2^-23 sum |h W| of the exact ones; their size is 3e-7 of the logits' at d = 5120 in
- * 8 bits (a plain fp32 product: 1e-7).  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in difr_out, optional: a wait that
- * runs out also leaves NaN in the place of every logit that was not computed.
+ * 8 bits (a plain fp32 product: 1e-7).  No workspace.  Any T from 1, any V from 1, any d.  `device_status` as in
+ * difr_out, optional: a wait that runs out also leaves NaN in the place of every logit that was not computed.
  *
  * In all of these calls a row's results are the same bits whatever other rows the batch holds, given the same types, strides
  * and alignment (the norm adds squares in another order where a matrix has rows off the 16-byte boundaries).

@@ -47,7 +47,10 @@ __device__ __forceinline__ float2 row_scale(float ss, float inv_d, float eps, F 
   const bool huge = ss > 3.0e38f;
   if (huge || m < 0x1p-100f) {
     const float unit = huge ? 0x1p-80f : 0x1p80f;
-    return make_float2(unit, rsqrtf(__fadd_rn(__fmul_rn(again(unit), inv_d), eps * unit * unit)));
+    const float root = rsqrtf(__fadd_rn(__fmul_rn(again(unit), inv_d), eps * unit * unit));
+    // (half of the unit each: small values of a huge row stay normal numbers as long as their y is one)
+    const float part = huge ? 0x1p-40f : 0x1p40f;
+    return make_float2(part, part * root);
   }
   if (m > 3.0e38f) return make_float2(1.f, 0.5f * rsqrtf(__fadd_rn(0.25f * mean, 0.25f * eps)));
   return make_float2(1.f, rsqrtf(m));

@@ -22,7 +22,8 @@
 //
 // Measured: one token x 128256 x 4096 in 4 bits 46 us (6.1 TB/s); 4096 tokens 848 to 892 us in bf16, 4.8 to 5.1 PFLOP/s at the
 // power cap (1.2 to 1.4 GHz, tensor pipe 83 % active); 4096 x 152064 x 5120 in 8 bits 2400 to 2510 us with bf16 logits, 2.5 to
-// 2.66 PFLOP/s (95 % active), 2610 to 2710 us with fp32 ones.  Tiles go in rounds over all pairs, not in stretches per pair: the latter's W slabs leave L2, 3604 us.
+// 2.66 PFLOP/s (95 % active), 2610 to 2710 us with fp32 ones.  Tiles go in rounds over all pairs, not in stretches per pair:
+// the latter's W slabs leave L2, 3604 us.
 //
 // Warps: 0 TMA, 1 MMA, 2 TMEM allocation, 4..11 epilogue (two per lane quarter, half of the tile's columns each).
 #include <cuda.h>

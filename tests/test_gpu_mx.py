@@ -740,6 +740,27 @@ def test_rows_whose_squares_are_subnormal(d, dtype):
         assert torch.all(((got - y).abs() <= (2.0 ** -3 + 2 * Y_ERR) * y.abs() + 2.0 ** -18 * (1 + Y_ERR) * top)[keep])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [700, 1001, 20000])
+def test_small_values_in_huge_and_tiny_rows(d, dtype):
+    """Values of all magnitudes beside those that fix the root: y is as exact as anywhere while it is a normal number."""
+    x = torch.exp2(torch.rand(6, d, generator=torch.Generator().manual_seed(d)) * 110 - 100)
+    x[0] = torch.exp2(torch.rand(d, generator=torch.Generator().manual_seed(d + 1)) * 20 - 70)
+    x[:, 0] = torch.tensor([3e19, 1e21, 1e30, 1e38, 1e-25, 1e-30])
+    x[4:, 1:] *= 2.0 ** -95
+    x[4:] = x[4:].clamp(max=1e-25)
+    x = x.to(DTYPES[dtype])
+    w = (1 + 0.2 * randn(d, seed=3)).to(DTYPES[dtype])
+    h = torch.empty(6, d, dtype=torch.bfloat16, device="cuda")
+    difr.difr_rms_norm(x.cuda(), w.cuda(), 1e-42, difr.NormOut(h=h))
+    _, y = ref.rms_norm(x, None, w, 1e-42)
+    assert w.abs().max() < 2  # r / sqrt(..) is a normal number, too
+    normal = y.abs() > 2.0 ** -125
+    assert normal[:4].any(1).all()
+    err = (h.double().cpu() - y).abs()
+    assert torch.all((err <= (2.0 ** -8 + Y_ERR * (1 + 2.0 ** -8)) * y.abs())[normal])
+
+
 # ------------------------------------------------------------------ waits that run out
 @pytest.mark.parametrize("fmt", [4, 8])
 @pytest.mark.parametrize("T,V,d,ld,out_dtype", [
