@@ -526,10 +526,10 @@ difr_status difr_philox(const uint32_t* ctr, const uint32_t* key, int64_t n, uin
 difr_status difr_selftest_wait(int32_t* status2, int64_t limit_cycles, difr_stream_t stream);
 
 /*
- * Validation aid: how difr_mx_logits ends where a wait runs out, in a kernel of its own that computes nothing.  Every
- * pair of CTAs takes its first `done_tiles` tiles for finished and leaves them alone; then its warps wait on a barrier
- * that nothing arrives at, give up after `limit_cycles` SM clocks (1 .. 1e9), write NaN in the place of all other logits
- * and DIFR_ERR_TIMEOUT to device_status.  The kernel ends normally and the context stays usable.
+ * Validation aid (version 301): how difr_mx_logits ends where a wait runs out, in a kernel of its own that computes
+ * nothing.  Every pair of CTAs takes its first `done_tiles` tiles for finished and leaves them alone; then its warps wait
+ * on a barrier that nothing arrives at, give up after `limit_cycles` SM clocks (1 .. 1e9), write NaN in the place of all
+ * other logits and DIFR_ERR_TIMEOUT to device_status.  The kernel ends normally and the context stays usable.
  */
 difr_status difr_selftest_mx_wait(int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
                                   int32_t done_tiles, int64_t limit_cycles, int32_t* device_status,

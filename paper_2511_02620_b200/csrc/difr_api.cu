@@ -722,6 +722,6 @@ const char* difr_status_string(difr_status status) {
   return "unknown status";
 }
 
-int difr_version(void) { return 300; }
+int difr_version(void) { return 301; }
 
 }  // extern "C"
