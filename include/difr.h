@@ -18,6 +18,7 @@
  *   randomness   difr_expand_seeds (seeds that also depend on the context)
  *   LM head      difr_rms_norm (the final norm: the h that scoring takes, also in 8 or 4 bits), difr_mx_quantize,
  *                difr_mx_dequantize, difr_mx_logits (a head held in 8 or 4 bits)
+ *   decoding     difr_block_norm (the norms before and after a block, with its gate and residual scale)
  *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes
  *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_debug_plan_override,
  *                difr_status_string, difr_version
@@ -502,6 +503,38 @@ difr_status difr_rms_norm(const void* x, int64_t ldx, const void* residual, int6
 difr_status difr_mx_logits(const void* h_codes, const void* h_scales, const void* W_codes, const void* W_scales,
                            int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
                            int32_t* device_status, difr_stream_t stream);
+
+/*
+ * ---- A decoding step's operators (version 310) ----
+ *
+ * The norms before and after a block, with its gate and residual scale, for models that norm a block's output as well (a
+ * sandwich of norms), gate it or scale the residual stream.  With x the last block's output its h is the final one.
+ *
+ *   n = x / sqrt(mean(x^2) + post_eps) * (post_weight + weight_offset)     (n = x without post_weight)
+ *   r = round(residual_scale * residual + scale * (gate * n))              (to the inputs' type; without a gate: scale * n)
+ *   y = r / sqrt(mean(r^2) + eps) * (weight + weight_offset)
+ *   h = bf16(y), codes / scales = microscaled(y)
+ *
+ * All in fp32 but the means, rounded where it says so.  x, residual, gate and both weights [d] have the type `dtype`;
+ * weight_offset is 1 for checkpoints that hold weights minus one, else 0.  gate is [T, d] (row stride ld_gate >= d) or one
+ * row for all tokens (ld_gate 0).  out->residual receives r; out->h, out->codes and out->scales as in difr_rms_norm, and
+ * what is said there of rows with a NaN or an infinity and of values at the ends of fp32 holds for both norms.  weight may
+ * be NULL where out->residual alone is asked for.  out->residual may be x's or residual's own buffer, and out->h that of a
+ * bf16 x or residual, at the same stride; buffers that overlap in another way give undefined results.
+ * d <= 32768; eps > 0; post_eps > 0 with post_weight; finite scale, residual_scale and weight_offset.
+ */
+typedef struct {
+  const void* post_weight; /* nullable */
+  const void* gate;        /* nullable */
+  int64_t ld_gate;
+  float post_eps;
+  float scale;             /* of the block's output */
+  float residual_scale;    /* of the residual */
+  float weight_offset;
+} difr_block;
+difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const difr_block* block,
+                            const void* weight, int32_t dtype, int64_t T, int64_t d, float eps, const difr_norm_out* out,
+                            difr_stream_t stream);
 
 /*
  * Validation aid, not part of the scoring path: writes the fp32 logits

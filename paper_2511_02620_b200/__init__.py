@@ -22,7 +22,7 @@ EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_
            "difr_score_both", "difr_score_gm_filtered", "difr_score_ipt_filtered", "difr_score_gm_static",
            "difr_admissible", "difr_exfiltratable_bits", "difr_detect", "difr_expand_seeds", "difr_logits", "difr_philox",
            "difr_mx_codes_bytes", "difr_mx_scales_bytes", "difr_mx_quantize", "difr_mx_dequantize", "difr_rms_norm",
-           "difr_mx_logits",
+           "difr_mx_logits", "difr_block_norm",
            "difr_selftest_wait", "difr_selftest_mx_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
 DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
@@ -59,6 +59,12 @@ class _CNormOut(ctypes.Structure):
     _fields_ = [("residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64), ("h", ctypes.c_void_p),
                 ("ldh", ctypes.c_int64), ("mx_format", ctypes.c_int32), ("codes", ctypes.c_void_p),
                 ("scales", ctypes.c_void_p)]
+
+
+class _CBlock(ctypes.Structure):
+    _fields_ = [("post_weight", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
+                ("post_eps", ctypes.c_float), ("scale", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("weight_offset", ctypes.c_float)]
 
 
 _lib = None
@@ -127,6 +133,9 @@ def lib() -> ctypes.CDLL:
         L.difr_rms_norm.argtypes = [v, i64, v, i64, v, i32, i64, i64, ctypes.c_float, ctypes.POINTER(_CNormOut), v]
         L.difr_mx_logits.restype = ctypes.c_int
         L.difr_mx_logits.argtypes = [v, v, v, v, i32, i64, i64, i64, v, i32, i64, v, v]
+        L.difr_block_norm.restype = ctypes.c_int
+        L.difr_block_norm.argtypes = [v, i64, v, i64, ctypes.POINTER(_CBlock), v, i32, i64, i64, ctypes.c_float,
+                                      ctypes.POINTER(_CNormOut), v]
         L.difr_selftest_mx_wait.restype = ctypes.c_int
         L.difr_selftest_mx_wait.argtypes = [i32, i64, i64, i64, v, i32, i64, i32, i64, v, v]
         _lib = L
@@ -527,14 +536,25 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
     """Final root-mean-square norm of x (+ residual); `out.h` feeds the scoring calls, `out.mx` difr_mx_logits."""
     dtype, ldx, device = _matrix(x, "x", _ANY_DTYPE)
     shape = x.shape
-    if (not isinstance(weight, _torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
-            or weight.dim() != 1 or weight.numel() != shape[1] or not weight.is_contiguous()):
-        raise TypeError(f"weight must be a contiguous {x.dtype} [{shape[1]}] on {x.device}")
-    residual_p = stream_p = h_p = codes_p = scales_p = None
-    ldr = ld_stream = ldh = fmt = 0
+    _check_weight(weight, "weight", x, device)
+    residual_p, ldr = None, 0
     if residual is not None:
         ldr = _matrix(residual, "residual", (dtype,), shape, device)[1]
         residual_p = residual.data_ptr()
+    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, residual_p, ldr, weight.data_ptr(), dtype, shape[0],
+          shape[1], eps, ctypes.byref(_norm_out(out, shape, dtype, device)))
+    return out
+
+
+def _check_weight(weight, name, x, device):
+    if (not isinstance(weight, _torch.Tensor) or weight.dtype != x.dtype or weight.get_device() != device
+            or weight.dim() != 1 or weight.numel() != x.shape[1] or not weight.is_contiguous()):
+        raise TypeError(f"{name} must be a contiguous {x.dtype} [{x.shape[1]}] on {x.device}")
+
+
+def _norm_out(out, shape, dtype, device):
+    stream_p = h_p = codes_p = scales_p = None
+    ld_stream = ldh = fmt = 0
     if out.residual is not None:
         ld_stream = _matrix(out.residual, "out.residual", (dtype,), shape, device)[1]
         stream_p = out.residual.data_ptr()
@@ -547,10 +567,7 @@ def difr_rms_norm(x, weight, eps, out: NormOut, residual=None, stream=None) -> N
         if (mx.rows, mx.d) != shape:
             raise TypeError(f"out.mx is {mx.rows} x {mx.d}, x {tuple(shape)}")
         fmt, codes_p, scales_p = mx.format, mx.codes.data_ptr(), mx.scales.data_ptr()
-    c = _CNormOut(stream_p, ld_stream, h_p, ldh, fmt, codes_p, scales_p)
-    _call("difr_rms_norm", device, stream, x.data_ptr(), ldx, residual_p, ldr, weight.data_ptr(), dtype, shape[0],
-          shape[1], eps, ctypes.byref(c))
-    return out
+    return _CNormOut(stream_p, ld_stream, h_p, ldh, fmt, codes_p, scales_p)
 
 
 def _check_status_word(t, device):
@@ -585,3 +602,32 @@ def difr_selftest_mx_wait(format: int, d: int, logits, done_tiles: int, limit_cy
     _call("difr_selftest_mx_wait", device, stream, format, logits.shape[0], d, logits.shape[1], logits.data_ptr(), dtype,
           ld, done_tiles, limit_cycles, None if device_status is None else device_status.data_ptr())
     return logits
+
+
+# ------------------------------------------------- a decoding step: block norm
+def difr_block_norm(x, residual, weight, eps, out: NormOut, post_weight=None, post_eps=None, gate=None, scale=1.0,
+                    residual_scale=1.0, weight_offset=0.0, stream=None) -> NormOut:
+    """Norms before and after a block, with its gate ([T, d], or [1, d] for all tokens) and residual scale: the stream
+    residual_scale * residual + scale * gate * norm(x) to `out.residual`, its norm to `out.h` / `out.mx`.  Without
+    `post_weight` x is taken as it is; `post_eps` None: `eps`; `weight` None: the stream alone.  See include/difr.h."""
+    dtype, ldx, device = _matrix(x, "x", _ANY_DTYPE)
+    shape = x.shape
+    ldr = _matrix(residual, "residual", (dtype,), shape, device)[1]
+    weight_p = post_p = gate_p = None
+    ld_gate = 0
+    if weight is not None:
+        _check_weight(weight, "weight", x, device)
+        weight_p = weight.data_ptr()
+    if post_weight is not None:
+        _check_weight(post_weight, "post_weight", x, device)
+        post_p = post_weight.data_ptr()
+    if gate is not None:
+        rows = gate.shape[0] if isinstance(gate, _torch.Tensor) and gate.dim() == 2 else -1
+        ld_gate = _matrix(gate, "gate", (dtype,), (1 if rows == 1 else shape[0], shape[1]), device)[1]
+        gate_p = gate.data_ptr()
+        if rows == 1:
+            ld_gate = 0
+    block = _CBlock(post_p, gate_p, ld_gate, eps if post_eps is None else post_eps, scale, residual_scale, weight_offset)
+    _call("difr_block_norm", device, stream, x.data_ptr(), ldx, residual.data_ptr(), ldr, ctypes.byref(block), weight_p,
+          dtype, shape[0], shape[1], eps, ctypes.byref(_norm_out(out, shape, dtype, device)))
+    return out

@@ -17,17 +17,6 @@ namespace {
 
 using namespace difr;
 
-constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxD = (int64_t)1 << 20, kMaxLd = (int64_t)1 << 40;
-
-int elem_bytes(int32_t dtype) { return dtype == DIFR_F32 ? 4 : 2; }
-bool known_dtype(int32_t dtype) { return dtype == DIFR_BF16 || dtype == DIFR_F16 || dtype == DIFR_F32; }
-bool known_format(int32_t f) { return f == DIFR_MX8 || f == DIFR_MX4; }
-bool aligned_to(const void* p, int n) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(n - 1)) == 0; }
-// rows of `ld` elements that all start on 16-byte boundaries
-bool vector_rows(const void* p, int64_t ld, int32_t dtype) {
-  return aligned16(p) && (ld * elem_bytes(dtype)) % 16 == 0;
-}
-
 // Streaming multiprocessors and resident CTA pairs of the current device; DIFR_ERR_ARCH for another architecture.
 difr_status device_pairs(int* pairs) {
   constexpr int kMaxDevices = 64;

@@ -1,0 +1,30 @@
+// Parameter blocks and launchers of a decoding step's operators: block norm, 4-bit weights with group scales, verification of
+// drafted tokens (host-visible part).
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "mx_kernels.h"
+
+namespace difr {
+
+struct BlockNormParams {
+  const void* x;            // [T][ldx]
+  const void* residual;     // [T][ld_residual]
+  const void* post_weight;  // [d], nullable: no norm after the block
+  const void* gate;         // [T][ld_gate], nullable; ld_gate 0: one row for all tokens
+  const void* weight;       // [d], nullable: only the stream is wanted
+  void* residual_out;       // [T][ld_residual_out], nullable
+  void* h;                  // bf16 [T][ldh], nullable
+  unsigned char* codes;     // nullable: microscaled output
+  unsigned char* scales;
+  int64_t T, ldx, ld_residual, ld_gate, ld_residual_out, ldh;
+  int d, fmt;
+  float eps, post_eps, inv_d, alpha, beta, weight_offset;
+  int threads_per_row, rows_per_cta;
+  bool vec;                 // all rows start on 16-byte boundaries and d is a multiple of 8
+};
+cudaError_t launch_block_norm(const BlockNormParams& p, int dtype, cudaStream_t stream);
+
+}  // namespace difr
