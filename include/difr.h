@@ -18,8 +18,10 @@
  *   randomness   difr_expand_seeds (seeds that also depend on the context)
  *   LM head      difr_rms_norm (the final norm: the h that scoring takes, also in 8 or 4 bits), difr_mx_quantize,
  *                difr_mx_dequantize, difr_mx_logits (a head held in 8 or 4 bits)
- *   decoding     difr_block_norm (the norms before and after a block, with its gate and residual scale)
- *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes
+ *   decoding     difr_block_norm (the norms before and after a block, with its gate and residual scale),
+ *                difr_verify_drafts (drafted tokens against the target's logits, from given random words)
+ *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes,
+ *                difr_verify_workspace_bytes
  *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_debug_plan_override,
  *                difr_status_string, difr_version
  *
@@ -535,6 +537,52 @@ typedef struct {
 difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const difr_block* block,
                             const void* weight, int32_t dtype, int64_t T, int64_t d, float eps, const difr_norm_out* out,
                             difr_stream_t stream);
+
+/*
+ * Verification of drafted tokens (speculative decoding): what a server does with a draft, and a verifier that knows its
+ * random words replays.  Request b has the drafted tokens offsets[b] .. offsets[b + 1] - 1 (n_b of them, none allowed) and
+ * one row of target logits for each and one more: its rows start at offsets[b] + b, row j predicting draft j.  With
+ * p = softmax(row / temperature) (temperature 0: one at the largest logit, ties: lowest id), mu = (word + 1/2) 2^-32 and
+ * q the draft's probabilities (without draft_probs the draft was certain: q = 1 at its token)
+ *
+ *   draft j is accepted iff mu_j q_j(x_j) < p_j(x_j); m = the first refused one, or n_b
+ *   the next token is the smallest id i with sum over k <= i of r(k) > mu sum of r  (mu from sample_words[b]),
+ *   r = max(p_m - q_m, 0), or p_m where that is zero everywhere, or p of the last row where none was refused
+ *
+ * so that the tokens are distributed as the target's.  A filter is applied by the caller: ids at -infinity have no
+ * probability.  What decides is computed in fp64; p_draft is within 2^-16 of the definition's, relative.  Two kernels.
+ */
+typedef struct {
+  const void* logits;           /* [n_drafts + B, V] of type `dtype`, row stride ld >= V elements */
+  int64_t ld;
+  int32_t dtype;                /* difr_dtype */
+  int32_t max_drafts;           /* largest n_b, 0 .. 255 */
+  const float* draft_probs;     /* [n_drafts, V], row stride ld_draft >= V, nullable; NaN counts as no probability */
+  int64_t ld_draft;
+  const int32_t* draft_tokens;  /* [n_drafts] */
+  const int32_t* offsets;       /* [B + 1], from 0 to n_drafts */
+  const uint32_t* accept_words; /* [n_drafts], e.g. words of difr_philox */
+  const uint32_t* sample_words; /* [B] */
+  float temperature;            /* >= 0 */
+  const float* temperatures;    /* [B], nullable: one per request; the scalar is then ignored */
+} difr_drafts;
+typedef struct {
+  int32_t* tokens;        /* [B, max_drafts + 1]: the accepted drafts, the next token, -1 in the rest */
+  int32_t* n_accepted;    /* [B] */
+  float* p_draft;         /* [n_drafts], nullable: p_j(x_j) of every drafted token, those behind a refusal too */
+  uint32_t* status;       /* [B], nullable.  bit0: a drafted id outside [0, V) (p = 0, refused); bit1: the row it ended at has
+                             a NaN, +infinity or no finite logit (no next token: -1); bit2: offsets descend, leave
+                             [0, n_drafts] or hold more than max_drafts; bit3: unusable temperature (2, 3: nothing accepted,
+                             all tokens -1) */
+  void* workspace;        /* >= difr_verify_workspace_bytes, 16-byte aligned; scratch */
+  size_t workspace_bytes;
+} difr_drafts_out;
+/* Scratch bytes for the sizes of a call, whatever its type; 0 for sizes the library rejects
+ * (B < 1, n_drafts < 0, V < 1 or > 2^28, more than 2^30 rows). */
+size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V);
+/* B == 0 returns DIFR_OK without launching. */
+difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_drafts, int64_t V, const difr_drafts_out* out,
+                               difr_stream_t stream);
 
 /*
  * Validation aid, not part of the scoring path: writes the fp32 logits

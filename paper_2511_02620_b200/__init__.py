@@ -22,7 +22,7 @@ EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_
            "difr_score_both", "difr_score_gm_filtered", "difr_score_ipt_filtered", "difr_score_gm_static",
            "difr_admissible", "difr_exfiltratable_bits", "difr_detect", "difr_expand_seeds", "difr_logits", "difr_philox",
            "difr_mx_codes_bytes", "difr_mx_scales_bytes", "difr_mx_quantize", "difr_mx_dequantize", "difr_rms_norm",
-           "difr_mx_logits", "difr_block_norm",
+           "difr_mx_logits", "difr_block_norm", "difr_verify_workspace_bytes", "difr_verify_drafts",
            "difr_selftest_wait", "difr_selftest_mx_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
 DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
@@ -65,6 +65,18 @@ class _CBlock(ctypes.Structure):
     _fields_ = [("post_weight", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("ld_gate", ctypes.c_int64),
                 ("post_eps", ctypes.c_float), ("scale", ctypes.c_float), ("residual_scale", ctypes.c_float),
                 ("weight_offset", ctypes.c_float)]
+
+
+class _CDrafts(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("max_drafts", ctypes.c_int32),
+                ("draft_probs", ctypes.c_void_p), ("ld_draft", ctypes.c_int64), ("draft_tokens", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p), ("accept_words", ctypes.c_void_p), ("sample_words", ctypes.c_void_p),
+                ("temperature", ctypes.c_float), ("temperatures", ctypes.c_void_p)]
+
+
+class _CDraftsOut(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_void_p), ("n_accepted", ctypes.c_void_p), ("p_draft", ctypes.c_void_p),
+                ("status", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 _lib = None
@@ -136,6 +148,10 @@ def lib() -> ctypes.CDLL:
         L.difr_block_norm.restype = ctypes.c_int
         L.difr_block_norm.argtypes = [v, i64, v, i64, ctypes.POINTER(_CBlock), v, i32, i64, i64, ctypes.c_float,
                                       ctypes.POINTER(_CNormOut), v]
+        L.difr_verify_workspace_bytes.restype = ctypes.c_size_t
+        L.difr_verify_workspace_bytes.argtypes = [i64, i64, i64]
+        L.difr_verify_drafts.restype = ctypes.c_int
+        L.difr_verify_drafts.argtypes = [ctypes.POINTER(_CDrafts), i64, i64, i64, ctypes.POINTER(_CDraftsOut), v]
         L.difr_selftest_mx_wait.restype = ctypes.c_int
         L.difr_selftest_mx_wait.argtypes = [i32, i64, i64, i64, v, i32, i64, i32, i64, v, v]
         _lib = L
@@ -604,7 +620,7 @@ def difr_selftest_mx_wait(format: int, d: int, logits, done_tiles: int, limit_cy
     return logits
 
 
-# ------------------------------------------------- a decoding step: block norm
+# ------------------------------------------------- a decoding step: block norm, verification of drafted tokens
 def difr_block_norm(x, residual, weight, eps, out: NormOut, post_weight=None, post_eps=None, gate=None, scale=1.0,
                     residual_scale=1.0, weight_offset=0.0, stream=None) -> NormOut:
     """Norms before and after a block, with its gate ([T, d], or [1, d] for all tokens) and residual scale: the stream
@@ -630,4 +646,71 @@ def difr_block_norm(x, residual, weight, eps, out: NormOut, post_weight=None, po
     block = _CBlock(post_p, gate_p, ld_gate, eps if post_eps is None else post_eps, scale, residual_scale, weight_offset)
     _call("difr_block_norm", device, stream, x.data_ptr(), ldx, residual.data_ptr(), ldr, ctypes.byref(block), weight_p,
           dtype, shape[0], shape[1], eps, ctypes.byref(_norm_out(out, shape, dtype, device)))
+    return out
+
+
+def difr_verify_workspace_bytes(B: int, n_drafts: int, V: int) -> int:
+    return int(lib().difr_verify_workspace_bytes(B, n_drafts, V))
+
+
+@dataclass(slots=True)
+class DraftOut:
+    """Output tensors and workspace of difr_verify_drafts (mirrors `difr_drafts_out`); p_draft and status may be None."""
+    tokens: "object"      # int32 [B, max_drafts + 1]: accepted drafts, the next token, -1 in the rest
+    n_accepted: "object"  # int32 [B]
+    p_draft: "object"     # float [n_drafts]: the target's probability of every drafted token
+    status: "object"      # int32 [B] (uint32 bits)
+    workspace: "object"   # uint8 [difr_verify_workspace_bytes(B, n_drafts, V)]
+
+    @staticmethod
+    def allocate(B: int, n_drafts: int, max_drafts: int, V: int, device="cuda"):
+        import torch
+
+        i = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=device)
+        return DraftOut(i(B, max_drafts + 1), i(B), torch.empty(n_drafts, dtype=torch.float32, device=device), i(B),
+                        torch.empty(difr_verify_workspace_bytes(B, n_drafts, V), dtype=torch.uint8, device=device))
+
+
+def _vector(t, name, dtype, n, device):
+    """Address of a contiguous CUDA vector of n elements."""
+    if not isinstance(t, _torch.Tensor) or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} [{n}]")
+    if t.get_device() != device:
+        raise TypeError(f"{name} is on {t.device}, not on CUDA device {device}")
+    return t.data_ptr()
+
+
+def difr_verify_drafts(logits, draft_tokens, offsets, accept_words, sample_words, temperature, out: DraftOut,
+                       draft_probs=None, stream=None) -> DraftOut:
+    """Accepts or refuses drafted tokens against the target's logits [n_drafts + B, V] from given random words (uint32 bits
+    in int32 tensors) and samples each request's next token; `temperature` is a number or a float tensor [B].  Request b
+    has drafts offsets[b] .. offsets[b + 1] and rows offsets[b] + b ..; see include/difr.h."""
+    dtype, ld, device = _matrix(logits, "logits", _ANY_DTYPE)
+    rows, V = logits.shape
+    i32 = _torch.int32
+    B, D = sample_words.shape[0], draft_tokens.shape[0]
+    if rows != D + B:
+        raise TypeError(f"logits: expected {D} + {B} rows, got {rows}")
+    probs_p, ld_probs = None, 0
+    if draft_probs is not None:
+        ld_probs = _matrix(draft_probs, "draft_probs", (DIFR_F32,), (D, V), device)[1]
+        probs_p = draft_probs.data_ptr()
+    temps_p = None
+    if isinstance(temperature, _torch.Tensor):
+        temps_p = _vector(temperature, "temperature", _torch.float32, B, device)
+        temperature = 0.0
+    tokens, ws = out.tokens, out.workspace
+    if (not isinstance(tokens, _torch.Tensor) or tokens.dtype != i32 or tokens.dim() != 2 or tokens.shape[0] != B
+            or tokens.shape[1] < 1 or not tokens.is_contiguous() or tokens.get_device() != device):
+        raise TypeError(f"out.tokens must be a contiguous int32 [{B}, max_drafts + 1] on CUDA device {device}")
+    if not isinstance(ws, _torch.Tensor) or ws.dtype != _torch.uint8 or not ws.is_contiguous() or ws.get_device() != device:
+        raise TypeError(f"out.workspace must be contiguous bytes (uint8) on CUDA device {device}")
+    c = _CDrafts(logits.data_ptr(), ld, dtype, tokens.shape[1] - 1, probs_p, ld_probs,
+                 _vector(draft_tokens, "draft_tokens", i32, D, device), _vector(offsets, "offsets", i32, B + 1, device),
+                 _vector(accept_words, "accept_words", i32, D, device),
+                 _vector(sample_words, "sample_words", i32, B, device), temperature, temps_p)
+    o = _CDraftsOut(tokens.data_ptr(), _vector(out.n_accepted, "out.n_accepted", i32, B, device),
+                    None if out.p_draft is None else _vector(out.p_draft, "out.p_draft", _torch.float32, D, device),
+                    None if out.status is None else _vector(out.status, "out.status", i32, B, device), ws.data_ptr(), ws.numel())
+    _call("difr_verify_drafts", device, stream, ctypes.byref(c), B, D, V, ctypes.byref(o))
     return out

@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(CSRC, "libdifr.so")
 SOURCES = ["difr_api.cu", "difr_mx_api.cu", "k0_expand_seeds.cu", "k1_fused_score.cu", "k2_finalize.cu",
            "k2_filtered.cu", "k2_select.cu", "k3_detect.cu", "k4_norm.cu", "k5_mx_convert.cu", "k6_mx_logits.cu",
-           "difr_step_api.cu", "k7_block_norm.cu"]
+           "difr_step_api.cu", "k7_block_norm.cu", "k10_verify.cu"]
 HEADERS = ["difr_device.cuh", "difr_host.h", "difr_kernels.h", "difr_plan.h", "mx_device.cuh", "mx_kernels.h", "norm_device.cuh",
            "step_kernels.h",
            os.path.join("..", "..", "include", "difr.h")]

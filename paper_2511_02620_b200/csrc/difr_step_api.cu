@@ -1,4 +1,4 @@
-// C ABI of a decoding step's operators: the block norm.  Argument checks and launches; nothing here computes.
+// C ABI of a decoding step's operators: block norm, verification of drafted tokens.  Argument checks and launches; nothing here computes.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -35,6 +35,15 @@ difr_status device_sms(int* sms) {
   if (n < 0) return DIFR_ERR_ARCH;
   *sms = n;
   return DIFR_OK;
+}
+
+// Records of a row: its vectors, of which the first may begin before the row.
+int64_t verify_chunks(int64_t V, int elem) {
+  const int64_t n = 16 / elem;
+  return ((V + 2 * (n - 1)) / n + kVerifyChunkVecs - 1) / kVerifyChunkVecs;
+}
+bool verify_supported(int64_t B, int64_t n_drafts, int64_t V) {
+  return n_drafts + B <= kMaxRows && V <= ((int64_t)1 << 28) && B <= ((int64_t)1 << 27);
 }
 
 }  // namespace
@@ -84,6 +93,46 @@ difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, in
           (!out->residual || vector_rows(out->residual, out->ld_residual, dtype)) &&
           (!out->h || vector_rows(out->h, out->ldh, DIFR_BF16));
   return launch_block_norm(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+}
+
+size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {
+  if (B < 1 || n_drafts < 0 || V < 1 || B > kMaxRows || n_drafts > kMaxRows || !verify_supported(B, n_drafts, V)) return 0;
+  return (size_t)(n_drafts + B) * (size_t)verify_chunks(V, 4) * sizeof(float4);
+}
+
+difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_drafts, int64_t V, const difr_drafts_out* out,
+                               difr_stream_t stream) {
+  if (!in || !out || !known_dtype(in->dtype) || B < 0 || n_drafts < 0 || V <= 0) return DIFR_ERR_INVALID_ARG;
+  if (in->max_drafts < 0 || in->max_drafts > kVerifyMaxDrafts) return DIFR_ERR_INVALID_ARG;
+  if (!in->temperatures && (!(in->temperature >= 0.f) || !isfinite(in->temperature))) return DIFR_ERR_INVALID_ARG;
+  if (in->ld < V || (in->draft_probs && in->ld_draft < V)) return DIFR_ERR_INVALID_ARG;
+  if (B > kMaxRows || n_drafts > kMaxRows || !verify_supported(B, n_drafts, V) || in->ld > kMaxLd ||
+      (in->draft_probs && in->ld_draft > kMaxLd))
+    return DIFR_ERR_SHAPE;
+  if (B == 0) return DIFR_OK;
+  if (!in->logits || !in->offsets || !in->sample_words || !out->tokens || !out->n_accepted) return DIFR_ERR_INVALID_ARG;
+  if (n_drafts > 0 && (!in->draft_tokens || !in->accept_words)) return DIFR_ERR_INVALID_ARG;
+  if (!aligned_to(in->logits, elem_bytes(in->dtype)) || !aligned_to(in->draft_probs, 4) || !aligned_to(in->draft_tokens, 4) ||
+      !aligned_to(in->offsets, 4) || !aligned_to(in->accept_words, 4) || !aligned_to(in->sample_words, 4) ||
+      !aligned_to(in->temperatures, 4) || !aligned_to(out->tokens, 4) || !aligned_to(out->n_accepted, 4) ||
+      !aligned_to(out->p_draft, 4) || !aligned_to(out->status, 4) || !aligned16(out->workspace))
+    return DIFR_ERR_ALIGN;
+  VerifyParams p;
+  memset(&p, 0, sizeof p);
+  p.chunks = (int)verify_chunks(V, elem_bytes(in->dtype));
+  if (!out->workspace || out->workspace_bytes < (size_t)(n_drafts + B) * (size_t)p.chunks * sizeof(float4))
+    return DIFR_ERR_WORKSPACE;
+  int sms = 0;
+  const difr_status ds = device_sms(&sms);
+  if (ds != DIFR_OK) return ds;
+  p.logits = in->logits; p.probs = in->draft_probs; p.drafted = in->draft_tokens; p.offsets = in->offsets;
+  p.accept_words = in->accept_words; p.sample_words = in->sample_words;
+  p.temperatures = in->temperatures; p.temperature = in->temperature;
+  p.tokens = out->tokens; p.n_accepted = out->n_accepted; p.p_draft = out->p_draft; p.status = out->status;
+  p.records = static_cast<float4*>(out->workspace);
+  p.ld = in->ld; p.ld_probs = in->ld_draft;
+  p.B = (int)B; p.n_drafts = (int)n_drafts; p.V = (int)V; p.max_drafts = in->max_drafts;
+  return launch_verify_drafts(p, in->dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
 }
 
 }  // extern "C"

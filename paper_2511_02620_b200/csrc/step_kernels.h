@@ -27,4 +27,27 @@ struct BlockNormParams {
 };
 cudaError_t launch_block_norm(const BlockNormParams& p, int dtype, cudaStream_t stream);
 
+struct VerifyParams {
+  const void* logits;            // [n_drafts + B][ld]
+  const float* probs;            // [n_drafts][ld_probs], nullable
+  const int32_t* drafted;        // [n_drafts]
+  const int32_t* offsets;        // [B + 1]
+  const uint32_t* accept_words;  // [n_drafts]
+  const uint32_t* sample_words;  // [B]
+  const float* temperatures;     // [B], nullable
+  int32_t* tokens;               // [B][max_drafts + 1]
+  int32_t* n_accepted;           // [B]
+  float* p_draft;                // [n_drafts], nullable
+  uint32_t* status;              // [B], nullable
+  float4* records;               // [n_drafts + B][chunks]: largest logit, sum of exponentials, first id of the largest
+  int64_t ld, ld_probs;
+  float temperature;
+  int B, n_drafts, V, max_drafts, chunks;
+};
+constexpr int kVerifyMaxDrafts = 255;
+constexpr int kVerifyChunkVecs = 1024;  // 16-byte vectors of logits per record
+// the bits of difr_drafts_out.status
+constexpr uint32_t kDraftBadToken = 1, kDraftBadRow = 2, kDraftBadOffsets = 4, kDraftBadTemperature = 8;
+cudaError_t launch_verify_drafts(const VerifyParams& p, int dtype, cudaStream_t stream);
+
 }  // namespace difr

@@ -20,3 +20,68 @@ def block_stream(x, residual, post_weight, post_eps, gate, scale, residual_scale
         n = n * gate.double()
     a, b = f32(residual_scale) * residual.double(), f32(scale) * n
     return a + b, a.abs() + b.abs()
+
+
+def uniform(word):
+    return ((int(word) % 2 ** 32) + 0.5) / 2 ** 32
+
+
+def probabilities(row, temperature):
+    """softmax of one row of logits in 64 bits; None where the row is broken."""
+    row = row.double()
+    if torch.isnan(row).any() or (row == float("inf")).any() or not torch.isfinite(row).any():
+        return None
+    if temperature == 0:
+        p = torch.zeros_like(row)
+        p[int((row == row.max()).nonzero()[0, 0])] = 1.0
+        return p
+    e = torch.exp((row - row.max()) / temperature)
+    return e / e.sum()
+
+
+def verify(logits, drafted, offsets, accept_words, sample_words, temperatures, max_drafts, probs=None):
+    """(tokens, n_accepted, p_draft, status) request by request, as the header tells it; one temperature per request."""
+    B, V = len(sample_words), logits.shape[1]
+    D = len(drafted)
+    tokens = torch.full((B, max_drafts + 1), -1, dtype=torch.int32)
+    n_accepted = torch.zeros(B, dtype=torch.int32)
+    status = torch.zeros(B, dtype=torch.int32)
+    p_draft = torch.full((D,), float("nan"), dtype=torch.float64)
+    for b in range(B):
+        o0, o1, t = int(offsets[b]), int(offsets[b + 1]), f32(float(temperatures[b]))
+        if o0 < 0 or o1 < o0 or o1 > D or o1 - o0 > max_drafts:
+            status[b] |= 4
+        if not (t >= 0) or t == float("inf"):
+            status[b] |= 8
+        if status[b]:
+            continue
+        P = [probabilities(logits[o0 + b + j], t) for j in range(o1 - o0 + 1)]
+        known = [0 <= int(drafted[i]) < V for i in range(o0, o1)]
+        if not all(known):
+            status[b] |= 1
+        for j in range(o1 - o0):
+            if P[j] is not None:
+                p_draft[o0 + j] = float(P[j][int(drafted[o0 + j])]) if known[j] else 0.0
+        m, refused = 0, False
+        while m < o1 - o0 and P[m] is not None:
+            x = int(drafted[o0 + m])
+            q = 1.0 if probs is None else float(probs[o0 + m, x]) if known[m] else 0.0
+            refused = not (uniform(accept_words[o0 + m]) * q < float(p_draft[o0 + m]))
+            if refused:
+                break
+            tokens[b, m] = x
+            m += 1
+        n_accepted[b] = m
+        if P[m] is None:
+            status[b] |= 2
+            continue
+        r = P[m].clone()
+        if refused and probs is not None:
+            r = (r - torch.nan_to_num(probs[o0 + m].double(), nan=float("inf"))).clamp(min=0)
+        elif refused and known[m]:
+            r[int(drafted[o0 + m])] = 0
+        if float(r.sum()) <= 0:
+            r = P[m]
+        c = torch.cumsum(r, 0)
+        tokens[b, m] = int(torch.searchsorted(c, c[-1:] * uniform(sample_words[b]), right=True).clamp(max=int(r.nonzero()[-1])))
+    return tokens, n_accepted, p_draft, status

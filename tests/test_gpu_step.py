@@ -168,3 +168,290 @@ def test_block_norm_refusals():
             difr.difr_block_norm(x, x, weight, 1e-6, o)
     empty = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
     difr.difr_block_norm(empty, empty, w, 1e-6, difr.NormOut(h=empty))
+
+
+# ------------------------------------------------------------------ verification of drafted tokens
+def make_drafts(B, K, V, dtype, probs, temperature, seed=0, ragged=True, near=0.6):
+    """Target logits, drafts sampled near them, words; `temperature` per request or one for all."""
+    g = torch.Generator().manual_seed(seed)
+    n = [int(torch.randint(0, K + 1, (1,), generator=g)) if ragged else K for _ in range(B)]
+    off = torch.tensor([0] + n).cumsum(0).to(torch.int32)
+    D = int(off[-1])
+    logits = (2.5 * torch.randn(D + B, V, generator=g)).to(DTYPES[dtype])
+    t = torch.as_tensor(temperature, dtype=torch.float32).expand(B)
+    drafted = torch.zeros(D, dtype=torch.int32)
+    q = torch.zeros(D, V)
+    for b in range(B):
+        for j in range(n[b]):
+            i = int(off[b]) + j
+            z = (logits[i + b].float() + near * torch.randn(V, generator=g)) / (float(t[b]) or 0.5)
+            q[i] = torch.softmax(z, 0)
+            drafted[i] = int(torch.multinomial(q[i], 1, generator=g))
+    words = lambda k: torch.randint(-2 ** 31, 2 ** 31, (k,), generator=g, dtype=torch.int64).to(torch.int32)
+    return dict(logits=logits, drafted=drafted, offsets=off, accept=words(D), sample=words(B), t=t, K=K,
+                probs=q if probs else None)
+
+
+def run_verify(s, out=None, **kw):
+    B, D, V = s["sample"].numel(), s["drafted"].numel(), s["logits"].shape[1]
+    if out is None:
+        out = difr.DraftOut.allocate(B, D, s["K"], V)
+        for x in (out.tokens, out.n_accepted, out.status):
+            x.fill_(-77)
+        out.p_draft.fill_(math.nan)
+        out.workspace.fill_(0xAB)
+    t = s["t"]
+    one = float(t[0]) if B and torch.all(t == t[0]) else t.contiguous().cuda()
+    c = lambda x: None if x is None else x.cuda()
+    return difr.difr_verify_drafts(c(s["logits"]), c(s["drafted"]), c(s["offsets"]), c(s["accept"]), c(s["sample"]), one, out,
+                                   draft_probs=c(s["probs"]), **kw)
+
+
+def check_verify(s, out=None):
+    out = run_verify(s) if out is None else out
+    tokens, n, p, status = ref.verify(s["logits"], s["drafted"], s["offsets"], s["accept"], s["sample"], s["t"], s["K"], s["probs"])
+    assert torch.equal(out.n_accepted.cpu(), n)
+    assert torch.equal(out.tokens.cpu(), tokens)
+    assert torch.equal(out.status.cpu(), status)
+    got = out.p_draft.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(p))
+    err = (got - p).abs()
+    assert torch.all(torch.isnan(p) | (err <= 2.0 ** -16 * p + 2.0 ** -149))
+    return out
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temperature", [0.0, 0.7, 1.0, 8.0])
+@pytest.mark.parametrize("probs", [True, False])
+@pytest.mark.parametrize("B,K,V", [(1, 0, 1), (1, 1, 2), (5, 3, 7), (9, 4, 33), (64, 5, 1000), (3, 4, 4096), (4, 2, 8193), (7, 8, 32003)])
+def test_verification(B, K, V, probs, temperature, dtype):
+    check_verify(make_drafts(B, K, V, dtype, probs, temperature, seed=B + V))
+
+
+@pytest.mark.parametrize("B,K,V,dtype", [(2, 3, 151937, "bf16"), (1, 4, 128256, "f32"), (1, 1, 1000003, "f16")])
+def test_verification_of_large_vocabularies(B, K, V, dtype):
+    check_verify(make_drafts(B, K, V, dtype, True, 1.0, seed=V, ragged=False))
+
+
+def test_many_requests_of_one_draft_each_and_the_longest_drafts():
+    check_verify(make_drafts(3000, 1, 50, "f32", True, 1.0, seed=1))
+    check_verify(make_drafts(2, 255, 40, "f32", True, 1.0, seed=2, ragged=False, near=0.01))
+
+
+def test_a_temperature_per_request():
+    """Zero, small and large ones in one batch, and values that are none."""
+    t = torch.tensor([0.0, 0.1, 1.0, 30.0, -1.0, math.nan, math.inf, 1e-40, 1e30, 0.5])
+    s = make_drafts(10, 4, 1003, "f32", True, t.nan_to_num(1.0, 1.0).clamp(min=0), seed=3)
+    s["t"] = t
+    out = check_verify(s)
+    assert out.status.tolist() == [0, 0, 0, 0, 8, 8, 8, 0, 0, 0]
+
+
+def test_acceptance_next_to_the_border():
+    """Draft probabilities within 2^-22 of p / mu, on both sides: decided as in 64 bits."""
+    B, V = 400, 5000
+    s = make_drafts(B, 1, V, "f32", True, 1.0, seed=4, ragged=False)
+    side = 0
+    for b in range(B):
+        p = ref.probabilities(s["logits"][2 * b], 1.0)
+        x = int(s["drafted"][b])
+        s["probs"][b, x] = float(p[x]) / ref.uniform(s["accept"][b]) * (1 + (-1) ** b * 2.0 ** -22)
+    out = check_verify(s)
+    assert 150 < int(out.n_accepted.sum()) < 250
+
+
+def test_samples_next_to_the_borders_of_ids():
+    """Equal logits: id i ends at (i + 1) / V.  Words one below and one above that border."""
+    V = 4096
+    at = torch.tensor([0, 1, 17, 511, 512, 513, 2047, 3000, 4094])
+    word = ((at + 1) * (2 ** 32 // V)).repeat_interleave(2) - torch.tensor([1, 0]).repeat(at.numel())
+    word = torch.where(word >= 2 ** 31, word - 2 ** 32, word).to(torch.int32)
+    B = word.numel()
+    s = dict(logits=torch.full((B, V), 3.25), drafted=torch.zeros(0, dtype=torch.int32), offsets=torch.zeros(B + 1, dtype=torch.int32),
+             accept=torch.zeros(0, dtype=torch.int32), sample=word, t=torch.ones(B), K=0, probs=None)
+    out = check_verify(s)
+    assert out.tokens[:, 0].tolist() == [v for i in at.tolist() for v in (i, i + 1)]
+
+
+def test_extreme_words():
+    """The smallest and the largest word: first and last id with any probability left."""
+    V = 3000
+    logits = torch.full((4, V), -math.inf)
+    logits[:, 100:2900] = randn(4, 2800, seed=6)
+    s = dict(logits=logits, drafted=torch.zeros(0, dtype=torch.int32), offsets=torch.zeros(5, dtype=torch.int32),
+             accept=torch.zeros(0, dtype=torch.int32), sample=torch.tensor([0, -1, 0, -1], dtype=torch.int32), t=torch.ones(4), K=0,
+             probs=None)
+    out = check_verify(s)
+    assert out.tokens[:, 0].tolist() == [100, 2899, 100, 2899]
+
+
+def test_masked_and_broken_rows():
+    """Rows of masked ids, a single finite id, the type's lowest value as a mask; NaN, +infinity and nothing but -infinity stop a
+    request where it reaches them, and only there."""
+    B, K, V = 12, 2, 777
+    s = make_drafts(B, K, V, "f32", True, 1.0, seed=7, ragged=False, near=0.05)
+    l = s["logits"]
+    for b in range(B):
+        r = (K + 1) * b
+        if b == 0:
+            l[r, 5:] = -math.inf
+        elif b == 1:
+            l[r, :] = -math.inf
+            l[r, 400] = -3e38
+        elif b == 2:
+            l[r, 1:] = torch.finfo(torch.float32).min
+        elif b == 3:
+            l[r, 9] = math.nan
+        elif b == 4:
+            l[r, 776] = math.inf
+        elif b == 5:
+            l[r, :] = -math.inf
+        elif b == 6:
+            l[r + 1, 3] = math.nan
+        elif b == 7:
+            l[r + 2, 3] = math.nan
+        elif b == 8:
+            l[r] = torch.finfo(torch.float32).min
+        elif b == 9:
+            l[r] = torch.finfo(torch.float32).max
+    out = check_verify(s)
+    assert out.status[3:6].tolist() == [2, 2, 2] and out.n_accepted[3:6].tolist() == [0, 0, 0]
+    assert torch.all(out.tokens[3:6] == -1)
+    s["probs"] = None
+    check_verify(s)
+    s["t"] = torch.zeros(B)
+    check_verify(s)
+
+
+def test_drafts_that_are_no_ids_and_probabilities_that_are_none():
+    B, K, V = 40, 3, 300
+    for probs in (True, False):
+        s = make_drafts(B, K, V, "f32", probs, 1.0, seed=8, near=0.05)
+        s["drafted"][::3] = V
+        s["drafted"][1::5] = -1
+        s["drafted"][2::7] = 2 ** 31 - 1
+        if probs:
+            s["probs"][::4, 11] = math.nan
+            s["probs"][1::4] = math.nan
+        out = check_verify(s)
+        assert int((out.status == 1).sum()) > 5
+        s["t"] = torch.zeros(B)
+        check_verify(s)
+
+
+def test_a_draft_that_leaves_nothing():
+    """q at or above p everywhere (q = p counts as such in 64 bits only where p is a short number): p itself is sampled."""
+    V = 64
+    s = make_drafts(30, 1, V, "f32", True, 1.0, seed=9, ragged=False)
+    s["logits"][:] = 1.0
+    s["probs"][:] = 1.0  # no distribution: refuses nearly every draft and leaves nothing of p = 1 / 64
+    out = check_verify(s)
+    assert int((out.n_accepted == 0).sum()) >= 25 and int(out.tokens.max()) < V
+
+
+def test_offsets_that_are_none():
+    s = make_drafts(6, 4, 100, "f32", True, 1.0, seed=10, ragged=False)
+    s["offsets"] = torch.tensor([0, 4, 2, 8, 30, -1, 3], dtype=torch.int32)
+    out = check_verify_status(s)
+    assert out.status.tolist() == [0, 4, 4, 4, 4, 4]
+    assert torch.all(out.tokens[1:] == -1) and torch.all(out.n_accepted[1:] == 0)
+
+
+def check_verify_status(s):
+    out = run_verify(s)
+    tokens, n, _, status = ref.verify(s["logits"], s["drafted"], s["offsets"], s["accept"], s["sample"], s["t"], s["K"], s["probs"])
+    assert torch.equal(out.tokens.cpu(), tokens) and torch.equal(out.n_accepted.cpu(), n) and torch.equal(out.status.cpu(), status)
+    return out
+
+
+@pytest.mark.parametrize("dtype,ld,offset", [("f32", 1001, 0), ("f32", 1003, 1), ("bf16", 1001, 0), ("bf16", 1007, 3), ("f16", 1024, 5)])
+def test_rows_at_every_alignment(dtype, ld, offset):
+    V = 997
+    s = make_drafts(6, 3, V, dtype, True, 1.0, seed=11)
+    want = check_verify(s)
+    rows, D = s["logits"].shape[0], s["drafted"].numel()
+    buf = torch.full((rows * ld + 16,), math.nan, dtype=DTYPES[dtype], device="cuda")
+    lg = torch.as_strided(buf, (rows, V), (ld, 1), offset).copy_(s["logits"].cuda())
+    qbuf = torch.full((D * ld + 16,), math.nan, device="cuda")
+    q = torch.as_strided(qbuf, (D, V), (ld, 1), offset).copy_(s["probs"].cuda())
+    out = difr.DraftOut.allocate(6, D, 3, V)
+    c = lambda x: s[x].cuda()
+    difr.difr_verify_drafts(lg, c("drafted"), c("offsets"), c("accept"), c("sample"), 1.0, out, draft_probs=q)
+    assert torch.equal(out.tokens, want.tokens) and torch.equal(out.n_accepted, want.n_accepted)
+
+
+def test_verification_captured_replayed_and_on_another_stream():
+    s = make_drafts(5, 4, 3001, "bf16", True, 0.9, seed=12)
+    dev = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in s.items()}
+    D = s["drafted"].numel()
+    out = difr.DraftOut.allocate(5, D, 4, 3001)
+    args = (dev["logits"], dev["drafted"], dev["offsets"], dev["accept"], dev["sample"], 0.9, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        difr.difr_verify_drafts(*args, draft_probs=dev["probs"])
+    for seed in (13, 14):
+        new = torch.randint(-2 ** 31, 2 ** 31, (5,), generator=torch.Generator().manual_seed(seed), dtype=torch.int64).to(torch.int32)
+        s["sample"] = new
+        dev["sample"].copy_(new)
+        graph.replay()
+        check_verify(s, out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = difr.DraftOut.allocate(5, D, 4, 3001)
+    difr.difr_verify_drafts(*args[:-1], other, draft_probs=dev["probs"], stream=side)
+    side.synchronize()
+    assert torch.equal(other.tokens, out.tokens)
+
+
+def test_verified_tokens_have_the_targets_distribution():
+    """Words of the library's own Philox; the next token after a draft of one, over 40000 requests, is distributed as p."""
+    V, B = 12, 40000
+    g = torch.Generator().manual_seed(15)
+    target, draft = torch.randn(V, generator=g) * 1.5, torch.randn(V, generator=g) * 1.5
+    q = torch.softmax(draft, 0)
+    ctr = torch.zeros(2 * B, 4, dtype=torch.int32)
+    ctr[:, 0] = torch.arange(2 * B)
+    words = difr.difr_philox(ctr.cuda(), torch.full((2 * B, 2), 99, dtype=torch.int32).cuda(), torch.empty(2 * B, 4, dtype=torch.int32, device="cuda"))
+    drafted = torch.multinomial(q, B, replacement=True, generator=g).to(torch.int32).cuda()
+    out = difr.DraftOut.allocate(B, B, 1, V)
+    difr.difr_verify_drafts(target.cuda().expand(2 * B, V).contiguous(), drafted, torch.arange(B + 1, dtype=torch.int32, device="cuda"),
+                            words[:B, 0].contiguous(), words[B:, 0].contiguous(), 1.0, out, draft_probs=q.cuda().expand(B, V).contiguous())
+    first = torch.bincount(out.tokens[:, 0].long().cpu(), minlength=V).double() / B
+    p = torch.softmax(target.double(), 0)
+    # five standard deviations of each frequency
+    assert torch.all((first - p).abs() <= 5 * torch.sqrt(p * (1 - p) / B))
+    assert abs(float(out.n_accepted.double().mean()) - float(torch.minimum(p, q.double()).sum())) <= 5 * 0.5 / math.sqrt(B)
+
+
+def test_verification_refusals():
+    s = make_drafts(3, 2, 50, "f32", True, 1.0, seed=16, ragged=False)
+    d = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in s.items()}
+    out = difr.DraftOut.allocate(3, 6, 2, 50)
+
+    def call(o=out, temperature=1.0, **kw):
+        a = {**d, **kw}
+        return difr.difr_verify_drafts(a["logits"], a["drafted"], a["offsets"], a["accept"], a["sample"], temperature, o,
+                                       draft_probs=a["probs"])
+
+    call()
+    for bad in (dict(logits=d["logits"][:-1]), dict(logits=d["logits"].double()), dict(logits=d["logits"].T), dict(drafted=d["drafted"].long()),
+                dict(drafted=d["drafted"][:-1]), dict(offsets=d["offsets"][:-1]), dict(accept=s["accept"]), dict(sample=d["sample"][:2]),
+                dict(probs=d["probs"][:, :-1]), dict(probs=d["probs"].half()), dict(temperature=torch.ones(2, device="cuda"))):
+        with pytest.raises(TypeError):
+            call(**bad)
+    for bad in (dict(o=difr.DraftOut(out.tokens.long(), out.n_accepted, out.p_draft, out.status, out.workspace)),
+                dict(o=difr.DraftOut(out.tokens, out.n_accepted[:2], out.p_draft, out.status, out.workspace)),
+                dict(o=difr.DraftOut(out.tokens, out.n_accepted, out.p_draft[:2], out.status, out.workspace)),
+                dict(o=difr.DraftOut(out.tokens, out.n_accepted, out.p_draft, out.status, out.workspace.float()))):
+        with pytest.raises(TypeError):
+            call(**bad)
+    for status, bad in ((-4, dict(o=difr.DraftOut(out.tokens, out.n_accepted, out.p_draft, out.status, out.workspace[:16]))),
+                        (-1, dict(temperature=-0.5)), (-1, dict(temperature=math.nan)), (-1, dict(temperature=math.inf)),
+                        (-3, dict(o=difr.DraftOut(out.tokens, out.n_accepted, out.p_draft, out.status, out.workspace[8:])))):
+        with pytest.raises(difr.DifrError) as e:
+            call(**bad)
+        assert e.value.status == status
+    call(o=difr.DraftOut(out.tokens, out.n_accepted, None, None, out.workspace))
+    e = lambda *shape: torch.empty(*shape, dtype=torch.int32, device="cuda")
+    difr.difr_verify_drafts(torch.empty(0, 50, device="cuda"), e(0), torch.zeros(1, dtype=torch.int32, device="cuda"), e(0), e(0), 1.0,
+                            difr.DraftOut(e(0, 3), e(0), None, None, torch.empty(0, dtype=torch.uint8, device="cuda")))

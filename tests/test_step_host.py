@@ -64,9 +64,50 @@ def struct_layouts(structs):
 
 
 def test_structs_have_the_headers_layout():
-    structs = {"difr_block": difr._CBlock}
+    structs = {"difr_block": difr._CBlock, "difr_drafts": difr._CDrafts, "difr_drafts_out": difr._CDraftsOut}
     got = struct_layouts(structs)
     for name, cls in structs.items():
         assert int(got[name]) == ctypes.sizeof(cls), name
         for f, _ in cls._fields_:
             assert int(got[f"{name}.{f}"]) == getattr(cls, f).offset, (name, f)
+
+
+def test_sizes_of_the_verification():
+    size = difr.difr_verify_workspace_bytes
+    assert size(1, 0, 1) == 16 and size(2, 3, 4096) == 5 * 2 * 16 and size(2, 3, 4090) == 5 * 16
+    for bad in ((0, 0, 10), (1, -1, 10), (1, 0, 0), (1, 0, (1 << 28) + 1), (1, 1 << 30, 10), ((1 << 27) + 1, 0, 10)):
+        assert size(*bad) == 0
+
+
+@host_only
+def test_refusals_of_the_verification():
+    fields = dict(logits=P, ld=100, dtype=2, max_drafts=4, draft_probs=P, ld_draft=100, draft_tokens=P, offsets=P, accept_words=P,
+                  sample_words=P, temperature=1.0, temperatures=None)
+    outs = dict(tokens=P, n_accepted=P, p_draft=P, status=P, workspace=P, workspace_bytes=1 << 20)
+
+    def verify(B=3, D=6, V=100, **kw):
+        i, o = difr._CDrafts(), difr._CDraftsOut()
+        for k, v in {**fields, **kw}.items():
+            if k in fields:
+                setattr(i, k, v)
+        for k, v in {**outs, **kw}.items():
+            if k in outs:
+                setattr(o, k, v)
+        return difr.lib().difr_verify_drafts(ctypes.byref(i), B, D, V, ctypes.byref(o), None)
+
+    assert verify() == CUDA and verify(p_draft=None, status=None, draft_probs=None) == CUDA
+    for name in ("logits", "draft_tokens", "offsets", "accept_words", "sample_words", "tokens", "n_accepted"):
+        assert verify(**{name: None}) == INVALID, name
+    assert verify(D=0, draft_tokens=None, accept_words=None) == CUDA
+    for name in ("draft_probs", "draft_tokens", "offsets", "accept_words", "sample_words", "temperatures", "tokens", "n_accepted",
+                 "p_draft", "status"):
+        assert verify(**{name: P + 2}) == ALIGN, name
+    assert verify(logits=P + 1, dtype=0) == ALIGN and verify(workspace=ODD) == ALIGN
+    assert verify(dtype=3) == INVALID and verify(max_drafts=-1) == INVALID and verify(max_drafts=256) == INVALID
+    assert verify(B=-1) == INVALID and verify(D=-1) == INVALID and verify(V=0) == INVALID
+    assert verify(ld=99) == INVALID and verify(ld_draft=99) == INVALID and verify(ld_draft=99, draft_probs=None) == CUDA
+    for t in (-1.0, float("nan"), float("inf")):
+        assert verify(temperature=t) == INVALID and verify(temperature=t, temperatures=P) == CUDA
+    assert verify(V=(1 << 28) + 1, ld=1 << 29, ld_draft=1 << 29) == SHAPE and verify(B=1 << 28) == SHAPE
+    assert verify(workspace=None) == WORKSPACE and verify(workspace_bytes=difr.difr_verify_workspace_bytes(3, 6, 100) - 1) == WORKSPACE
+    assert verify(B=0, logits=None, offsets=None) == OK
