@@ -19,9 +19,10 @@
  *   LM head      difr_rms_norm (the final norm: the h that scoring takes, also in 8 or 4 bits), difr_mx_quantize,
  *                difr_mx_dequantize, difr_mx_logits (a head held in 8 or 4 bits)
  *   decoding     difr_block_norm (the norms before and after a block, with its gate and residual scale),
+ *                difr_w4_quantize, difr_w4_dequantize, difr_w4_logits (a head held as 4-bit integers with group scales),
  *                difr_verify_drafts (drafted tokens against the target's logits, from given random words)
  *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes,
- *                difr_verify_workspace_bytes
+ *                difr_w4_codes_bytes, difr_w4_scales_bytes, difr_w4_workspace_bytes, difr_verify_workspace_bytes
  *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_debug_plan_override,
  *                difr_status_string, difr_version
  *
@@ -537,6 +538,38 @@ typedef struct {
 difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, int64_t ld_residual, const difr_block* block,
                             const void* weight, int32_t dtype, int64_t T, int64_t d, float eps, const difr_norm_out* out,
                             difr_stream_t stream);
+
+/*
+ * 4-bit weights with group scales, for heads of servers that quantise weights alone: a value is an integer code -8 .. 7
+ * times the bf16 scale of its group of `group` = 32, 64 or 128 values along a row; the hidden states stay bf16.
+ *
+ * codes  [rows][pitch] bytes, pitch = 16 ceil(d / 32): two's complement, two to a byte, the even column in the low half;
+ *        the columns behind d zero.  16-byte aligned.
+ * scales bf16 [rows][8 ceil(groups / 8)], groups = ceil(d / group), those behind the last group zero.  16-byte aligned.
+ *
+ * difr_w4_quantize: scale = bf16(largest magnitude of the group / 7), below 2^-126: 0; code = value / scale rounded to the
+ * nearest integer, ties to even, by the quotient itself; zero where the scale is.  A group with a NaN or an infinity gets the
+ * scale NaN and zero codes: all its values are NaN, and so are the logits of its id.  (Codes of -8 and scales of either sign
+ * come from other quantisers only.)
+ * difr_w4_dequantize: DIFR_F32 exact, DIFR_BF16 rounded (a product has up to eleven bits), where it does not leave the
+ * normal numbers.
+ */
+size_t difr_w4_codes_bytes(int64_t rows, int64_t d);                /* 0 for sizes the library rejects, as for the */
+size_t difr_w4_scales_bytes(int64_t rows, int64_t d, int32_t group); /* microscaled formats, or an unknown group    */
+difr_status difr_w4_quantize(const void* x, int32_t dtype, int64_t rows, int64_t d, int64_t ldx, int32_t group, void* codes,
+                             void* scales, difr_stream_t stream);
+difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t group, int64_t rows, int64_t d, void* out,
+                               int32_t dtype, int64_t ldo, difr_stream_t stream);
+
+/*
+ * logits[t, v] = h[t, :] . W[v, :] with h bf16 [T, d] (row stride ldh >= d) and W [V, d] in 4 bits, accumulated in fp32;
+ * `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or DIFR_BF16.  Any T from 1, any V from 1, any d.
+ * The logits of a row of h with a NaN or an infinity are NaN, and so are those of an id with such a scale.
+ */
+size_t difr_w4_workspace_bytes(int64_t T, int64_t d);  /* scratch bytes of a call; 0 for sizes the library rejects */
+difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, const void* W_scales, int32_t group, int64_t T,
+                           int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, void* workspace,
+                           size_t workspace_bytes, int32_t* device_status, difr_stream_t stream);
 
 /*
  * Verification of drafted tokens (speculative decoding): what a server does with a draft, and a verifier that knows its

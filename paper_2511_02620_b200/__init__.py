@@ -23,6 +23,8 @@ EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_
            "difr_admissible", "difr_exfiltratable_bits", "difr_detect", "difr_expand_seeds", "difr_logits", "difr_philox",
            "difr_mx_codes_bytes", "difr_mx_scales_bytes", "difr_mx_quantize", "difr_mx_dequantize", "difr_rms_norm",
            "difr_mx_logits", "difr_block_norm", "difr_verify_workspace_bytes", "difr_verify_drafts",
+           "difr_w4_codes_bytes", "difr_w4_scales_bytes", "difr_w4_quantize", "difr_w4_dequantize", "difr_w4_workspace_bytes",
+           "difr_w4_logits",
            "difr_selftest_wait", "difr_selftest_mx_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
 DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
@@ -148,6 +150,18 @@ def lib() -> ctypes.CDLL:
         L.difr_block_norm.restype = ctypes.c_int
         L.difr_block_norm.argtypes = [v, i64, v, i64, ctypes.POINTER(_CBlock), v, i32, i64, i64, ctypes.c_float,
                                       ctypes.POINTER(_CNormOut), v]
+        L.difr_w4_codes_bytes.restype = ctypes.c_size_t
+        L.difr_w4_codes_bytes.argtypes = [i64, i64]
+        L.difr_w4_scales_bytes.restype = ctypes.c_size_t
+        L.difr_w4_scales_bytes.argtypes = [i64, i64, i32]
+        L.difr_w4_workspace_bytes.restype = ctypes.c_size_t
+        L.difr_w4_workspace_bytes.argtypes = [i64, i64]
+        L.difr_w4_quantize.restype = ctypes.c_int
+        L.difr_w4_quantize.argtypes = [v, i32, i64, i64, i64, i32, v, v, v]
+        L.difr_w4_dequantize.restype = ctypes.c_int
+        L.difr_w4_dequantize.argtypes = [v, v, i32, i64, i64, v, i32, i64, v]
+        L.difr_w4_logits.restype = ctypes.c_int
+        L.difr_w4_logits.argtypes = [v, i64, v, v, i32, i64, i64, i64, v, i32, i64, v, ctypes.c_size_t, v, v]
         L.difr_verify_workspace_bytes.restype = ctypes.c_size_t
         L.difr_verify_workspace_bytes.argtypes = [i64, i64, i64]
         L.difr_verify_drafts.restype = ctypes.c_int
@@ -620,7 +634,7 @@ def difr_selftest_mx_wait(format: int, d: int, logits, done_tiles: int, limit_cy
     return logits
 
 
-# ------------------------------------------------- a decoding step: block norm, verification of drafted tokens
+# ---------------- a decoding step: block norm, 4-bit weights with group scales, verification of drafted tokens
 def difr_block_norm(x, residual, weight, eps, out: NormOut, post_weight=None, post_eps=None, gate=None, scale=1.0,
                     residual_scale=1.0, weight_offset=0.0, stream=None) -> NormOut:
     """Norms before and after a block, with its gate ([T, d], or [1, d] for all tokens) and residual scale: the stream
@@ -647,6 +661,95 @@ def difr_block_norm(x, residual, weight, eps, out: NormOut, post_weight=None, po
     _call("difr_block_norm", device, stream, x.data_ptr(), ldx, residual.data_ptr(), ldr, ctypes.byref(block), weight_p,
           dtype, shape[0], shape[1], eps, ctypes.byref(_norm_out(out, shape, dtype, device)))
     return out
+
+
+def difr_w4_codes_bytes(rows: int, d: int) -> int:
+    return int(lib().difr_w4_codes_bytes(rows, d))
+
+
+def difr_w4_scales_bytes(rows: int, d: int, group: int) -> int:
+    return int(lib().difr_w4_scales_bytes(rows, d, group))
+
+
+def difr_w4_workspace_bytes(T: int, d: int) -> int:
+    return int(lib().difr_w4_workspace_bytes(T, d))
+
+
+@dataclass(slots=True)
+class W4Tensor:
+    """A tensor of `rows` x `d` 4-bit integers with group scales (layout in include/difr.h)."""
+    codes: "object"   # uint8 [rows, 16 ceil(d / 32)]
+    scales: "object"  # bf16 [rows, 8 ceil(groups / 8)]
+    group: int        # 32, 64 or 128
+    rows: int
+    d: int
+
+    @staticmethod
+    def allocate(rows: int, d: int, group: int, device="cuda"):
+        import torch
+
+        if group not in (32, 64, 128) or (rows > 0 and difr_w4_codes_bytes(rows, d) == 0):
+            raise ValueError(f"no 4-bit tensor of {rows} x {d} values in groups of {group}")
+        return W4Tensor(torch.empty(rows, (d + 31) // 32 * 16, dtype=torch.uint8, device=device),
+                        torch.empty(rows, _w4_scale_pitch(d, group), dtype=torch.bfloat16, device=device), group, rows, d)
+
+
+def _w4_scale_pitch(d, group):
+    return ((d + group - 1) // group + 7) // 8 * 8
+
+
+def _check_w4(w, name, device):
+    if not isinstance(w, W4Tensor) or w.group not in (32, 64, 128):
+        raise TypeError(f"{name} must be a W4Tensor in groups of 32, 64 or 128")
+    _check_bytes(w.codes, w.rows * ((w.d + 31) // 32 * 16), name, "codes", device)
+    s, n = w.scales, w.rows * _w4_scale_pitch(w.d, w.group)
+    if not isinstance(s, _torch.Tensor) or s.dtype != _torch.bfloat16 or s.numel() != n or not s.is_contiguous():
+        raise TypeError(f"{name}.scales must be {n} contiguous values of bf16")
+    if s.get_device() != device:
+        raise TypeError(f"{name}.scales is on {s.device}, not on CUDA device {device}")
+
+
+def difr_w4_quantize(x, out: W4Tensor, stream=None) -> W4Tensor:
+    """4-bit codes and group scales of a matrix (bf16, fp16 or fp32); see include/difr.h."""
+    dtype, ld, device = _matrix(x, "x", _ANY_DTYPE)
+    _check_w4(out, "out", device)
+    if (out.rows, out.d) != x.shape:
+        raise TypeError(f"out is {out.rows} x {out.d}, x {tuple(x.shape)}")
+    _call("difr_w4_quantize", device, stream, x.data_ptr(), dtype, out.rows, out.d, ld, out.group, out.codes.data_ptr(),
+          out.scales.data_ptr())
+    return out
+
+
+def difr_w4_dequantize(w: W4Tensor, out, stream=None):
+    """The values of a 4-bit tensor, as fp32 (exact) or bf16 (rounded)."""
+    dtype, ld, device = _matrix(out, "out", _WIDE_DTYPE)
+    _check_w4(w, "w", device)
+    if (w.rows, w.d) != out.shape:
+        raise TypeError(f"out is {tuple(out.shape)}, the tensor {w.rows} x {w.d}")
+    _call("difr_w4_dequantize", device, stream, w.codes.data_ptr(), w.scales.data_ptr(), w.group, w.rows, w.d, out.data_ptr(),
+          dtype, ld)
+    return out
+
+
+def difr_w4_logits(h, W: W4Tensor, logits, workspace, device_status=None, stream=None):
+    """Logits [T, V] (fp32 or bf16) of bf16 hidden states and a head of 4-bit integers with group scales; `workspace` is a
+    uint8 tensor of difr_w4_workspace_bytes(T, d) bytes."""
+    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
+    ldh = _matrix(h, "h", (DIFR_BF16,), None, device)[1]
+    _check_w4(W, "W", device)
+    T, d = h.shape
+    if W.d != d:
+        raise TypeError(f"h has {d} values per row, W {W.d}")
+    if logits.shape != (T, W.rows):
+        raise TypeError(f"logits: expected {(T, W.rows)}, got {tuple(logits.shape)}")
+    _check_status_word(device_status, device)
+    if (not isinstance(workspace, _torch.Tensor) or workspace.dtype != _torch.uint8 or not workspace.is_contiguous()
+            or workspace.get_device() != device):
+        raise TypeError(f"workspace must be contiguous bytes (uint8) on CUDA device {device}")
+    _call("difr_w4_logits", device, stream, h.data_ptr(), ldh, W.codes.data_ptr(), W.scales.data_ptr(), W.group, T, d, W.rows,
+          logits.data_ptr(), dtype, ld, workspace.data_ptr(), workspace.numel(),
+          None if device_status is None else device_status.data_ptr())
+    return logits
 
 
 def difr_verify_workspace_bytes(B: int, n_drafts: int, V: int) -> int:

@@ -1,4 +1,4 @@
-// C ABI of a decoding step's operators: block norm, verification of drafted tokens.  Argument checks and launches; nothing here computes.
+// C ABI of a decoding step's operators: block norm, 4-bit weights with group scales, verification of drafted tokens.  Argument checks and launches; nothing here computes.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -11,6 +11,7 @@
 #include "difr_host.h"
 #include "mx_device.cuh"
 #include "step_kernels.h"
+#include "w4_device.cuh"
 
 namespace {
 
@@ -35,6 +36,29 @@ difr_status device_sms(int* sms) {
   if (n < 0) return DIFR_ERR_ARCH;
   *sms = n;
   return DIFR_OK;
+}
+
+bool known_group(int32_t g) { return g == 32 || g == 64 || g == 128; }
+
+difr_status w4_convert_checks(const void* codes, const void* scales, int32_t group, int64_t rows, int64_t d, const void* plain,
+                              int32_t dtype, int64_t ld) {
+  if (!known_group(group) || !known_dtype(dtype) || rows < 0 || d <= 0 || ld < d) return DIFR_ERR_INVALID_ARG;
+  if (rows > kMaxRows || d > kMaxD || ld > kMaxLd) return DIFR_ERR_SHAPE;
+  if (rows == 0) return DIFR_OK;
+  if (!codes || !scales || !plain) return DIFR_ERR_INVALID_ARG;
+  if (!aligned16(codes) || !aligned16(scales) || !aligned_to(plain, elem_bytes(dtype))) return DIFR_ERR_ALIGN;
+  return DIFR_OK;
+}
+
+W4ConvertParams w4_convert_params(const void* codes, const void* scales, int32_t group, int64_t rows, int64_t d,
+                                  const void* plain, int32_t dtype, int64_t ld) {
+  W4ConvertParams p;
+  memset(&p, 0, sizeof p);
+  p.codes = static_cast<unsigned char*>(const_cast<void*>(codes));
+  p.scales = static_cast<__nv_bfloat16*>(const_cast<void*>(scales));
+  p.rows = rows; p.ld = ld; p.d = (int)d; p.group = group;
+  p.vec = d % 8 == 0 && vector_rows(plain, ld, dtype);
+  return p;
 }
 
 // Records of a row: its vectors, of which the first may begin before the row.
@@ -93,6 +117,72 @@ difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, in
           (!out->residual || vector_rows(out->residual, out->ld_residual, dtype)) &&
           (!out->h || vector_rows(out->h, out->ldh, DIFR_BF16));
   return launch_block_norm(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+}
+
+size_t difr_w4_codes_bytes(int64_t rows, int64_t d) {
+  if (rows < 1 || d < 1 || rows > kMaxRows || d > kMaxD) return 0;
+  return (size_t)rows * (size_t)w4_pitch_bytes(d);
+}
+
+size_t difr_w4_scales_bytes(int64_t rows, int64_t d, int32_t group) {
+  if (rows < 1 || d < 1 || rows > kMaxRows || d > kMaxD || !known_group(group)) return 0;
+  return (size_t)rows * (size_t)w4_scale_pitch(d, group) * 2;
+}
+
+difr_status difr_w4_quantize(const void* x, int32_t dtype, int64_t rows, int64_t d, int64_t ldx, int32_t group, void* codes,
+                             void* scales, difr_stream_t stream) {
+  const difr_status st = w4_convert_checks(codes, scales, group, rows, d, x, dtype, ldx);
+  if (st != DIFR_OK || rows == 0) return st;
+  int sms = 0;
+  const difr_status ds = device_sms(&sms);
+  if (ds != DIFR_OK) return ds;
+  W4ConvertParams p = w4_convert_params(codes, scales, group, rows, d, x, dtype, ldx);
+  p.in = x;
+  return launch_w4_quantize(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+}
+
+difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t group, int64_t rows, int64_t d, void* out,
+                               int32_t dtype, int64_t ldo, difr_stream_t stream) {
+  const difr_status st = w4_convert_checks(codes, scales, group, rows, d, out, dtype, ldo);
+  if (st != DIFR_OK) return st;
+  if (dtype == DIFR_F16) return DIFR_ERR_INVALID_ARG;  // a bf16 scale's range is not fp16's
+  if (rows == 0) return DIFR_OK;
+  int sms = 0;
+  const difr_status ds = device_sms(&sms);
+  if (ds != DIFR_OK) return ds;
+  W4ConvertParams p = w4_convert_params(codes, scales, group, rows, d, out, dtype, ldo);
+  p.out = out;
+  return launch_w4_dequantize(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+}
+
+size_t difr_w4_workspace_bytes(int64_t T, int64_t d) {
+  if (T < 1 || d < 1 || T > kMaxRows || d > kMaxD) return 0;
+  return 16;
+}
+
+difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, const void* W_scales, int32_t group, int64_t T,
+                           int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, void* workspace,
+                           size_t workspace_bytes, int32_t* device_status, difr_stream_t stream) {
+  if (!known_group(group) || (dtype != DIFR_F32 && dtype != DIFR_BF16)) return DIFR_ERR_INVALID_ARG;
+  if (T < 0 || d <= 0 || V <= 0 || ldh < d || ld < V) return DIFR_ERR_INVALID_ARG;
+  if (T > kMaxRows || d > kMaxD || V > kMaxRows || ldh > kMaxLd || ld > kMaxLd) return DIFR_ERR_SHAPE;
+  if (T == 0) return DIFR_OK;
+  if (!h || !W_codes || !W_scales || !logits) return DIFR_ERR_INVALID_ARG;
+  if (!aligned_to(h, 2) || !aligned16(W_codes) || !aligned16(W_scales) || !aligned_to(logits, elem_bytes(dtype)) ||
+      !aligned_to(device_status, 4) || !aligned16(workspace))
+    return DIFR_ERR_ALIGN;
+  if (!workspace || workspace_bytes < difr_w4_workspace_bytes(T, d)) return DIFR_ERR_WORKSPACE;
+  int sms = 0;
+  const difr_status ds = device_sms(&sms);
+  if (ds != DIFR_OK) return ds;
+  W4LogitsParams p;
+  memset(&p, 0, sizeof p);
+  p.h = static_cast<const __nv_bfloat16*>(h);
+  p.codes = static_cast<const unsigned char*>(W_codes);
+  p.scales = static_cast<const __nv_bfloat16*>(W_scales);
+  p.logits = logits; p.ldh = ldh; p.ld = ld; p.device_status = device_status;
+  p.T = (int)T; p.d = (int)d; p.V = (int)V; p.group = group;
+  return launch_w4_logits(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
 }
 
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {

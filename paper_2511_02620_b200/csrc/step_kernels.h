@@ -2,6 +2,7 @@
 // drafted tokens (host-visible part).
 #pragma once
 #include <cuda.h>
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -26,6 +27,29 @@ struct BlockNormParams {
   bool vec;                 // all rows start on 16-byte boundaries and d is a multiple of 8
 };
 cudaError_t launch_block_norm(const BlockNormParams& p, int dtype, cudaStream_t stream);
+
+struct W4ConvertParams {
+  const void* in;         // quantise: [rows][ld]
+  void* out;              // dequantise: [rows][ld]
+  unsigned char* codes;
+  __nv_bfloat16* scales;
+  int64_t rows, ld;
+  int d, group;
+  bool vec;               // the rows of `in` / `out` start on 16-byte boundaries and d is a multiple of 8
+};
+cudaError_t launch_w4_quantize(const W4ConvertParams& p, int dtype, cudaStream_t stream);
+cudaError_t launch_w4_dequantize(const W4ConvertParams& p, int dtype, cudaStream_t stream);
+
+struct W4LogitsParams {
+  const __nv_bfloat16* h;  // [T][ldh]
+  const unsigned char* codes;
+  const __nv_bfloat16* scales;
+  void* logits;            // [T][ld]
+  int64_t ldh, ld;
+  int32_t* device_status;
+  int T, d, V, group;
+};
+cudaError_t launch_w4_logits(const W4LogitsParams& p, int dtype, cudaStream_t stream);
 
 struct VerifyParams {
   const void* logits;            // [n_drafts + B][ld]

@@ -85,3 +85,53 @@ def verify(logits, drafted, offsets, accept_words, sample_words, temperatures, m
         c = torch.cumsum(r, 0)
         tokens[b, m] = int(torch.searchsorted(c, c[-1:] * uniform(sample_words[b]), right=True).clamp(max=int(r.nonzero()[-1])))
     return tokens, n_accepted, p_draft, status
+
+
+# ------------------------------------------------------------------ 4-bit weights with group scales
+def w4_groups(d, group):
+    return (d + group - 1) // group
+
+
+def bf16_nearest(v):
+    """Nearest bf16 to positive 64-bit values, ties to even, by comparison (no rounding instruction): normal numbers only."""
+    m, e = torch.frexp(v)                      # v = m 2^e, 1/2 <= m < 1
+    scaled = m * 256                           # eight bits
+    low = torch.floor(scaled)
+    over = scaled - low
+    up = (over > 0.5) | ((over == 0.5) & (low % 2 == 1))
+    return torch.ldexp(low + up.double(), e - 8)
+
+
+def w4_quantize(x, group):
+    """(codes [rows, groups * group], scales [rows, groups], both 64-bit) of rows of values."""
+    rows, d = x.shape
+    b = torch.nn.functional.pad(x.double(), (0, -d % group)).view(rows, -1, group)
+    top = b.abs().amax(-1)
+    bad = ~torch.isfinite(b).all(-1)
+    seventh = torch.where(bad | (top == 0), 1.0, top) / 7  # (64 bits: 29 more than the values' own)
+    s = torch.where((top == 0) | (bf16_nearest(seventh) < 2.0 ** -126), 0.0, bf16_nearest(seventh))
+    ok = ~bad & (s > 0)
+    q = torch.where(ok.unsqueeze(-1), b, 0.0) / torch.where(ok, s, 1.0).unsqueeze(-1)
+    low = torch.floor(q)
+    # the border above `low`, compared by products that 64 bits hold exactly
+    over = torch.where(ok.unsqueeze(-1), b, 0.0) - (low + 0.5) * torch.where(ok, s, 1.0).unsqueeze(-1)
+    code = low + ((over > 0) | ((over == 0) & (low % 2 != 0))).double()
+    return torch.where(ok.unsqueeze(-1), code, 0.0).flatten(1), torch.where(bad, float("nan"), s)
+
+
+def w4_pack(codes, scales, d, group):
+    """Stored form of codes [rows, >= d] and scales [rows, groups]: uint8 and bf16, padded with zeros."""
+    rows, groups = codes.shape[0], w4_groups(d, group)
+    c = torch.zeros(rows, (d + 31) // 32 * 32, dtype=torch.int64)
+    c[:, :d] = codes[:, :d].long() & 15
+    s = torch.zeros(rows, (groups + 7) // 8 * 8, dtype=torch.bfloat16)
+    s[:, :groups] = scales.to(torch.bfloat16)
+    return (c[:, 0::2] | (c[:, 1::2] << 4)).to(torch.uint8), s
+
+
+def w4_values(codes, scales, d, group):
+    """64-bit values [rows, d] of codes and scales as they are stored."""
+    c = codes.long()
+    c = torch.stack((c & 15, c >> 4), -1).flatten(1)[:, :d]
+    c = torch.where(c >= 8, c - 16, c).double()
+    return c * scales.double()[:, :w4_groups(d, group)].repeat_interleave(group, 1)[:, :d]

@@ -455,3 +455,312 @@ def test_verification_refusals():
     e = lambda *shape: torch.empty(*shape, dtype=torch.int32, device="cuda")
     difr.difr_verify_drafts(torch.empty(0, 50, device="cuda"), e(0), torch.zeros(1, dtype=torch.int32, device="cuda"), e(0), e(0), 1.0,
                             difr.DraftOut(e(0, 3), e(0), None, None, torch.empty(0, dtype=torch.uint8, device="cuda")))
+
+
+# ------------------------------------------------------------------ 4-bit weights with group scales
+def w4_of(rows, d, group):
+    """A tensor whose buffers are full of a value that nothing writes."""
+    w = difr.W4Tensor.allocate(rows, d, group)
+    w.codes.fill_(0x5A)
+    w.scales.fill_(math.nan)
+    return w
+
+
+def assert_w4_equal(w, x, group):
+    codes, scales = ref.w4_pack(*ref.w4_quantize(x, group), x.shape[1], group)
+    assert torch.equal(w.codes.cpu(), codes)
+    assert torch.equal(torch.isnan(w.scales.cpu()), torch.isnan(scales))
+    assert torch.equal(w.scales.cpu().nan_to_num(), scales.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,d", [(1, 1), (1, 32), (3, 31), (5, 33), (2, 100), (129, 128), (130, 1056), (257, 1749), (9, 70),
+                                    (20, 1030), (7, 4096), (1, 8192)])
+def test_w4_quantisation_is_bit_exact(rows, d, group, dtype):
+    x = randn(rows, d, seed=rows + d).to(DTYPES[dtype])
+    w = w4_of(rows, d, group)
+    difr.difr_w4_quantize(x.cuda(), w)
+    assert_w4_equal(w, x, group)
+
+
+@pytest.mark.parametrize("group", [32, 128])
+def test_w4_every_rounding_border(group):
+    """All codes, all midpoints and their fp32 neighbours under scales that are no powers of two; largest magnitudes whose
+    seventh is a bf16 midpoint, and their neighbours."""
+    rows = []
+    for mant in (128, 129, 173, 200, 255):
+        for e in (-126, -60, -9, 0, 40, 110):
+            s = math.ldexp(mant, e - 7)
+            if s < 2.0 ** -126 or 7 * s > 3e38:
+                continue
+            pts = torch.tensor([s * k / 2 for k in range(-14, 15)], dtype=torch.float64).float()
+            pts = torch.cat([pts, torch.nextafter(pts, torch.tensor(math.inf)), torch.nextafter(pts, torch.tensor(-math.inf))])
+            pts = pts[pts.abs() <= 7 * s]
+            for i in range(0, pts.numel(), group - 1):
+                row = torch.zeros(group)
+                row[:pts[i:i + group - 1].numel()] = pts[i:i + group - 1]
+                row[-1] = 7 * s
+                rows.append(row)
+    for m in range(257, 512, 14):  # 7 * odd nine-bit numbers: a seventh lies between two bf16
+        top = torch.tensor(7.0 * m)
+        for v in (top, torch.nextafter(top, torch.tensor(math.inf)), torch.nextafter(top, torch.tensor(0.0))):
+            row = v * torch.linspace(-1, 1, group)
+            row[0] = v
+            rows.append(row)
+    x = torch.stack(rows)
+    w = w4_of(x.shape[0], group, group)
+    difr.difr_w4_quantize(x.cuda(), w)
+    assert_w4_equal(w, x, group)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_w4_extreme_groups(group):
+    x = randn(12, 3 * group - 5, seed=5)
+    x[0] = 0.0
+    x[1] = -0.0
+    x[2] = torch.finfo(torch.float32).max
+    x[3, :group] = 1e-45
+    x[3, group:2 * group] = -3e-39
+    x[4] = x[4] * 1e-42
+    x[5, group + 3] = math.nan
+    x[6, 0] = math.inf
+    x[7, 3 * group - 6] = -math.inf
+    x[8] = -torch.finfo(torch.float32).max
+    x[9] = 7 * torch.finfo(torch.float32).tiny
+    x[10] = 6.9 * torch.finfo(torch.float32).tiny
+    x[11, group:] = 0.0
+    w = w4_of(12, x.shape[1], group)
+    difr.difr_w4_quantize(x.cuda(), w)
+    assert_w4_equal(w, x, group)
+    out = torch.empty_like(x, device="cuda")
+    difr.difr_w4_dequantize(w, out)
+    want = ref.w4_values(w.codes.cpu(), w.scales.cpu(), x.shape[1], group)
+    assert torch.equal(torch.isnan(out.cpu()), torch.isnan(want))
+    assert torch.equal(out.cpu().double().nan_to_num(), want.nan_to_num())
+
+
+def random_w4(rows, d, group, seed=0, std=None):
+    """Codes over the whole range, -8 among them, scales of either sign over a few powers of two, eight bits each."""
+    g = torch.Generator().manual_seed(seed)
+    codes = torch.randint(-8, 8, (rows, d), generator=g)
+    scales = torch.randint(128, 256, (rows, ref.w4_groups(d, group)), generator=g).double()
+    scales *= 2.0 ** torch.randint(-10, -6, scales.shape, generator=g) * (std or d ** -0.5) / 8
+    scales = scales.to(torch.bfloat16) * (1 - 2 * torch.randint(0, 2, scales.shape, generator=g))
+    c, s = ref.w4_pack(codes, scales, d, group)
+    return difr.W4Tensor(c.cuda(), s.cuda(), group, rows, d), ref.w4_values(c, s, d, group)
+
+
+@pytest.mark.parametrize("out_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("rows,d,ld", [(1, 1, 1), (3, 31, 40), (129, 256, 256), (70, 1749, 1749), (5, 4096, 4104), (9, 70, 70), (20, 1030, 1034)])
+def test_w4_dequantisation(rows, d, ld, group, out_dtype):
+    w, values = random_w4(rows, d, group, seed=d)
+    buf = torch.full((rows, ld), -7.0, dtype=DTYPES[out_dtype], device="cuda")
+    difr.difr_w4_dequantize(w, buf[:, :d])
+    assert torch.equal(buf[:, :d].cpu(), values.to(DTYPES[out_dtype]))
+    assert torch.all(buf[:, d:] == -7.0)
+
+
+@pytest.mark.parametrize("offset,ld", [(0, 72), (1, 72), (0, 67), (8, 80)])
+def test_w4_quantisation_of_strided_rows(offset, ld):
+    buf = randn(40, ld + 8, seed=ld).to(torch.bfloat16)
+    w = w4_of(40, 65, 64)
+    difr.difr_w4_quantize(buf.cuda()[:, offset:offset + 65], w)
+    assert_w4_equal(w, buf[:, offset:offset + 65], 64)
+
+
+def w4_logits(h, W, dtype=torch.float32, ld=None, offset=0, status=True):
+    T, V = h.shape[0], W.rows
+    ld = ld or V
+    buf = torch.full((T * ld + offset,), -7.0, dtype=dtype, device="cuda")
+    logits = torch.as_strided(buf, (T, V), (ld, 1), offset)
+    word = torch.zeros(1, dtype=torch.int32, device="cuda") if status else None
+    ws = torch.full((difr.difr_w4_workspace_bytes(T, W.d),), 0xAB, dtype=torch.uint8, device="cuda")
+    difr.difr_w4_logits(h.cuda() if not h.is_cuda else h, W, logits, ws, word)
+    assert not status or int(word) == 0
+    if ld > V:
+        assert torch.all(torch.as_strided(buf, (T - 1, ld - V), (ld, 1), offset + V) == -7.0)
+    return logits
+
+
+def check_w4_logits(got, h, values):
+    """The sum of ceil(d / 16) steps, each of which may drop what lies below the last bit of the largest number in it, and
+    two roundings more: (steps + 2) 2^-23 of the sizes added up; bf16 rounds once more."""
+    h, values = h.double().cpu(), values
+    want, size = h @ values.T, h.abs() @ values.abs().T
+    fp32 = ((h.shape[1] + 15) // 16 + 2) * 2.0 ** -23 * size
+    half = 2.0 ** -8 if got.dtype == torch.bfloat16 else 0.0
+    err = (got.double().cpu() - want).abs()
+    assert torch.all(err <= fp32 + half * (want.abs() + fp32) + 2.0 ** -134)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T,V,d", [(1, 1, 1), (1, 128, 32), (1, 1000, 4096), (2, 129, 31), (3, 257, 33), (5, 300, 100), (16, 1000, 1749),
+                                   (17, 1003, 2048), (33, 777, 130), (64, 2000, 1024), (65, 640, 70), (129, 1001, 513), (300, 515, 1030),
+                                   (777, 400, 256), (1, 20000, 8191)])
+def test_w4_logits(T, V, d, group, out):
+    W, values = random_w4(V, d, group, seed=T + V + d)
+    h = randn(T, d, seed=d).to(torch.bfloat16)
+    check_w4_logits(w4_logits(h, W, DTYPES[out]), h, values)
+
+
+@pytest.mark.parametrize("out,ld,offset", [("f32", 1008, 0), ("f32", 1001, 1), ("bf16", 1001, 0), ("bf16", 1002, 1), ("bf16", 1008, 3)])
+@pytest.mark.parametrize("T", [1, 9, 130])
+def test_w4_logits_of_strided_rows(T, out, ld, offset):
+    d = 333
+    W, values = random_w4(1001, d, 64, seed=1)
+    h = randn(T, d + 11, seed=2).to(torch.bfloat16).cuda()[:, 3:3 + d]
+    check_w4_logits(w4_logits(h, W, DTYPES[out], ld, offset), h, values)
+
+
+def test_w4_logits_of_small_integers_are_exact():
+    """Sums that fp32 holds: every product and every partial sum is an integer below 2^24."""
+    g = torch.Generator().manual_seed(3)
+    for T, V, d in ((1, 500, 4096), (40, 500, 2048), (200, 300, 999)):
+        codes = torch.randint(-8, 8, (V, d), generator=g)
+        scales = torch.tensor([1.0, 2.0, 3.0, 7.0])[torch.randint(0, 4, (V, ref.w4_groups(d, 32)), generator=g)]
+        c, s = ref.w4_pack(codes, scales, d, 32)
+        h = torch.randint(-16, 17, (T, d), generator=g).to(torch.bfloat16)
+        want = h.double() @ ref.w4_values(c, s, d, 32).T
+        assert torch.equal(w4_logits(h, difr.W4Tensor(c.cuda(), s.cuda(), 32, V, d)).double().cpu(), want)
+
+
+def test_w4_logits_where_sizes_differ_by_a_lot():
+    """Hidden states with outliers of 2^20, rows of weights whose scales are 2^-100 to 2^80 times the others', groups of one row
+    that are up to 2^11 apart, ids of zero scales."""
+    T, V, d = 20, 600, 640
+    W, _ = random_w4(V, d, 64, seed=4)
+    s = W.scales.cpu().float()
+    s *= 2.0 ** torch.randint(-100, 81, (V, 1), generator=torch.Generator().manual_seed(5)).float()
+    s[:, 3] *= 2.0 ** 11
+    s[::7] = 0.0
+    W.scales.copy_(s.to(torch.bfloat16))
+    values = ref.w4_values(W.codes.cpu(), W.scales.cpu(), d, 64)
+    h = randn(T, d, seed=6)
+    h[::2, 5] *= 2.0 ** 20
+    h[1] *= 2.0 ** -90
+    h[3] = 0.0
+    h[4] *= 2.0 ** 30
+    h = h.to(torch.bfloat16)
+    for t in (slice(0, T), slice(3, 4), slice(0, 1)):
+        check_w4_logits(w4_logits(h[t], W), h[t], values)
+
+
+def test_w4_logits_of_broken_rows_and_groups():
+    """A NaN or an infinity in a row of h spoils that row, a NaN or infinite scale that id; nothing else."""
+    T, V, d = 30, 400, 300
+    W, _ = random_w4(V, d, 32, seed=7)
+    W.scales[5, 2] = math.nan
+    W.scales[399, 9] = math.inf
+    W.scales[128, 0] = -math.inf
+    h = randn(T, d, seed=8).to(torch.bfloat16)
+    h[3, 7], h[11, 299], h[29, 0] = math.nan, math.inf, -math.inf
+    got = w4_logits(h, W).cpu()
+    bad = torch.zeros(T, V, dtype=torch.bool)
+    bad[[3, 11, 29]] = True
+    bad[:, [5, 399, 128]] = True
+    assert torch.equal(torch.isnan(got), bad)
+    values = ref.w4_values(W.codes.cpu(), W.scales.cpu(), d, 32)
+    rows, ids = ~bad.all(1), ~bad.all(0)
+    check_w4_logits(got[rows][:, ids], h[rows], values[ids])
+
+
+@pytest.mark.parametrize("T", [1, 4, 60, 300])
+def test_w4_logits_do_not_notice_their_batch(T):
+    """A row alone, in the batch, and at another place of it: the same bits."""
+    W, _ = random_w4(1111, 1024, 128, seed=9)
+    h = randn(T, 1024, seed=10).to(torch.bfloat16)
+    whole = w4_logits(h, W)
+    for t in {0, T // 2, T - 1}:
+        assert torch.equal(w4_logits(h[t:t + 1], W)[0], whole[t])
+    assert torch.equal(w4_logits(h.flip(0), W).flip(0), whole)
+
+
+def test_w4_logits_captured_and_on_another_stream():
+    W, values = random_w4(3000, 512, 64, seed=11)
+    for T in (1, 70):
+        h = randn(T, 512, seed=12).to(torch.bfloat16).cuda()
+        want = w4_logits(h, W)
+        logits, ws = torch.empty_like(want), torch.empty(difr.difr_w4_workspace_bytes(T, 512), dtype=torch.uint8, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            difr.difr_w4_logits(h, W, logits, ws)
+        for seed in (13, 14):
+            h.copy_(randn(T, 512, seed=seed).to(torch.bfloat16))
+            graph.replay()
+            check_w4_logits(logits, h, values)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        other = torch.empty_like(logits)
+        difr.difr_w4_logits(h, W, other, torch.empty_like(ws), stream=side)
+        side.synchronize()
+        assert torch.equal(other, logits)
+
+
+def test_w4_logits_of_a_head_beyond_32_bits_of_bytes():
+    """Codes of more than 2^32 bytes, logits of more than 2^31 elements: ids at both ends."""
+    V, d = 600_000, 16384  # 4.9e9 bytes of codes
+    w = difr.W4Tensor(torch.randint(0, 256, (V, d // 2), dtype=torch.uint8, device="cuda"),
+                      torch.rand(V, d // 128, device="cuda").to(torch.bfloat16), 128, V, d)
+    h = randn(3600, d, seed=15).to(torch.bfloat16)
+    h_all = h.cuda()
+    logits = torch.empty(3600, V, dtype=torch.bfloat16, device="cuda")
+    difr.difr_w4_logits(h_all, w, logits, torch.empty(difr.difr_w4_workspace_bytes(3600, d), dtype=torch.uint8, device="cuda"))
+    for ids in (slice(0, 40), slice(V - 40, V)):
+        values = ref.w4_values(w.codes[ids].cpu(), w.scales[ids].cpu(), d, 128)
+        for rows in (slice(0, 3), slice(3597, 3600)):
+            check_w4_logits(logits[rows, ids], h[rows], values)
+
+
+def test_w4_refusals():
+    W, _ = random_w4(40, 64, 32, seed=16)
+    h = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    logits, ws = torch.empty(4, 40, device="cuda"), torch.empty(difr.difr_w4_workspace_bytes(4, 64), dtype=torch.uint8, device="cuda")
+    difr.difr_w4_logits(h, W, logits, ws)
+    for bad in ((h.half(), W, logits, ws), (h[:, :32], W, logits, ws), (h, W, logits[:, :39], ws), (h, W, logits.half(), ws),
+                (h, W, logits, ws.float()), (h, W, logits, ws.cpu()), (h.T, W, logits, ws), (h, "W", logits, ws),
+                (h, difr.W4Tensor(W.codes, W.scales, 48, 40, 64), logits, ws), (h, difr.W4Tensor(W.codes[:39], W.scales, 32, 40, 64), logits, ws)):
+        with pytest.raises(TypeError):
+            difr.difr_w4_logits(*bad)
+    for status, args in ((-4, (h, W, logits, ws[:ws.numel() - 1])), (-3, (h, W, logits, torch.empty(ws.numel() + 8, dtype=torch.uint8, device="cuda")[8:])),
+                         (-3, (h, difr.W4Tensor(torch.empty(40 * 32 + 8, dtype=torch.uint8, device="cuda")[8:], W.scales, 32, 40, 64), logits, ws))):
+        with pytest.raises(difr.DifrError) as e:
+            difr.difr_w4_logits(*args)
+        assert e.value.status == status
+    with pytest.raises(ValueError):
+        difr.W4Tensor.allocate(4, 64, 48)
+    with pytest.raises(TypeError):
+        difr.difr_w4_dequantize(W, torch.empty(40, 64, dtype=torch.float16, device="cuda"))
+    with pytest.raises(TypeError):
+        difr.difr_w4_quantize(torch.zeros(39, 64, device="cuda"), W)
+    difr.difr_w4_logits(h[:0], W, logits[:0], ws)
+    difr.difr_w4_quantize(torch.empty(0, 64, device="cuda"), difr.W4Tensor.allocate(0, 64, 32))
+
+
+# ------------------------------------------------------------------ together
+def test_a_decoding_step_from_block_to_tokens():
+    """The last block's output through norms and 4-bit head into the verification of drafts sampled near its logits: each step
+    against its own statement on the step before it."""
+    B, K, d, V = 9, 4, 512, 3000
+    T = B * (K + 1)
+    x, r, w, pw, g = block_inputs(T, d, "bf16", "token")
+    out = run_block(x, r, w, 1e-6, pw, None, g, scale=0.5)
+    check_stream(out.residual, x, r, "bf16", pw, 1e-6, g, scale=0.5)
+    check_h(out.h, out.residual, w, 1e-6)
+    W = w4_of(V, d, 64)
+    head = randn(V, d, seed=20, std=2.5 * d ** -0.5)
+    difr.difr_w4_quantize(head.cuda(), W)
+    assert_w4_equal(W, head, 64)
+    logits = w4_logits(out.h, W)
+    check_w4_logits(logits, out.h.cpu(), ref.w4_values(W.codes.cpu(), W.scales.cpu(), d, 64))
+    s = make_drafts(B, K, V, "f32", True, 0.8, seed=21, ragged=False)
+    s["logits"] = logits.cpu()
+    gen = torch.Generator().manual_seed(22)
+    for b in range(B):
+        for j in range(K):
+            q = torch.softmax((s["logits"][b * (K + 1) + j] + 0.3 * torch.randn(V, generator=gen)) / 0.8, 0)
+            s["probs"][b * K + j] = q
+            s["drafted"][b * K + j] = int(torch.multinomial(q, 1, generator=gen))
+    check_verify(s)

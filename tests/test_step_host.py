@@ -111,3 +111,49 @@ def test_refusals_of_the_verification():
     assert verify(V=(1 << 28) + 1, ld=1 << 29, ld_draft=1 << 29) == SHAPE and verify(B=1 << 28) == SHAPE
     assert verify(workspace=None) == WORKSPACE and verify(workspace_bytes=difr.difr_verify_workspace_bytes(3, 6, 100) - 1) == WORKSPACE
     assert verify(B=0, logits=None, offsets=None) == OK
+
+
+def test_sizes_of_4_bit_tensors():
+    assert difr.difr_w4_codes_bytes(3, 33) == 3 * 32 and difr.difr_w4_codes_bytes(128256, 4096) == 128256 * 2048
+    assert difr.difr_w4_scales_bytes(3, 33, 32) == 3 * 16 and difr.difr_w4_scales_bytes(2, 1025, 128) == 2 * 32
+    for rows, d in ((0, 1), (1, 0), (-1, 5), ((1 << 30) + 1, 1), (1, (1 << 20) + 1)):
+        assert difr.difr_w4_codes_bytes(rows, d) == 0 and difr.difr_w4_scales_bytes(rows, d, 32) == 0
+        assert difr.difr_w4_workspace_bytes(rows, d) == 0
+    assert difr.difr_w4_scales_bytes(4, 64, 48) == 0
+    w = difr.W4Tensor.allocate(5, 300, 64, device="cpu")
+    assert w.codes.numel() == difr.difr_w4_codes_bytes(5, 300) and 2 * w.scales.numel() == difr.difr_w4_scales_bytes(5, 300, 64)
+
+
+@host_only
+def test_refusals_of_4_bit_tensors():
+    L = difr.lib()
+
+    def q(x=P, dtype=0, rows=8, d=64, ld=64, group=32, codes=P, scales=P):
+        return L.difr_w4_quantize(x, dtype, rows, d, ld, group, codes, scales, None)
+
+    assert q(x=None) == INVALID and q(codes=None) == INVALID and q(scales=None) == INVALID
+    assert q(dtype=3) == INVALID and q(group=16) == INVALID and q(group=0) == INVALID and q(group=96) == INVALID
+    assert q(rows=-1) == INVALID and q(d=0) == INVALID and q(ld=63) == INVALID
+    assert q(rows=(1 << 30) + 1) == SHAPE and q(d=(1 << 20) + 1, ld=1 << 21) == SHAPE
+    assert q(codes=ODD) == ALIGN and q(scales=ODD) == ALIGN and q(x=P + 1) == ALIGN and q(x=P + 2, dtype=2) == ALIGN
+    assert q(rows=0, x=None, codes=None, scales=None) == OK and q() == CUDA
+
+    def dq(codes=P, scales=P, group=64, rows=8, d=64, out=P, dtype=0, ld=64):
+        return L.difr_w4_dequantize(codes, scales, group, rows, d, out, dtype, ld, None)
+
+    assert dq(out=None) == INVALID and dq(codes=None) == INVALID and dq(group=5) == INVALID and dq(ld=10) == INVALID
+    assert dq(dtype=1) == INVALID and dq(rows=0, out=None) == OK and dq() == CUDA
+
+    def logits(h=P, ldh=64, wc=P, ws=P, group=32, T=8, d=64, V=100, out=P, dtype=2, ld=100, work=P, nbytes=1 << 20, status=None):
+        return L.difr_w4_logits(h, ldh, wc, ws, group, T, d, V, out, dtype, ld, work, nbytes, status, None)
+
+    for name in ("h", "wc", "ws", "out"):
+        assert logits(**{name: None}) == INVALID
+    for name in ("wc", "ws", "work"):
+        assert logits(**{name: ODD}) == ALIGN
+    assert logits(h=P + 1) == ALIGN and logits(out=P + 2) == ALIGN and logits(out=P + 1, dtype=0) == ALIGN and logits(status=P + 2) == ALIGN
+    assert logits(group=48) == INVALID and logits(dtype=1) == INVALID and logits(ld=99) == INVALID and logits(ldh=63) == INVALID
+    assert logits(T=-1) == INVALID and logits(V=0) == INVALID and logits(d=0) == INVALID
+    assert logits(T=(1 << 30) + 1) == SHAPE and logits(V=(1 << 30) + 1, ld=1 << 31) == SHAPE
+    assert logits(work=None) == WORKSPACE and logits(nbytes=difr.difr_w4_workspace_bytes(8, 64) - 1) == WORKSPACE
+    assert logits(T=0, h=None, wc=None) == OK and logits() == CUDA
