@@ -6,51 +6,15 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "../../include/difr.h"
 #include "difr_host.h"
+#include "logit_plan.h"
 #include "mx_device.cuh"
 #include "mx_kernels.h"
 
 namespace {
 
 using namespace difr;
-
-// Streaming multiprocessors and resident CTA pairs of the current device; DIFR_ERR_ARCH for another architecture.
-difr_status device_pairs(int* pairs) {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int> cached[kMaxDevices];  // 0: not asked yet, -1: another architecture, otherwise pairs
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return DIFR_ERR_CUDA;
-  const bool slot = dev >= 0 && dev < kMaxDevices;
-  int n = slot ? cached[dev].load(std::memory_order_relaxed) : 0;
-  if (n == 0) {
-    int major = 0, sms = 0;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-      return DIFR_ERR_CUDA;
-    n = -1;
-    if (major == 10) {
-      n = mx_logits_max_resident_pairs();
-      if (n <= 0) return DIFR_ERR_CUDA;
-      if (n > sms / 2) n = sms / 2;
-    }
-    if (slot) cached[dev].store(n, std::memory_order_relaxed);
-  }
-  if (n < 0) return DIFR_ERR_ARCH;
-  *pairs = n;
-  return DIFR_OK;
-}
-
-int common_divisor(int a, int b) {
-  while (b != 0) {
-    const int r = a % b;
-    a = b;
-    b = r;
-  }
-  return a;
-}
 
 // Codes of a microscaled tensor as bytes: box of 128 bytes (128-byte swizzle) x box_rows rows.
 bool codes_tmap(CUtensorMap* map, const void* base, int fmt, int64_t rows, int64_t d, int box_rows) {
@@ -80,19 +44,6 @@ bool scales_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t d, in
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The logits [T, V] as the epilogue stores them: pieces of 128 ids x some tokens.
-bool logits_tmap(CUtensorMap* map, void* base, int32_t dtype, int64_t T, int64_t V, int64_t ld) {
-  EncodeTiledFn fn = encode_tiled_fn();
-  if (fn == nullptr) return false;
-  const cuuint64_t dims[2] = {(cuuint64_t)V, (cuuint64_t)T};
-  const cuuint64_t strides[1] = {(cuuint64_t)(ld * elem_bytes(dtype))};
-  const cuuint32_t box[2] = {128, (cuuint32_t)mx_out_tokens(elem_bytes(dtype))};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(map, dtype == DIFR_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims,
-            strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-            CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 bool mx_supported(int64_t rows, int64_t d) { return rows <= kMaxRows && d <= kMaxD; }
 
 // (empty batches carry no buffers: the pointers are looked at only where there are rows)
@@ -116,49 +67,20 @@ difr_status product_checks(int32_t format, int64_t T, int64_t d, int64_t V, int3
 // How a product of T >= 1 tokens is cut into tiles: the kernel's parameters, tokens per tile, grid.
 difr_status mx_plan(int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
                     int32_t* device_status, MxLogitsParams* out, int* tokens_per_tile, int* grid) {
-  // tokens per tile: the smallest width that holds all tokens, tiles of 256 beyond 128
-  int bn = 16;
-  while (bn < 256 && bn < T) bn *= 2;
-  const int64_t n_vt = (V + kMxPairM - 1) / kMxPairM;
-  if (n_vt * ((T + bn - 1) / bn) > (int64_t)1 << 29) return DIFR_ERR_SHAPE;  // tile numbers are 32-bit
+  if (too_many_tiles(T, V, 16)) return DIFR_ERR_SHAPE;
   int pairs = 0;
   const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
-  // Where tiles of 256 leave half of the pairs idle, tiles of 128: twice as many, each about half as long (1024 x 1000 x
-  // 8192 in 8 bits, 16 tiles: 20 us instead of 26; 600 x 3000 x 6000, 36 tiles: 17.3 instead of 22).  Otherwise W would
-  // only be loaded twice as often (777 x 32000 x 1749: 60 us instead of 52).
-  if (bn == 256 && n_vt * ((T + 255) / 256) <= pairs / 2) bn = 128;
-  const int64_t n_tt = (T + bn - 1) / bn;
   MxLogitsParams p;
   memset(&p, 0, sizeof p);
   const int64_t pitch = mx_pitch_bytes(format, d);
-  p.logits = logits; p.ld = ld; p.device_status = device_status;
-  p.T = (int)T; p.V = (int)V;
-  p.k_steps = (int)((pitch + 127) / 128);
-  p.last_mmas = (int)((pitch - (int64_t)(p.k_steps - 1) * 128 + 31) / 32);
-  p.n_vt = (int)n_vt; p.n_tt = (int)n_tt;
-  p.n_tiles = (int)(n_vt * n_tt);
-  // the last token tile is only as wide as its tokens (in steps of 16, what the MMA takes)
-  p.last_tokens = (int)((T - (n_tt - 1) * bn + 15) / 16 * 16);
-  // tokens of a raster group: about 32 MB of codes, a quarter of L2, so that they stay there while W passes
-  const int64_t per_tile = (int64_t)bn * pitch;
-  int64_t group = ((int64_t)32 << 20) / per_tile;
-  if (group < 1) group = 1;
-  if (group > n_tt) group = n_tt;
-  p.group = (int)group;
   // W is read once where there is one token tile; one that L2 cannot keep for the next call either (96 of its 126 MB) goes
   // by it.  Codes of d = 2048 in 8 bits, read again in every call, 48 tokens: 260 MB 51.9 us by it, 53.4 otherwise; 112 MB
   // 27.2 and 27.9; 80 MB 16.6 and 17.3, but there it also puts out what other kernels keep in L2.  One token: 0 to 4 %.
-  p.w_once = n_tt == 1 && V * pitch > ((int64_t)96 << 20);
-  p.pack_pairs = dtype == DIFR_BF16 && ld % 2 == 0 && aligned_to(logits, 4);
-  p.tile_stores = bn == 256 && vector_rows(logits, ld, dtype) && ld <= ((int64_t)1 << 36);
-  const int n_pairs = p.n_tiles < pairs ? p.n_tiles : pairs;
-  // a pair's token tiles follow each other in steps of n_pairs - shift: prime to their number, all come in turn
-  if (n_pairs > 1)
-    while (p.shift < n_pairs - 1 && common_divisor(n_pairs - p.shift, p.group) != 1) ++p.shift;
+  plan_logit_tiles(T, V, pitch, V * pitch, 16, logits, dtype, ld, device_status, pairs, &p, tokens_per_tile, grid);
+  p.k_steps = (int)((pitch + 127) / 128);
+  p.last_mmas = (int)((pitch - (int64_t)(p.k_steps - 1) * 128 + 31) / 32);
   *out = p;
-  *tokens_per_tile = bn;
-  *grid = 2 * n_pairs;
   return DIFR_OK;
 }
 

@@ -5,10 +5,9 @@
 #include <stdint.h>
 #include <string.h>
 
-#include <atomic>
-
 #include "../../include/difr.h"
 #include "difr_host.h"
+#include "logit_plan.h"
 #include "mx_device.cuh"
 #include "step_kernels.h"
 #include "w4_device.cuh"
@@ -16,27 +15,6 @@
 namespace {
 
 using namespace difr;
-
-// Streaming multiprocessors of the current device; DIFR_ERR_ARCH for another architecture.
-difr_status device_sms(int* sms) {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int> cached[kMaxDevices];  // 0: not asked yet, -1: another architecture
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return DIFR_ERR_CUDA;
-  const bool slot = dev >= 0 && dev < kMaxDevices;
-  int n = slot ? cached[dev].load(std::memory_order_relaxed) : 0;
-  if (n == 0) {
-    int major = 0;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-      return DIFR_ERR_CUDA;
-    if (major != 10) n = -1;
-    if (slot) cached[dev].store(n, std::memory_order_relaxed);
-  }
-  if (n < 0) return DIFR_ERR_ARCH;
-  *sms = n;
-  return DIFR_OK;
-}
 
 bool known_group(int32_t g) { return g == 32 || g == 64 || g == 128; }
 
@@ -59,6 +37,22 @@ W4ConvertParams w4_convert_params(const void* codes, const void* scales, int32_t
   p.rows = rows; p.ld = ld; p.d = (int)d; p.group = group;
   p.vec = d % 8 == 0 && vector_rows(plain, ld, dtype);
   return p;
+}
+
+// Workspace of the product: exponents of the tokens, then h as fp16 in rows of whole 64 values.
+int64_t w4_h16_pitch(int64_t d) { return (d + 63) / 64 * 64; }
+int64_t w4_exponent_bytes(int64_t T) { return (T * 4 + 255) / 256 * 256; }
+
+// Tensor map of rows of bytes (codes) or fp16 (h): boxes of 128 bytes (128-byte swizzle) x box_rows rows.
+bool rows_tmap(CUtensorMap* map, const void* base, CUtensorMapDataType type, int elem, int64_t rows, int64_t cols, int box_rows) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(cols * elem)};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, type, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Records of a row: its vectors, of which the first may begin before the row.
@@ -100,8 +94,8 @@ difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, in
       !aligned_to(block->gate, eb) || (out->residual && !aligned_to(out->residual, eb)) || (out->h && !aligned_to(out->h, 2)))
     return DIFR_ERR_ALIGN;
   if (out->mx_format != 0 && (!aligned16(out->codes) || !aligned16(out->scales))) return DIFR_ERR_ALIGN;
-  int sms = 0;
-  const difr_status ds = device_sms(&sms);
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
   BlockNormParams p;
   memset(&p, 0, sizeof p);
@@ -133,8 +127,8 @@ difr_status difr_w4_quantize(const void* x, int32_t dtype, int64_t rows, int64_t
                              void* scales, difr_stream_t stream) {
   const difr_status st = w4_convert_checks(codes, scales, group, rows, d, x, dtype, ldx);
   if (st != DIFR_OK || rows == 0) return st;
-  int sms = 0;
-  const difr_status ds = device_sms(&sms);
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
   W4ConvertParams p = w4_convert_params(codes, scales, group, rows, d, x, dtype, ldx);
   p.in = x;
@@ -147,8 +141,8 @@ difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t gr
   if (st != DIFR_OK) return st;
   if (dtype == DIFR_F16) return DIFR_ERR_INVALID_ARG;  // a bf16 scale's range is not fp16's
   if (rows == 0) return DIFR_OK;
-  int sms = 0;
-  const difr_status ds = device_sms(&sms);
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
   W4ConvertParams p = w4_convert_params(codes, scales, group, rows, d, out, dtype, ldo);
   p.out = out;
@@ -157,7 +151,7 @@ difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t gr
 
 size_t difr_w4_workspace_bytes(int64_t T, int64_t d) {
   if (T < 1 || d < 1 || T > kMaxRows || d > kMaxD) return 0;
-  return 16;
+  return (size_t)(w4_exponent_bytes(T) + T * w4_h16_pitch(d) * 2);
 }
 
 difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, const void* W_scales, int32_t group, int64_t T,
@@ -172,17 +166,34 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
       !aligned_to(device_status, 4) || !aligned16(workspace))
     return DIFR_ERR_ALIGN;
   if (!workspace || workspace_bytes < difr_w4_workspace_bytes(T, d)) return DIFR_ERR_WORKSPACE;
-  int sms = 0;
-  const difr_status ds = device_sms(&sms);
+  if (too_many_tiles(T, V, 32)) return DIFR_ERR_SHAPE;
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
   W4LogitsParams p;
   memset(&p, 0, sizeof p);
+  int bn = 0, grid = 0;
+  const int64_t pitch = w4_pitch_bytes(d), h16_pitch = w4_h16_pitch(d);
+  plan_logit_tiles(T, V, h16_pitch * 2, V * pitch, 32, logits, dtype, ld, device_status, pairs, &p, &bn, &grid);
   p.h = static_cast<const __nv_bfloat16*>(h);
-  p.codes = static_cast<const unsigned char*>(W_codes);
   p.scales = static_cast<const __nv_bfloat16*>(W_scales);
-  p.logits = logits; p.ldh = ldh; p.ld = ld; p.device_status = device_status;
-  p.T = (int)T; p.d = (int)d; p.V = (int)V; p.group = group;
-  return launch_w4_logits(p, dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+  p.token_exp = static_cast<int*>(workspace);
+  p.h16 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + w4_exponent_bytes(T));
+  p.ldh = ldh; p.d = (int)d; p.group = group; p.h16_pitch = (int)h16_pitch;
+  p.k_steps = (int)((d + 127) / 128);
+  p.last_mmas = (int)((d - (int64_t)(p.k_steps - 1) * 128 + 15) / 16);
+  CUtensorMap tw, th, th_last, tout;
+  if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, 128) ||
+      !rows_tmap(&th, p.h16, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, T, h16_pitch, bn / 2))
+    return DIFR_ERR_CUDA;
+  th_last = th;
+  if (p.last_tokens != bn && !rows_tmap(&th_last, p.h16, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, T, h16_pitch, p.last_tokens / 2))
+    return DIFR_ERR_CUDA;
+  memset(&tout, 0, sizeof tout);
+  if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
+  return launch_w4_logits(bn, dtype, tw, th, th_last, tout, p, grid, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
+             ? DIFR_OK
+             : DIFR_ERR_CUDA;
 }
 
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {
@@ -212,8 +223,8 @@ difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_draft
   p.chunks = (int)verify_chunks(V, elem_bytes(in->dtype));
   if (!out->workspace || out->workspace_bytes < (size_t)(n_drafts + B) * (size_t)p.chunks * sizeof(float4))
     return DIFR_ERR_WORKSPACE;
-  int sms = 0;
-  const difr_status ds = device_sms(&sms);
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
   p.logits = in->logits; p.probs = in->draft_probs; p.drafted = in->draft_tokens; p.offsets = in->offsets;
   p.accept_words = in->accept_words; p.sample_words = in->sample_words;

@@ -31,6 +31,7 @@
 #include <string.h>
 
 #include "difr_kernels.h"
+#include "logit_tiles.cuh"
 #include "mx_device.cuh"
 #include "mx_kernels.h"
 
@@ -44,6 +45,7 @@ constexpr int kMxTmemCols = 512;
 
 template <int FMT, int BN>
 struct MxTile {
+  static constexpr int tokens = BN;
   static constexpr int words = FMT == kMx8 ? 1 : 2;       // scale words per slice (128 values each)
   static constexpr int row_blocks = BN > 128 ? 2 : 1;     // 128-token blocks of scales
   static constexpr int a_bytes = 128 * kMxSlice;
@@ -55,7 +57,7 @@ struct MxTile {
   static constexpr int bar_bytes = 512;
   // 256-token tiles leave through shared memory: out_buffers pieces in flight for each half of the epilogue
   static constexpr int out_buffers = BN == 256 ? 3 : 0;
-  static constexpr int out_bytes = 2 * out_buffers * kMxOutBytes;
+  static constexpr int out_bytes = 2 * out_buffers * kLogitOutBytes;
   static constexpr int fit = (227 * 1024 - 1024 - bar_bytes - out_bytes) / stage_bytes;
   static constexpr int stages = fit > 12 ? 12 : fit;
   static constexpr int smem_bytes = stages * stage_bytes + out_bytes + bar_bytes + 1024;  // + slack for 1024-byte alignment
@@ -73,146 +75,6 @@ struct MxTile {
   static_assert(sf_col0 + stages * sf_cols <= kMxTmemCols, "TMEM columns");
   static_assert(stages >= 4, "pipeline depth");
 };
-
-// Which chunk of the accumulator the `i`-th load of an epilogue half takes (-1: none).  Overlapping accumulators start
-// with the shared columns: the last ones of accumulator 0, the first ones of accumulator 1.
-template <int FMT, int BN>
-__device__ __forceinline__ int epi_chunk(int i, int half, int acc) {
-  using Tl = MxTile<FMT, BN>;
-  if (Tl::overlap) {
-    constexpr int shared = 2 * Tl::shared_loads, rest = Tl::chunks - shared;
-    if (i < Tl::shared_loads) return (acc == 0 ? rest : 0) + half * Tl::shared_loads + i;
-    return (acc == 0 ? 0 : shared) + half * (rest / 2) + i - Tl::shared_loads;
-  }
-  const int c = i * 2 + half;
-  return c < Tl::chunks ? c : -1;
-}
-
-// Token columns of one TMEM load -> logits.  r[j] is the logit of id `v` (this lane's) for token t0 + j.
-template <int N>
-__device__ __forceinline__ void store_chunk(const MxLogitsParams& p, const uint32_t (&r)[N], int t0, int v, float*) {
-  float* dst = static_cast<float*>(p.logits) + (int64_t)t0 * p.ld + v;
-  const bool ok = v < p.V;
-  const int n = p.T - t0;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if (j < n && ok) __stcs(dst, __uint_as_float(r[j]));
-    dst += p.ld;
-  }
-}
-template <int N>
-__device__ __forceinline__ void store_chunk(const MxLogitsParams& p, const uint32_t (&r)[N], int t0, int v,
-                                            __nv_bfloat16*) {
-  __nv_bfloat16* base = static_cast<__nv_bfloat16*>(p.logits) + (int64_t)t0 * p.ld;
-  const int n = p.T - t0;
-  if (p.pack_pairs) {
-    // neighbouring lanes trade: the even one takes ids v, v + 1 of token j, the odd one ids v - 1, v of token j + 1
-    const bool odd = (v & 1) != 0;
-    const int v0 = v & ~1;
-    __nv_bfloat16* dst = base + v0 + (odd ? p.ld : 0);
-#pragma unroll
-    for (int j = 0; j < N; j += 2) {
-      const float a = __uint_as_float(r[j]), b = __uint_as_float(r[j + 1]);
-      const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
-      __nv_bfloat162 two = odd ? __floats2bfloat162_rn(got, b) : __floats2bfloat162_rn(a, got);
-      if (j + (odd ? 1 : 0) < n) {
-        if (v0 + 1 < p.V)
-          __stcs(reinterpret_cast<uint32_t*>(dst), *reinterpret_cast<uint32_t*>(&two));
-        else if (v0 < p.V)
-          *dst = two.x;
-      }
-      dst += 2 * p.ld;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (j < n && v < p.V) base[(int64_t)j * p.ld + v] = __float2bfloat16_rn(__uint_as_float(r[j]));
-  }
-}
-
-// The staged way out of a 32-token chunk, for the four warps (128 ids) of an epilogue half: through pieces in shared
-// memory that leave by TMA, whole rows of 128 ids at a time.  (Stored from registers, a warp's 32 ids of one token
-// are a request of 128 or 64 bytes each, and the requests, not the bytes, were what the epilogue took its time for.)
-template <typename OUT>
-struct OutPieces {
-  static constexpr int kTokens = mx_out_tokens((int)sizeof(OUT));
-  OUT* buf;        // this half's pieces
-  int next;        // the one to fill
-  uint64_t policy;
-
-  template <int BUFFERS>
-  __device__ __forceinline__ void store(const MxLogitsParams& p, const CUtensorMap* map, const uint32_t (&r)[32], int t0,
-                                        int v_block, int quarter, int lane, int half) {
-    const bool issuer = quarter == 0 && lane == 0;
-#pragma unroll
-    for (int k = 0; k < 32 / kTokens; ++k) {
-      if (t0 + k * kTokens >= p.T) break;  // the same in all four warps
-      if (issuer) bulk_wait_read<BUFFERS - 1>();  // the store that last left from this piece has read it
-      named_barrier(1 + half, 128);
-      OUT* dst = buf + next * (kMxOutBytes / (int)sizeof(OUT));
-#pragma unroll
-      for (int j = 0; j < kTokens; ++j)
-        dst[j * 128 + quarter * 32 + lane] = from_float<OUT>(__uint_as_float(r[k * kTokens + j]));
-      fence_async_shared();
-      named_barrier(1 + half, 128);
-      if (issuer) {
-        if (v_block < p.V) tma_store_2d(map, v_block, t0 + k * kTokens, smem_u32(dst), policy);
-        bulk_commit();
-      }
-      if (++next == BUFFERS) next = 0;
-    }
-  }
-};
-
-// The tiles of one pair.  Tiles are numbered in groups of token tiles (a group's tokens stay in L2 while W passes by),
-// inside a group along the vocabulary, inside that along the group's token tiles, and are dealt out in rounds of one
-// tile per pair: the pairs that run at the same time share a few rows of W.  From round to round the deal shifts by
-// `shift` pairs, chosen so that the narrower last token tiles reach all pairs alike.
-struct TileWalk {
-  const MxLogitsParams& p;
-  const int pair, n_pairs;
-  int round0, turn;  // first tile of the round, pair that is dealt to first
-
-  __device__ __forceinline__ TileWalk(const MxLogitsParams& params, int pr, int n)
-      : p(params), pair(pr), n_pairs(n), round0(0), turn(0) {}
-  __device__ __forceinline__ bool next(int& vt, int& tt) {
-    const int at = pair - turn;
-    const int i = round0 + (at < 0 ? at + n_pairs : at);
-    if (i >= p.n_tiles) return false;
-    round0 += n_pairs;
-    turn += p.shift;
-    if (turn >= n_pairs) turn -= n_pairs;
-    const int per_group = p.group * p.n_vt;
-    const int g = i / per_group;
-    const int rem = i - g * per_group;
-    const int first = g * p.group;
-    const int cnt = min(p.group, p.n_tt - first);
-    vt = rem / cnt;
-    tt = first + rem - vt * cnt;
-    return true;
-  }
-};
-
-// After a wait that ran out: the warp's part of tile (vt, tt) and of the pair's next ones becomes NaN, so that no caller
-// takes what the buffer held before for logits.  `lane_id`: this lane's id inside a vocabulary tile.
-template <int FMT, int BN, typename OUT>
-__device__ __forceinline__ void fill_given_up(const MxLogitsParams& p, TileWalk& walk, int vt, int tt, int acc, int half,
-                                              int lane_id) {
-  using Tl = MxTile<FMT, BN>;
-  const OUT nan = from_float<OUT>(__int_as_float(0x7FC00000));
-  do {
-    const int v = vt * kMxPairM + lane_id;
-#pragma unroll 1
-    for (int i = 0; i < (Tl::chunks + 1) / 2; ++i) {
-      const int ch = epi_chunk<FMT, BN>(i, half, acc);
-      const int t0 = tt * BN + ch * Tl::chunk;
-      if (ch < 0 || v >= p.V) continue;
-#pragma unroll 1
-      for (int t = t0; t < t0 + Tl::chunk && t < p.T; ++t) static_cast<OUT*>(p.logits)[(int64_t)t * p.ld + v] = nan;
-    }
-    acc ^= 1;
-  } while (walk.next(vt, tt));
-}
 
 template <int FMT, int BN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMxThreads, 1)
@@ -296,7 +158,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int half = last ? p.last_tokens / 2 : BN / 2;
       const uint32_t bytes = (uint32_t)(Tl::load_bytes - (BN / 2 - half) * kMxSlice);
       const void* tmap_tokens = last ? &tmap_h_last : &tmap_h;
-      const int w_row = vt * kMxPairM + (int)cta * 128;
+      const int w_row = vt * kLogitPairM + (int)cta * 128;
       const int h_row = tt * BN + (int)cta * half;
       for (int k = 0; k < p.k_steps; ++k) {
         if (!__all_sync(0xffffffffu, mbar_wait(empty_bar(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
@@ -327,7 +189,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       bool ok = true;
       int vt, tt;
       for (; ok && walk.next(vt, tt); ++n_tile) {
-        const uint32_t idesc = umma_idesc_mx<FMT>(kMxPairM, tt == p.n_tt - 1 ? p.last_tokens : BN);
+        const uint32_t idesc = umma_idesc_mx<FMT>(kLogitPairM, tt == p.n_tt - 1 ? p.last_tokens : BN);
         // Separate accumulators: the tile before last has been read.  Overlapping ones: the shared columns of the last
         // tile have been read (every epilogue warp had then finished the tile before it).
         if (Tl::overlap) {
@@ -406,7 +268,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const bool ok = mbar_wait_cta(acc_full_bar(acc), acc_phase, false, abort_flag);
       __syncwarp();
       tc_fence_after();
-      const int v = vt * kMxPairM + (int)cta * 128 + quarter * 32 + lane;
+      const int v = vt * kLogitPairM + (int)cta * 128 + quarter * 32 + lane;
       const uint32_t free_bar = map_to_cta(acc_free_bar(acc), 0);
       // A tile store cuts rows at whole 16 bytes only: where the last ids end inside such a piece, they leave by plain
       // stores.
@@ -420,7 +282,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       auto load = [&](int c, int n) {
 #pragma unroll
         for (int q = 0; q < kFirst; ++q) {
-          const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
+          const int ch = epi_chunk<Tl>(c + q, half, acc);
           if (q < n && ch >= 0 && tt * BN + ch * Tl::chunk < p.T) {
             const uint32_t taddr = tmem_base + lane_addr + (uint32_t)(acc * Tl::acc_stride + ch * Tl::chunk);
             if constexpr (Tl::chunk == 32) tmem_ld_32x32(taddr, r[q]); else tmem_ld_32x16(taddr, r[q]);
@@ -448,7 +310,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         const int n_here = c == 0 ? kFirst : 1;
 #pragma unroll
         for (int q = 0; q < kFirst; ++q) {
-          const int ch = epi_chunk<FMT, BN>(c + q, half, acc);
+          const int ch = epi_chunk<Tl>(c + q, half, acc);
           const int t0 = tt * BN + ch * Tl::chunk;
           if (q < n_here && ch >= 0 && t0 < p.T) {
             if constexpr (BN == 256) {
@@ -469,7 +331,7 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
     if (BN == 256 && p.tile_stores) bulk_wait_all();  // the pieces stay until they have left
-    if (given_up) fill_given_up<FMT, BN, OUT>(p, walk, vt, tt, acc, half, (int)cta * 128 + quarter * 32 + lane);
+    if (given_up) fill_given_up<Tl, OUT>(p, walk, vt, tt, acc, half, (int)cta * 128 + quarter * 32 + lane);
   }
 
   __syncwarp();
@@ -516,7 +378,7 @@ mx_wait_selftest(const __grid_constant__ MxLogitsParams p, int done_tiles, long 
   __syncwarp();
   const bool given_up = BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !__all_sync(0xffffffffu, ok);
   if (given_up)
-    fill_given_up<FMT, BN, OUT>(p, walk, vt, tt, done_tiles & 1, half, (int)(blockIdx.x & 1) * 128 + quarter * 32 + lane);
+    fill_given_up<MxTile<FMT, BN>, OUT>(p, walk, vt, tt, done_tiles & 1, half, (int)(blockIdx.x & 1) * 128 + quarter * 32 + lane);
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
 }

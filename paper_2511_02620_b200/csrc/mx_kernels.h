@@ -38,13 +38,12 @@ struct MxConvertParams {
 cudaError_t launch_mx_quantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
 cudaError_t launch_mx_dequantize(const MxConvertParams& p, int dtype, cudaStream_t stream);
 
-struct MxLogitsParams {
+// The tiles of a product that makes logits.
+struct LogitTiles {
   void* logits;          // [T][ld]
   int64_t ld;
   int32_t* device_status;
   int T, V;
-  int k_steps;           // 128-byte slices of a row of codes
-  int last_mmas;         // MMAs (32 bytes of codes each) of the last slice
   int n_vt, n_tt;        // vocabulary tiles of 256 ids, token tiles
   int group;             // token tiles per raster group
   int last_tokens;       // width of the last token tile, a multiple of 16
@@ -54,9 +53,13 @@ struct MxLogitsParams {
   bool w_once;           // one token tile, and a W that does not fit L2: its rows need not stay there
   bool tile_stores;      // the rows of the logits start on 16-byte boundaries: tiles leave by TMA (256-token tiles only)
 };
-constexpr int kMxPairM = 256;  // vocabulary ids per tile of a CTA pair
-constexpr int kMxOutBytes = 8192;                            // a piece of a tile on its way out: 128 ids x
-constexpr int mx_out_tokens(int elem) { return kMxOutBytes / (128 * elem); }  // 16 (fp32) or 32 (bf16) tokens
+struct MxLogitsParams : LogitTiles {
+  int k_steps;           // 128-byte slices of a row of codes
+  int last_mmas;         // MMAs (32 bytes of codes each) of the last slice
+};
+constexpr int kLogitPairM = 256;  // vocabulary ids per tile of a CTA pair
+constexpr int kLogitOutBytes = 8192;                            // a piece of a tile on its way out: 128 ids x
+constexpr int logit_out_tokens(int elem) { return kLogitOutBytes / (128 * elem); }  // 16 (fp32) or 32 (bf16) tokens
 // `tokens_per_tile`: 16, 32, 64, 128 or 256; maps: codes of W, of h, of h for the last token tile, scales of W
 // and of h, logits (used with tile_stores only).
 cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,

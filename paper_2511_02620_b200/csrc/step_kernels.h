@@ -3,6 +3,7 @@
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -40,16 +41,20 @@ struct W4ConvertParams {
 cudaError_t launch_w4_quantize(const W4ConvertParams& p, int dtype, cudaStream_t stream);
 cudaError_t launch_w4_dequantize(const W4ConvertParams& p, int dtype, cudaStream_t stream);
 
-struct W4LogitsParams {
+struct W4LogitsParams : LogitTiles {
   const __nv_bfloat16* h;  // [T][ldh]
-  const unsigned char* codes;
   const __nv_bfloat16* scales;
-  void* logits;            // [T][ld]
-  int64_t ldh, ld;
-  int32_t* device_status;
-  int T, d, V, group;
+  __half* h16;             // [T][h16_pitch], workspace: h as the tensor cores take it
+  int* token_exp;          // [T], workspace: what the epilogue takes back of it
+  int64_t ldh;
+  int d, group, h16_pitch;
+  int k_steps;             // of 128 values
+  int last_mmas;           // MMAs (16 values each) of the last step
 };
-cudaError_t launch_w4_logits(const W4LogitsParams& p, int dtype, cudaStream_t stream);
+// `tokens_per_tile`: 32, 64, 128 or 256; maps: codes, h16, h16 for the last token tile, logits (used with tile_stores only).
+cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
+                             const CUtensorMap& h_last, const CUtensorMap& out, const W4LogitsParams& p, int grid,
+                             cudaStream_t stream);
 
 struct VerifyParams {
   const void* logits;            // [n_drafts + B][ld]
