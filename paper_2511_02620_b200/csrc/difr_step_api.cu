@@ -170,18 +170,22 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
   int pairs = 0;
   const difr_status ds = device_pairs(&pairs);
   if (ds != DIFR_OK) return ds;
+  const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   W4LogitsParams p;
   memset(&p, 0, sizeof p);
   int bn = 0, grid = 0;
   const int64_t pitch = w4_pitch_bytes(d), h16_pitch = w4_h16_pitch(d);
   plan_logit_tiles(T, V, h16_pitch * 2, V * pitch, 32, logits, dtype, ld, device_status, pairs, &p, &bn, &grid);
   p.h = static_cast<const __nv_bfloat16*>(h);
+  p.codes = static_cast<const unsigned char*>(W_codes);
   p.scales = static_cast<const __nv_bfloat16*>(W_scales);
   p.token_exp = static_cast<int*>(workspace);
   p.h16 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + w4_exponent_bytes(T));
   p.ldh = ldh; p.d = (int)d; p.group = group; p.h16_pitch = (int)h16_pitch;
   p.k_steps = (int)((d + 127) / 128);
-  p.last_mmas = (int)((d - (int64_t)(p.k_steps - 1) * 128 + 15) / 16);
+  p.half_last = d - (int64_t)(p.k_steps - 1) * 128 <= 64;
+  p.few = T <= kW4Few;
+  if (p.few) return launch_w4_few(dtype, p, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
   CUtensorMap tw, th, th_last, tout;
   if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, 128) ||
       !rows_tmap(&th, p.h16, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, T, h16_pitch, bn / 2))
@@ -191,9 +195,7 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
     return DIFR_ERR_CUDA;
   memset(&tout, 0, sizeof tout);
   if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
-  return launch_w4_logits(bn, dtype, tw, th, th_last, tout, p, grid, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess
-             ? DIFR_OK
-             : DIFR_ERR_CUDA;
+  return launch_w4_logits(bn, dtype, tw, th, th_last, tout, p, grid, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
 }
 
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {

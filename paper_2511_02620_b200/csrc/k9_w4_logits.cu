@@ -9,20 +9,29 @@
 // back.  What is smaller than 2^-31 of its row's largest hidden state, or in a group whose scale is below 2^-27 of its id's
 // largest, loses bits below 2^-39 (2^-35) of that largest.
 //
-// The vocabulary is the MMA's M side, as in the microscaled product.  Weights become fp16 on their way from shared memory to
-// TMEM, where the MMA takes its A operand from: a lane is an id, a thread turns words of eight codes into four pairs.
-// (word shifted & 0x03C003C0) ^ 0x4E004E00 are two numbers 24 + code in fp16, and one fma with (S, -24 S), S the scale, makes
-// them code * S, exactly: 24 S has ten bits.  A pair is the codes k and k + 4 of its eight, so `w4_prepare` lays out h in the
-// order 0 4 1 5 2 6 3 7.
+// Weights: a thread turns words of eight codes into four pairs of fp16.  (word shifted & 0x03C003C0) ^ 0x4E004E00 are two
+// numbers 24 + code, and one fma with (S, -24 S), S the scale, makes them code * S, exactly: 24 S has ten bits.  A pair is the
+// codes k and k + 4 of its word.
 //
-// CTAs run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads and converts its own 128 ids and
-// loads half of the tile's tokens, and the pair's first CTA issues the MMAs.  A step is 128 values of k: 64 TMEM columns of
-// converted weights (a slot), a stage of h; a stage of codes is two steps.
+// Two kernels, by the number of tokens alone; both take the vocabulary as the MMA's M side, read W once per token tile and
+// give the same bits (an MMA adds the same sixteen products in either).
 //
-// TMEM: two accumulators and the slots.  With BN = 256 the accumulators overlap by 128 columns, which the epilogue reads first.
+// Up to 16 tokens, `w4_few`: a warp takes 16 ids along all of k with mma.sync, codes straight from memory into the lanes that
+// convert them, four steps ahead.  Nothing meets anywhere, and 140 instructions a step of a warp leave memory the bound.
 //
+// More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
+// run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads and converts its own 128 ids and loads
+// half of the tile's tokens, and the pair's first CTA issues the MMAs.  A step is 128 values of k: 64 TMEM columns of
+// converted weights (a slot), a stage of h; a stage of codes is two steps.  TMEM: two accumulators and the slots; with BN =
+// 256 the accumulators overlap by 128 columns, which the epilogue reads first.  (An MMA of few tokens takes as long as one of
+// 128, 64 clocks: a step 512, where a step's bytes take 360.  Hence the other kernel.)
 // Warps: 0 TMA of h, 1 MMA, 2 TMEM allocation, 3 TMA of codes, 4..11 epilogue (two per lane quarter, half of the tile's columns
 // each), 12..19 conversion (two per lane quarter, even and odd steps).
+//
+// The order of k.  In mma.sync lane t of four holds, of a block of 128 values, the 32 at 32 t, and MMA 2 w + e / 2 .. adds
+// pairs q = 0, 1 (then 2, 3) of all four lanes' words w = 0 .. 3.  TMEM columns and h follow that: pair q of word w of
+// lane t is column 8 (2 w + q / 2) + 4 (q & 1) + t of a step.  Where the last block has 64 values at most, lane t holds the 16
+// at 16 t, two words.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <string.h>
@@ -40,6 +49,7 @@ constexpr int kW4TmemCols = 512;
 constexpr int kW4Step = 128;        // values of k
 constexpr int kW4SlotCols = 64;     // of a step: 128 fp16 a lane
 constexpr int kW4CodeBytes = 128 * 128;  // a stage of codes: two steps of 128 ids
+constexpr int kW4Ring = 8;          // barriers of steps
 
 template <int BN>
 struct W4Tile {
@@ -49,7 +59,7 @@ struct W4Tile {
   static constexpr int bar_bytes = 1024;
   static constexpr int out_buffers = BN == 256 ? 3 : 0;
   static constexpr int out_bytes = 2 * out_buffers * kLogitOutBytes;
-  static constexpr int h_stages = BN == 256 ? 4 : BN == 128 ? 5 : BN == 64 ? 6 : 8;
+  static constexpr int h_stages = BN == 256 ? 4 : 8;
   static constexpr int fit = (227 * 1024 - 1024 - bar_bytes - out_bytes - h_stages * h_bytes) / kW4CodeBytes;
   static constexpr int c_stages = fit > 12 ? 12 : fit;
   static constexpr int smem_bytes = h_stages * h_bytes + c_stages * kW4CodeBytes + out_bytes + bar_bytes + 1024;
@@ -64,7 +74,7 @@ struct W4Tile {
   static constexpr int chunks = BN / chunk;
   static constexpr int shared_loads = shared_cols / (2 * chunk);
   static_assert(c_stages >= 3 && slots >= 2, "pipeline depth");
-  static_assert((slots & (slots - 1)) == 0, "steps are counted modulo 2^32");
+  static_assert(slots <= kW4Ring && h_stages <= kW4Ring, "a step's barriers are waited for before their next turn");
 };
 
 // Instruction descriptor: dense, fp32 accumulator, fp16 A and B, both K-major.
@@ -104,14 +114,15 @@ __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr) {
 }
 
 // ------------------------------------------------------------------ hidden states
-// A row of h as fp16 times 2^e, e = 14 - exponent of its largest value, k in the order 0 4 1 5 2 6 3 7 of each eight, zeros
-// to whole 64; and -10 - e, the token's share of what the epilogue takes back.  A row with a NaN or an infinity is NaN.
+// A row of h as fp16 times 2^e, e = 14 - exponent of its largest value, in pairs in the order of k told above, zeros to whole
+// 64; and -10 - e, the token's share of what the epilogue takes back.  A row with a NaN or an infinity is NaN.  For
+// `w4_few` the 16 bytes of a word's four pairs lie together: [block][word][token][lane].
 constexpr int kPrepareThreads = 256;
 __global__ void __launch_bounds__(kPrepareThreads) w4_prepare(const W4LogitsParams p) {
   __shared__ uint32_t part[kPrepareThreads / 32];
   grid_release();
-  const int64_t t = blockIdx.x;
-  const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + t * p.ldh;
+  const int64_t token = blockIdx.x;
+  const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + token * p.ldh;
   const int d = p.d;
   uint32_t top = 0;  // magnitudes of bf16 compare like their bits, and a NaN's or an infinity's are above every number's
   for (int k = threadIdx.x; k < d; k += kPrepareThreads) top = max(top, (uint32_t)h[k] & 0x7FFFu);
@@ -123,35 +134,54 @@ __global__ void __launch_bounds__(kPrepareThreads) w4_prepare(const W4LogitsPara
   const bool broken = top >= 0x7F80u;
   const int e = broken || top == 0u ? 0 : 14 - (max((int)(top >> 7), 1) - 127);
   const float f1 = __int_as_float((127 + e / 2) << 23), f2 = __int_as_float((127 + e - e / 2) << 23);  // (|e| <= 141)
-  if (threadIdx.x == 0) p.token_exp[t] = -10 - e;
-  __half* out = p.h16 + t * p.h16_pitch;
+  if (threadIdx.x == 0) p.token_exp[token] = -10 - e;
+  __half2* out = reinterpret_cast<__half2*>(p.h16);
   for (int i = threadIdx.x; i < p.h16_pitch / 2; i += kPrepareThreads) {
-    // the pair at 2 i holds k = 8 (i / 4) + i % 4 and the one four further
-    const int k = (i >> 2) * 8 + (i & 3);
+    const int block = i >> 6, in = i & 63;
+    int w, q, t;
+    int64_t to;
+    if (p.few) {
+      q = in & 3; t = (in >> 2) & 3; w = in >> 4;
+      to = ((((int64_t)block * 4 + w) * p.T + token) * 4 + t) * 4 + q;
+    } else {
+      t = in & 3; q = ((in >> 2) & 1) + ((in >> 3) & 1) * 2; w = in >> 4;
+      to = token * (p.h16_pitch / 2) + i;
+    }
+    const int k = block * 128 + (p.half_last && block == p.k_steps - 1 ? 16 : 32) * t + 8 * w + q;
     const float a = k < d ? __uint_as_float((uint32_t)h[k] << 16) * f1 * f2 : 0.f;
     const float b = k + 4 < d ? __uint_as_float((uint32_t)h[k + 4] << 16) * f1 * f2 : 0.f;
     __half2 two = __floats2half2_rn(a, b);
     if (broken) two = __half2half2(__ushort_as_half((unsigned short)0x7FFF));
-    reinterpret_cast<__half2*>(out)[i] = two;
+    out[to] = two;
   }
 }
 
 // ------------------------------------------------------------------ scales
-// Exponent (floor log2) of the largest magnitude among a row's finite scales, 0 where there is none; scales below 2^-126
-// count as zero.
-__device__ __forceinline__ int row_exponent(const __nv_bfloat16* scales, int n8) {
-  uint32_t top = 0;
-  for (int i = 0; i < n8; ++i) {
-    const uint4 s = __ldg(reinterpret_cast<const uint4*>(scales) + i);
-    const uint32_t w[4] = {s.x, s.y, s.z, s.w};
+// Largest exponent field (times 2^7) of eight scales and `top`, NaN and infinities left out.
+__device__ __forceinline__ uint32_t fold_scales(uint4 s, uint32_t top) {
+  const uint32_t w[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t lo = w[k] & 0x7F80u, hi = (w[k] >> 16) & 0x7F80u;
-      if (lo != 0x7F80u) top = max(top, lo);
-      if (hi != 0x7F80u) top = max(top, hi);
-    }
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = w[k] & 0x7F80u, hi = (w[k] >> 16) & 0x7F80u;
+    if (lo != 0x7F80u) top = max(top, lo);
+    if (hi != 0x7F80u) top = max(top, hi);
   }
-  return top == 0u ? 0 : (int)(top >> 7) - 127;
+  return top;
+}
+// The exponent (floor log2) that is, 0 where no scale counts; scales below 2^-126 count as zero.
+__device__ __forceinline__ int scale_exponent(uint32_t top) { return top == 0u ? 0 : (int)(top >> 7) - 127; }
+// Of a row's scales i0, i0 + step .. (eights).
+__device__ __forceinline__ uint32_t fold_row(const __nv_bfloat16* scales, int i0, int step, int n8, uint32_t top) {
+  constexpr int U = 4;
+  for (int i = i0; i < n8; i += U * step) {
+    uint4 s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      s[u] = i + u * step < n8 ? __ldg(reinterpret_cast<const uint4*>(scales) + i + u * step) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fold_scales(s[u], top);
+  }
+  return top;
 }
 // A scale times 2^(10 - exponent) as a pair of fp16; NaN for a NaN or an infinity.
 __device__ __forceinline__ __half2 normal_scale(uint32_t bits16, int shift) {
@@ -160,17 +190,22 @@ __device__ __forceinline__ __half2 normal_scale(uint32_t bits16, int shift) {
   if (e == 255) s = __int_as_float(0x7FC00000);
   return __half2half2(__float2half_rn(s));
 }
-// The scales of a step, one for each 32 of its 128 values.
-__device__ __forceinline__ uint2 step_scales(const __nv_bfloat16* scales, int step, int group) {
-  if (group == 128) {
-    const uint32_t one = __ldg(reinterpret_cast<const unsigned short*>(scales) + step);
-    return make_uint2(one | (one << 16), one | (one << 16));
-  }
-  if (group == 64) {
-    const uint32_t two = __ldg(reinterpret_cast<const uint32_t*>(scales) + step);
-    return make_uint2(__byte_perm(two, 0, 0x1010), __byte_perm(two, 0, 0x3232));
-  }
-  return __ldg(reinterpret_cast<const uint2*>(scales) + step);
+// The scales of a step as they lie there, and one for each 32 of its 128 values.  (Two functions: what is done with a load
+// right behind it waits for it there and then.  Spread out when it came in, a step of conversion took 1570 clocks.)
+__device__ __forceinline__ uint2 load_step_scales(const __nv_bfloat16* scales, int step, int group) {
+  uint2 raw = make_uint2(0u, 0u);
+  if (group == 128)
+    raw.x = __ldg(reinterpret_cast<const unsigned short*>(scales) + step);
+  else if (group == 64)
+    raw.x = __ldg(reinterpret_cast<const uint32_t*>(scales) + step);
+  else
+    raw = __ldg(reinterpret_cast<const uint2*>(scales) + step);
+  return raw;
+}
+__device__ __forceinline__ uint2 spread_step_scales(uint2 raw, int group) {
+  if (group == 32) return raw;
+  const uint32_t lo = __byte_perm(raw.x, 0, 0x1010), hi = group == 128 ? lo : __byte_perm(raw.x, 0, 0x3232);
+  return make_uint2(lo, hi);
 }
 // Eight codes -> four pairs of fp16.
 __device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 offset, uint32_t* out) {
@@ -183,6 +218,11 @@ __device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 
   }
 }
 
+// x times 2^e, e from -276 to 230: three factors where one does not do, the rounding of the last to a subnormal apart exact.
+__device__ __forceinline__ float times_power(float x, int e) {
+  const int a = max(-120, min(120, e)), b = max(-120, min(120, e - a)), c = e - a - b;
+  return x * __int_as_float((127 + a) << 23) * __int_as_float((127 + b) << 23) * __int_as_float((127 + c) << 23);
+}
 // Takes the powers of two back: r[j] times 2^(ids's exponent + token's).  `mine`: the exponent of token t0 + lane.
 template <int N>
 __device__ __forceinline__ void take_back(uint32_t (&r)[N], int id_exp, int mine) {
@@ -194,20 +234,131 @@ __device__ __forceinline__ void take_back(uint32_t (&r)[N], int id_exp, int mine
     for (int j = 0; j < N; ++j)
       r[j] = __float_as_uint(__uint_as_float(r[j]) * __int_as_float(bits + __shfl_sync(0xffffffffu, more, j)));
   } else {
-#pragma unroll 1
-    for (int j = 0; j < N; ++j) {
-      const int e = id_exp + __shfl_sync(0xffffffffu, mine, j);
-      // (from -276 to 230: three factors, the sum's rounding to a subnormal last)
-      const int a = max(-120, min(120, e)), b = max(-120, min(120, e - a)), c = e - a - b;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i == j)
-          r[i] = __float_as_uint(__uint_as_float(r[i]) * __int_as_float((127 + a) << 23) * __int_as_float((127 + b) << 23) *
-                                 __int_as_float((127 + c) << 23));
-    }
+    for (int j = 0; j < N; ++j)
+      r[j] = __float_as_uint(times_power(__uint_as_float(r[j]), id_exp + __shfl_sync(0xffffffffu, mine, j)));
   }
 }
 
+// ------------------------------------------------------------------ up to 16 tokens
+constexpr int kFewWarps = 4, kFewIds = 16, kFewDepth = 4;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Codes are read once: past L1, where h is.
+__device__ __forceinline__ uint4 load_codes(const unsigned char* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+// NT: tiles of eight tokens.
+template <int NT, typename OUT>
+__global__ void __launch_bounds__(32 * kFewWarps) w4_few(const W4LogitsParams p) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t v0 = ((int64_t)blockIdx.x * kFewWarps + (threadIdx.x >> 5)) * kFewIds;
+  if (v0 >= p.V) return;
+  const int64_t pitch = w4_pitch_bytes(p.d), spitch = w4_scale_pitch(p.d, p.group);
+  const int64_t row[2] = {min(v0 + g, (int64_t)p.V - 1), min(v0 + g + 8, (int64_t)p.V - 1)};
+  const unsigned char* codes[2];
+  const __nv_bfloat16* scales[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    codes[r] = p.codes + row[r] * pitch;
+    scales[r] = p.scales + row[r] * spitch;
+  }
+  // of a step: this lane's 32 codes of both ids, and their scale
+  uint4 c[kFewDepth][2];
+  uint32_t s[kFewDepth][2];
+  const int per_scale = p.group / 32;
+  auto fetch = [&](int step, uint4 (&cc)[2], uint32_t (&ss)[2]) {
+    const bool half = p.half_last && step == p.k_steps - 1;
+    const int at = half ? step * 64 + 8 * t : step * 64 + 16 * t;  // bytes
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      cc[r] = make_uint4(0u, 0u, 0u, 0u);
+      ss[r] = 0u;
+      if (at < pitch) {
+        if (!half) {
+          cc[r] = load_codes(codes[r] + at);
+        } else {
+          const uint2 two = __ldg(reinterpret_cast<const uint2*>(codes[r] + at));
+          cc[r].x = two.x;
+          cc[r].y = two.y;
+        }
+        ss[r] = __ldg(reinterpret_cast<const unsigned short*>(scales[r]) + (at >> 4) / per_scale);
+      }
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kFewDepth; ++i)
+    if (i < p.k_steps) fetch(i, c[i], s[i]);
+  int shift[2], id_exp[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    uint32_t top = fold_row(scales[r], t, 4, (int)(spitch / 8), 0u);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    id_exp[r] = scale_exponent(top);
+    shift[r] = 10 - id_exp[r];
+  }
+  grid_wait();  // h comes from the kernel before
+  const uint4* h = reinterpret_cast<const uint4*>(p.h16) + g * 4 + t;  // [block][word][token][lane]
+  const int h_word = p.T * 4;
+  float acc[NT][4] = {};
+  const __half2 minus24 = __float2half2_rn(-24.f);
+  for (int s0 = 0; s0 < p.k_steps; s0 += kFewDepth) {
+#pragma unroll
+    for (int i = 0; i < kFewDepth; ++i) {
+      const int step = s0 + i;
+      if (step < p.k_steps) {
+        const int words = p.half_last && step == p.k_steps - 1 ? 2 : 4;
+        uint4 b[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            b[n][w] = w < words && n * 8 + g < p.T ? h[((int64_t)step * 4 + w) * h_word + n * 32] : make_uint4(0u, 0u, 0u, 0u);
+        __half2 scale[2], offset[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          scale[r] = normal_scale(s[i][r], shift[r]);
+          offset[r] = __hmul2(scale[r], minus24);
+        }
+        const uint32_t w0[4] = {c[i][0].x, c[i][0].y, c[i][0].z, c[i][0].w};
+        const uint32_t w1[4] = {c[i][1].x, c[i][1].y, c[i][1].z, c[i][1].w};
+        if (step + kFewDepth < p.k_steps) fetch(step + kFewDepth, c[i], s[i]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t a[4], a8[4];
+          convert_word(w0[w], scale[0], offset[0], a);
+          convert_word(w1[w], scale[1], offset[1], a8);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            mma_f16(acc[n], a[0], a8[0], a[1], a8[1], b[n][w].x, b[n][w].y);
+            mma_f16(acc[n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
+          }
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int token = n * 8 + 2 * t + (j & 1);
+      const int64_t v = v0 + g + (j >> 1) * 8;
+      if (token < p.T && v < p.V)
+        static_cast<OUT*>(p.logits)[(int64_t)token * p.ld + v] =
+            from_float<OUT>(times_power(acc[n][j], id_exp[j >> 1] + p.token_exp[token]));
+    }
+}
+
+// ------------------------------------------------------------------ more tokens
 template <int BN, typename OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kW4Threads, 1)
 w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_h,
@@ -220,26 +371,24 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   uint8_t* smem = smem_raw + (smem_base - raw_addr);
 
   // Both CTAs of a pair lay out their barriers at the same offsets.
-  //   h_full[s]   first CTA's copy is used: 1 arrival (its producer) + the bytes of both CTAs' loads
-  //   h_empty[s]  each CTA's own copy: 1 arrival, the commit of the MMAs that read the stage, delivered to both
-  //   c_full[s]   own: 1 arrival + the bytes of the CTA's codes;  c_empty[s] own: one arrival per conversion warp
-  //   a_full[s]   first CTA's copy is used: one arrival per conversion warp of the step, of both CTAs
-  //   a_empty[s]  each CTA's own copy: the commit of the MMAs that read the slot, delivered to both
+  //   full[g % 8]  of step g, first CTA's copy is used: 1 arrival (its producer of h) + the bytes of both CTAs' loads, one
+  //                arrival per conversion warp of the step, of both CTAs
+  //   done[g % 8]  of step g, each CTA's own copy: 1 arrival, the commit of its MMAs, delivered to both
+  //   c_full[s]    own: 1 arrival + the bytes of the CTA's codes;  c_empty[s] own: one arrival per conversion warp
   //   acc_full[a], acc_free[a]  as in the microscaled product
-  constexpr int HS = Tl::h_stages, CS = Tl::c_stages, AS = Tl::slots;
+  constexpr int HS = Tl::h_stages, CS = Tl::c_stages, AS = Tl::slots, R = kW4Ring;
   const uint32_t h_base = smem_base, c_base = smem_base + HS * Tl::h_bytes;
   uint8_t* out_pieces = smem + HS * Tl::h_bytes + CS * kW4CodeBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(out_pieces + Tl::out_bytes);
   const uint32_t bar0 = smem_u32(bars);
-  auto h_full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
-  auto h_empty = [&](int s) { return bar0 + 8u * (uint32_t)(HS + s); };
-  auto c_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + s); };
-  auto c_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + CS + s); };
-  auto a_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + s); };
-  auto a_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + AS + s); };
-  auto acc_full = [&](int a) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + 2 * AS + a); };
-  auto acc_free = [&](int a) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + 2 * AS + 2 + a); };
-  constexpr int kBars = 2 * HS + 2 * CS + 2 * AS + 4;
+  auto full = [&](uint32_t g) { return bar0 + 8u * (g % R); };
+  auto done = [&](uint32_t g) { return bar0 + 8u * (R + g % R); };
+  auto turn = [&](uint32_t g) { return (g / R) & 1u; };  // phase of a step's barriers
+  auto c_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * R + s); };
+  auto c_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * R + CS + s); };
+  auto acc_full = [&](int a) { return bar0 + 8u * (uint32_t)(2 * R + 2 * CS + a); };
+  auto acc_free = [&](int a) { return bar0 + 8u * (uint32_t)(2 * R + 2 * CS + 2 + a); };
+  constexpr int kBars = 2 * R + 2 * CS + 4;
   static_assert(kBars * 8 + 8 <= Tl::bar_bytes, "barrier block");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -251,17 +400,13 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   const int n_pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < HS; ++s) {
-      mbar_init(h_full(s), 1);
-      mbar_init(h_empty(s), 1);
+    for (uint32_t g = 0; g < R; ++g) {
+      mbar_init(full(g), 1 + kW4CvtWarps);
+      mbar_init(done(g), 1);
     }
     for (int s = 0; s < CS; ++s) {
       mbar_init(c_full(s), 1);
       mbar_init(c_empty(s), kW4CvtWarps);
-    }
-    for (int s = 0; s < AS; ++s) {
-      mbar_init(a_full(s), kW4CvtWarps);  // four warps of a step, of two CTAs
-      mbar_init(a_empty(s), 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full(a), 1);
@@ -293,9 +438,8 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     // ------------------------------------------------------------ TMA of h
     grid_wait();
     const uint64_t keep = l2_policy_evict_last();
-    const uint32_t full0_base = map_to_cta(h_full(0), 0);
-    int stage = 0;
-    uint32_t phase = 0;
+    const uint32_t full0_base = map_to_cta(full(0), 0);
+    uint32_t g = 0;  // step
     bool ok = true;
     int vt, tt;
     while (ok && walk.next(vt, tt)) {
@@ -303,18 +447,17 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int half = last ? p.last_tokens / 2 : BN / 2;
       const void* tmap_tokens = last ? &tmap_h_last : &tmap_h;
       const int h_row = tt * BN + (int)cta * half;
-      for (int k = 0; k < p.k_steps; ++k) {
-        if (!__all_sync(0xffffffffu, mbar_wait(h_empty(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
+      for (int k = 0; k < p.k_steps; ++k, ++g) {
+        if (g >= HS && !__all_sync(0xffffffffu, mbar_wait(done(g - HS), turn(g - HS), abort_flag))) { ok = false; break; }
         if (elect_one()) {
           // (the second box of the last step may lie behind the row: it reads zeros)
-          if (cta == 0) mbar_arrive_expect_tx(h_full(stage), 2u * 2u * (uint32_t)half * 128u);
-          const uint32_t full0 = full0_base + 8u * (uint32_t)stage;
-          const uint32_t dst = h_base + (uint32_t)(stage * Tl::h_bytes);
+          if (cta == 0) mbar_arrive_expect_tx(full(g), 2u * 2u * (uint32_t)half * 128u);
+          const uint32_t full0 = full0_base + 8u * (g % R);
+          const uint32_t dst = h_base + (g % HS) * (uint32_t)Tl::h_bytes;
           tma_load_2d_pair(dst, tmap_tokens, k * kW4Step, h_row, full0, keep);
           tma_load_2d_pair(dst + Tl::h_box, tmap_tokens, k * kW4Step + 64, h_row, full0, keep);
         }
         __syncwarp();
-        if (++stage == HS) { stage = 0; phase ^= 1u; }
       }
     }
   } else if (warp == 3) {
@@ -343,8 +486,9 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     if (cta == 0) {
       const uint64_t desc0 = umma_desc_k_major_sw128(h_base);
       const uint32_t desc_hi = (uint32_t)(desc0 >> 32), desc_lo0 = (uint32_t)desc0;
-      int stage = 0, slot = 0, acc = 0;
-      uint32_t phase = 0, slot_phase = 0, n_tile = 0;
+      int acc = 0;
+      uint32_t g = 0, n_tile = 0;
+      bool seen = false;
       bool ok = true;
       int vt, tt;
       for (; ok && walk.next(vt, tt); ++n_tile) {
@@ -364,31 +508,31 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * Tl::acc_stride);
-        // (a last token tile narrower than the others has its boxes closer together in the stage all the same)
         uint32_t accumulate = 0;
-        for (int k = 0; k < p.k_steps; ++k) {
-          if (!__all_sync(0xffffffffu, mbar_wait(h_full(stage), phase, abort_flag))) { ok = false; break; }
-          if (!__all_sync(0xffffffffu, mbar_wait(a_full(slot), slot_phase, abort_flag))) { ok = false; break; }
+        for (int k = 0; k < p.k_steps; ++k, ++g) {
+          if (!__all_sync(0xffffffffu, mbar_wait_cta(full(g), turn(g), seen, abort_flag))) { ok = false; break; }
+          // a look at the next step: its answer is there by the time it is needed
+          seen = mbar_peek_cta(full(g + 1), turn(g + 1));
           tc_fence_after();
-          const int n_mma = k + 1 < p.k_steps ? kW4Step / 16 : p.last_mmas;
-          const uint32_t b_lo = desc_lo0 + ((uint32_t)(stage * Tl::h_bytes) >> 4);
-          const uint32_t a_tmem = tmem_base + (uint32_t)(Tl::slot_col0 + slot * kW4SlotCols);
+          const uint32_t b_lo = desc_lo0 + (((g % HS) * (uint32_t)Tl::h_bytes) >> 4);
+          const uint32_t a_tmem = tmem_base + (uint32_t)Tl::slot_col0 + (g % AS) * kW4SlotCols;
+          const bool whole = !p.half_last || k + 1 < p.k_steps;
           if (elect_one()) {
+            // (a narrow last token tile has its second box at the same place)
 #pragma unroll
-            for (int kk = 0; kk < kW4Step / 16; ++kk) {
-              if (kk < n_mma) {
-                const uint64_t b_desc =
-                    ((uint64_t)desc_hi << 32) | (b_lo + (uint32_t)(kk >> 2) * (Tl::h_box >> 4) + 2u * (uint32_t)(kk & 3));
-                umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk, b_desc, idesc, kk == 0 ? accumulate : 1u);
-              }
+            for (int kk = 0; kk < 4; ++kk)
+              umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk, ((uint64_t)desc_hi << 32) | (b_lo + 2u * (uint32_t)kk), idesc,
+                                 kk == 0 ? accumulate : 1u);
+            if (whole) {
+#pragma unroll
+              for (int kk = 4; kk < 8; ++kk)
+                umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk,
+                                   ((uint64_t)desc_hi << 32) | (b_lo + (Tl::h_box >> 4) + 2u * (uint32_t)(kk & 3)), idesc, 1u);
             }
-            umma_commit_pair(h_empty(stage), 3);
-            umma_commit_pair(a_empty(slot), 3);
+            umma_commit_pair(done(g), 3);
           }
           __syncwarp();
           accumulate = 1;
-          if (++stage == HS) { stage = 0; phase ^= 1u; }
-          if (++slot == AS) { slot = 0; slot_phase ^= 1u; }
         }
         if (ok && elect_one()) umma_commit_pair(acc_full(acc), 3);
         __syncwarp();
@@ -402,64 +546,101 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
     const int r = quarter * 32 + lane;  // row of the CTA's 128
     const uint32_t row_smem = c_base + (uint32_t)r * 128u, swizzle = (uint32_t)(r & 7);
-    const uint32_t full0_base = map_to_cta(a_full(0), 0);
+    const uint32_t full0_base = map_to_cta(full(0), 0);
     const int64_t spitch = w4_scale_pitch(p.d, p.group);
+    const int n8 = (int)(spitch / 8);
     const __half2 minus24 = __float2half2_rn(-24.f);
     int stage = 0;
     uint32_t phase = 0, step0 = 0;  // steps of the tiles before
-    bool ok = true;
+    uint4 c[4];
+    // this thread's codes of the next stage, one ahead of the conversion
+    auto fetch = [&]() {
+      if (!__all_sync(0xffffffffu, mbar_wait_cta(c_full(stage), phase, false, abort_flag))) return false;
+      const uint32_t from = row_smem + (uint32_t)(stage * kW4CodeBytes);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(odd * 4 + j)) ^ swizzle) << 4));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(c_empty(stage));
+      if (++stage == CS) { stage = 0; phase ^= 1u; }
+      return true;
+    };
+    auto scales_of = [&](int vt) {
+      return p.scales + (int64_t)min(vt * kLogitPairM + (int)cta * 128 + r, p.V - 1) * spitch;
+    };
     int vt, tt;
-    while (ok && walk.next(vt, tt)) {
-      const int v = min(vt * kLogitPairM + (int)cta * 128 + r, p.V - 1);
-      const __nv_bfloat16* scales = p.scales + (int64_t)v * spitch;
-      const int shift = 10 - row_exponent(scales, (int)(spitch / 8));
-      uint2 sc = odd < p.k_steps ? step_scales(scales, odd, p.group) : make_uint2(0u, 0u);
+    bool more = walk.next(vt, tt), ok = true;
+    const __nv_bfloat16 *scales = nullptr, *next_scales = nullptr;
+    uint32_t top = 0;
+    uint2 raw = make_uint2(0u, 0u);
+    if (more) {
+      scales = scales_of(vt);
+      if (odd < p.k_steps) raw = load_step_scales(scales, odd, p.group);
+      top = fold_row(scales, 0, 1, n8, 0u);
+      ok = fetch();
+    }
+    while (more && ok) {
+      const int shift = 10 - scale_exponent(top);
+      more = walk.next(vt, tt);
+      next_scales = more ? scales_of(vt) : scales;
+      // the next tile's largest scale, eight scales a stage of codes: there are no more of them than stages
+      uint4 some = make_uint4(0u, 0u, 0u, 0u);
+      top = 0u;
       for (int k = 0; k < c_steps; ++k) {
         const int step = 2 * k + odd;
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(c_full(stage), phase, false, abort_flag))) { ok = false; break; }
-        if (step < p.k_steps) {
-          const uint32_t from = row_smem + (uint32_t)(stage * kW4CodeBytes);
-          uint4 c[4];
+        const bool mine = step < p.k_steps, half_step = p.half_last && step == p.k_steps - 1;
+        top = fold_scales(some, top);
+        if (k < n8) some = __ldg(reinterpret_cast<const uint4*>(next_scales) + k);
+        const uint32_t g = step0 + (uint32_t)step;
+        const uint32_t to = tmem_base + lane_addr + (uint32_t)Tl::slot_col0 + (g % AS) * kW4SlotCols;
+        uint32_t out[32];
+        __half2 s[4], off[4];
+        auto convert = [&](int half) {  // words 2 half and 2 half + 1 of the four chunks
 #pragma unroll
-          for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(odd * 4 + j)) ^ swizzle) << 4));
-          const uint2 here = sc;
-          if (step + 2 < p.k_steps) sc = step_scales(scales, step + 2, p.group);
-          const uint32_t g = step0 + (uint32_t)step;
-          const uint32_t slot = g % (uint32_t)AS, slot_phase = (g / (uint32_t)AS) & 1u;
-          const uint32_t to = tmem_base + lane_addr + (uint32_t)Tl::slot_col0 + slot * kW4SlotCols;
+          for (int t = 0; t < 4; ++t) {
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t out[32];
+            for (int w = 0; w < 2; ++w) {
+              uint32_t four[4];
+              convert_word(half == 0 ? (w == 0 ? c[t].x : c[t].y) : (w == 0 ? c[t].z : c[t].w), s[t], off[t], four);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t two = half == 0 ? here.x : here.y;
-              const __half2 s = normal_scale(j == 0 ? two & 0xFFFFu : two >> 16, shift);
-              const __half2 off = __hmul2(s, minus24);
-              const uint4& q = c[half * 2 + j];
-              convert_word(q.x, s, off, out + 16 * j);
-              convert_word(q.y, s, off, out + 16 * j + 4);
-              convert_word(q.z, s, off, out + 16 * j + 8);
-              convert_word(q.w, s, off, out + 16 * j + 12);
+              for (int q = 0; q < 4; ++q) out[8 * (2 * w + (q >> 1)) + 4 * (q & 1) + t] = four[q];
             }
-            if (half == 0) {
-              if (!__all_sync(0xffffffffu, mbar_wait_cta(a_empty((int)slot), slot_phase ^ 1u, false, abort_flag))) {
-                ok = false;
-                break;
-              }
-              tc_fence_after();
-            }
-            tmem_st_32x32(to + 32u * (uint32_t)half, out);
           }
-          if (!ok) break;
+        };
+        if (mine) {
+          uint2 here = spread_step_scales(raw, p.group);
+          if (half_step) {  // lane t of mma.sync: the 16 codes at 16 t
+            here = make_uint2(__byte_perm(here.x, 0, 0x1010), __byte_perm(here.x, 0, 0x3232));
+            c[3].x = c[1].z; c[3].y = c[1].w;
+            c[2].x = c[1].x; c[2].y = c[1].y;
+            c[1].x = c[0].z; c[1].y = c[0].w;
+          }
+          const bool in_tile = step + 2 < p.k_steps;
+          if (in_tile || (more && odd < p.k_steps))
+            raw = load_step_scales(in_tile ? scales : next_scales, in_tile ? step + 2 : odd, p.group);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t two = t < 2 ? here.x : here.y;
+            s[t] = normal_scale((t & 1) == 0 ? two & 0xFFFFu : two >> 16, shift);
+            off[t] = __hmul2(s[t], minus24);
+          }
+          convert(0);
+          if (g >= AS && !__all_sync(0xffffffffu, mbar_wait_cta(done(g - AS), turn(g - AS), false, abort_flag))) { ok = false; break; }
+          tc_fence_after();
+          tmem_st_32x32(to, out);
+          if (!half_step) convert(1);
+        }
+        if ((k + 1 < c_steps || more) && !fetch()) { ok = false; break; }
+        if (mine) {
+          if (!half_step) tmem_st_32x32(to + 32u, out);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster_nofence(full0_base + 8u * slot);  // (TMEM writes are ordered by the fence above)
+          if (lane == 0) mbar_arrive_cluster_nofence(full0_base + 8u * (g % R));  // (TMEM writes are ordered by the fence above)
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(c_empty(stage));
-        if (++stage == CS) { stage = 0; phase ^= 1u; }
       }
+      top = fold_scales(some, top);
+      if (ok && c_steps < n8) top = fold_row(next_scales, c_steps, 1, n8, top);
+      scales = next_scales;
       step0 += (uint32_t)p.k_steps;
     }
   } else if (warp >= kW4EpiWarp0) {
@@ -479,7 +660,7 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     bool given_up = false;
     while (walk.next(vt, tt)) {
       const int v = vt * kLogitPairM + (int)cta * 128 + quarter * 32 + lane;
-      const int id_exp = row_exponent(p.scales + (int64_t)min(v, p.V - 1) * spitch, (int)(spitch / 8));
+      const int id_exp = scale_exponent(fold_row(p.scales + (int64_t)min(v, p.V - 1) * spitch, 0, 1, (int)(spitch / 8), 0u));
       const bool ok = mbar_wait_cta(acc_full(acc), acc_phase, false, abort_flag);
       __syncwarp();
       tc_fence_after();
@@ -568,19 +749,18 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
 }
 
 // ------------------------------------------------------------------ launcher
-template <int BN, typename OUT>
-static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& hl, const CUtensorMap& out,
-                               const W4LogitsParams& p, int grid, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(w4_logits<BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, W4Tile<BN>::smem_bytes);
-  if (e != cudaSuccess) return e;
+// `w4_prepare`, and the kernel that may start while it runs.
+template <typename... P, typename... A>
+static cudaError_t launch_after_prepare(const W4LogitsParams& p, void (*kernel)(P...), int grid, int threads, int smem,
+                                        cudaStream_t stream, const A&... args) {
   w4_prepare<<<p.T, kPrepareThreads, 0, stream>>>(p);
-  e = cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
   cfg.gridDim = dim3((unsigned)grid, 1, 1);
-  cfg.blockDim = dim3(kW4Threads, 1, 1);
-  cfg.dynamicSmemBytes = W4Tile<BN>::smem_bytes;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   memset(&attr, 0, sizeof attr);
@@ -588,7 +768,16 @@ static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, w4_logits<BN, OUT>, w, h, hl, out, p);
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int BN, typename OUT>
+static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& hl, const CUtensorMap& out,
+                               const W4LogitsParams& p, int grid, cudaStream_t stream) {
+  const cudaError_t e =
+      cudaFuncSetAttribute(w4_logits<BN, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, W4Tile<BN>::smem_bytes);
+  if (e != cudaSuccess) return e;
+  return launch_after_prepare(p, w4_logits<BN, OUT>, grid, kW4Threads, W4Tile<BN>::smem_bytes, stream, w, h, hl, out, p);
 }
 
 template <typename OUT>
@@ -608,6 +797,15 @@ cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& 
                              cudaStream_t stream) {
   return dtype == kBf16 ? launch_typed<__nv_bfloat16>(tokens_per_tile, w, h, h_last, out, p, grid, stream)
                         : launch_typed<float>(tokens_per_tile, w, h, h_last, out, p, grid, stream);
+}
+
+cudaError_t launch_w4_few(int dtype, const W4LogitsParams& p, cudaStream_t stream) {
+  const int grid = (int)((p.V + (int64_t)kFewIds * kFewWarps - 1) / (kFewIds * kFewWarps));
+  if (dtype == kBf16)
+    return p.T <= 8 ? launch_after_prepare(p, w4_few<1, __nv_bfloat16>, grid, 32 * kFewWarps, 0, stream, p)
+                    : launch_after_prepare(p, w4_few<2, __nv_bfloat16>, grid, 32 * kFewWarps, 0, stream, p);
+  return p.T <= 8 ? launch_after_prepare(p, w4_few<1, float>, grid, 32 * kFewWarps, 0, stream, p)
+                  : launch_after_prepare(p, w4_few<2, float>, grid, 32 * kFewWarps, 0, stream, p);
 }
 
 }  // namespace difr
