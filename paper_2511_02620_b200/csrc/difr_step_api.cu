@@ -55,6 +55,19 @@ bool rows_tmap(CUtensorMap* map, const void* base, CUtensorMapDataType type, int
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Scales: boxes of eight of sixteen rows.
+bool scales_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t spitch) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)spitch, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(spitch * 2)};
+  const cuuint32_t box[2] = {8, 16};
+  const cuuint32_t estr[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // Records of a row: its vectors, of which the first may begin before the row.
 int64_t verify_chunks(int64_t V, int elem) {
   const int64_t n = 16 / elem;
@@ -177,7 +190,6 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
   const int64_t pitch = w4_pitch_bytes(d), h16_pitch = w4_h16_pitch(d);
   plan_logit_tiles(T, V, h16_pitch * 2, V * pitch, 32, logits, dtype, ld, device_status, pairs, &p, &bn, &grid);
   p.h = static_cast<const __nv_bfloat16*>(h);
-  p.codes = static_cast<const unsigned char*>(W_codes);
   p.scales = static_cast<const __nv_bfloat16*>(W_scales);
   p.token_exp = static_cast<int*>(workspace);
   p.h16 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + w4_exponent_bytes(T));
@@ -185,8 +197,12 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
   p.k_steps = (int)((d + 127) / 128);
   p.half_last = d - (int64_t)(p.k_steps - 1) * 128 <= 64;
   p.few = T <= kW4Few;
-  if (p.few) return launch_w4_few(dtype, p, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
   CUtensorMap tw, th, th_last, tout;
+  if (p.few) {
+    if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, 16) || !scales_tmap(&th, W_scales, V, w4_scale_pitch(d, group)))
+      return DIFR_ERR_CUDA;
+    return launch_w4_few(dtype, tw, th, p, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+  }
   if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, 128) ||
       !rows_tmap(&th, p.h16, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, T, h16_pitch, bn / 2))
     return DIFR_ERR_CUDA;

@@ -16,8 +16,8 @@
 // Two kernels, by the number of tokens alone; both take the vocabulary as the MMA's M side, read W once per token tile and
 // give the same bits (an MMA adds the same sixteen products in either).
 //
-// Up to 16 tokens, `w4_few`: a warp takes 16 ids along all of k with mma.sync, codes straight from memory into the lanes that
-// convert them, four steps ahead.  Nothing meets anywhere, and 140 instructions a step of a warp leave memory the bound.
+// Up to 16 tokens, `w4_few`: a warp takes 16 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, three
+// stages of two steps ahead, and meets nobody.
 //
 // More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
 // run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads and converts its own 128 ids and loads
@@ -35,6 +35,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <string.h>
+
+#include <type_traits>
 
 #include "difr_kernels.h"
 #include "logit_tiles.cuh"
@@ -183,12 +185,14 @@ __device__ __forceinline__ uint32_t fold_row(const __nv_bfloat16* scales, int i0
   }
   return top;
 }
-// A scale times 2^(10 - exponent) as a pair of fp16; NaN for a NaN or an infinity.
-__device__ __forceinline__ __half2 normal_scale(uint32_t bits16, int shift) {
-  const int e = (int)((bits16 >> 7) & 255u);
-  float s = e == 0 || e + shift <= 0 ? 0.f : __uint_as_float((bits16 << 16) + ((uint32_t)shift << 23));
-  if (e == 255) s = __int_as_float(0x7FC00000);
-  return __half2half2(__float2half_rn(s));
+// A scale times 2^(10 - exponent) as a pair of fp16.  That power as two factors: one would leave fp32 for tiny scales.  (An
+// infinity ends as NaN: 24 times it is taken off.)
+__device__ __forceinline__ float2 scale_factors(int exponent) {
+  const int shift = 10 - exponent;
+  return make_float2(__int_as_float((127 + shift / 2) << 23), __int_as_float((127 + shift - shift / 2) << 23));
+}
+__device__ __forceinline__ __half2 normal_scale(uint32_t bits16, float2 by) {
+  return __float2half2_rn(__uint_as_float(bits16 << 16) * by.x * by.y);
 }
 // The scales of a step as they lie there, and one for each 32 of its 128 values.  (Two functions: what is done with a load
 // right behind it waits for it there and then.  Spread out when it came in, a step of conversion took 1570 clocks.)
@@ -207,12 +211,24 @@ __device__ __forceinline__ uint2 spread_step_scales(uint2 raw, int group) {
   const uint32_t lo = __byte_perm(raw.x, 0, 0x1010), hi = group == 128 ? lo : __byte_perm(raw.x, 0, 0x3232);
   return make_uint2(lo, hi);
 }
-// Eight codes -> four pairs of fp16.
-__device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 offset, uint32_t* out) {
-  const uint32_t at[4] = {w << 6, w << 2, w >> 2, w >> 6};
+// Eight codes -> four pairs of fp16.  (The logic as one instruction with both constants in registers: it takes one immediate
+// only, and left to itself the compiler spent 14 of them on a word, which set the pace.  Shifts to the left go as products,
+// so that they share a pipe with the fma and not with the logic.)
+struct ConvertBits {
+  uint32_t mask, magic;
+};
+__device__ __forceinline__ ConvertBits convert_bits() {
+  ConvertBits b;
+  asm volatile("mov.b32 %0, 0x03C003C0;" : "=r"(b.mask));
+  asm volatile("mov.b32 %0, 0x4E004E00;" : "=r"(b.magic));
+  return b;
+}
+__device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 offset, ConvertBits k, uint32_t* out) {
+  const uint32_t at[4] = {w * 64u, w * 4u, w >> 2, w >> 6};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t bits = (at[i] & 0x03C003C0u) ^ 0x4E004E00u;
+    uint32_t bits;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(bits) : "r"(at[i]), "r"(k.mask), "r"(k.magic));  // (a & b) ^ c
     const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&bits), scale, offset);
     out[i] = *reinterpret_cast<const uint32_t*>(&v);
   }
@@ -241,7 +257,11 @@ __device__ __forceinline__ void take_back(uint32_t (&r)[N], int id_exp, int mine
 }
 
 // ------------------------------------------------------------------ up to 16 tokens
-constexpr int kFewWarps = 4, kFewIds = 16, kFewDepth = 4;
+constexpr int kFewWarps = 4, kFewIds = 16;
+constexpr int kFewStages = 3, kFewStageBytes = kFewIds * 128;      // codes of two steps of 16 ids
+constexpr int kFewScaleSlots = 4, kFewScaleBytes = kFewIds * 16;   // eight scales of 16 ids
+constexpr int kFewWarpBytes = kFewStages * kFewStageBytes + kFewScaleSlots * kFewScaleBytes;
+constexpr int kFewSmem = kFewWarps * kFewWarpBytes + kFewWarps * kFewStages * 8 + 1024;  // + barriers, alignment
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -249,112 +269,167 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Codes are read once: past L1, where h is.
-__device__ __forceinline__ uint4 load_codes(const unsigned char* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+__device__ __forceinline__ uint2 ld_shared_8(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
   return v;
+}
+__device__ __forceinline__ uint32_t ld_shared_2(uint32_t addr) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void tma_load_2d_hint(uint32_t dst_smem, const void* tmap, int x, int y, uint32_t bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
+      ::"r"(dst_smem), "l"(tmap), "r"(x), "r"(y), "r"(bar), "l"(policy)
+      : "memory");
 }
 
 // NT: tiles of eight tokens.
 template <int NT, typename OUT>
-__global__ void __launch_bounds__(32 * kFewWarps) w4_few(const W4LogitsParams p) {
-  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int64_t v0 = ((int64_t)blockIdx.x * kFewWarps + (threadIdx.x >> 5)) * kFewIds;
-  if (v0 >= p.V) return;
-  const int64_t pitch = w4_pitch_bytes(p.d), spitch = w4_scale_pitch(p.d, p.group);
-  const int64_t row[2] = {min(v0 + g, (int64_t)p.V - 1), min(v0 + g + 8, (int64_t)p.V - 1)};
-  const unsigned char* codes[2];
-  const __nv_bfloat16* scales[2];
-#pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    codes[r] = p.codes + row[r] * pitch;
-    scales[r] = p.scales + row[r] * spitch;
+__global__ void __launch_bounds__(32 * kFewWarps)
+w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_s,
+       const __grid_constant__ W4LogitsParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t code_ring = smem_base + (uint32_t)(warp * kFewStages * kFewStageBytes);
+  const uint32_t scale_ring = smem_base + (uint32_t)(kFewWarps * kFewStages * kFewStageBytes + warp * kFewScaleSlots * kFewScaleBytes);
+  const uint32_t bars = smem_base + (uint32_t)(kFewWarps * kFewWarpBytes + warp * kFewStages * 8);
+  volatile int* abort_flag = &abort_word;
+  if (threadIdx.x == 0) abort_word = 0;
+  if (lane == 0) {
+    for (int s = 0; s < kFewStages; ++s) mbar_init(bars + 8u * (uint32_t)s, 1);
+    mbar_fence_init();
   }
-  // of a step: this lane's 32 codes of both ids, and their scale
-  uint4 c[kFewDepth][2];
-  uint32_t s[kFewDepth][2];
-  const int per_scale = p.group / 32;
-  auto fetch = [&](int step, uint4 (&cc)[2], uint32_t (&ss)[2]) {
-    const bool half = p.half_last && step == p.k_steps - 1;
-    const int at = half ? step * 64 + 8 * t : step * 64 + 16 * t;  // bytes
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      cc[r] = make_uint4(0u, 0u, 0u, 0u);
-      ss[r] = 0u;
-      if (at < pitch) {
-        if (!half) {
-          cc[r] = load_codes(codes[r] + at);
-        } else {
-          const uint2 two = __ldg(reinterpret_cast<const uint2*>(codes[r] + at));
-          cc[r].x = two.x;
-          cc[r].y = two.y;
-        }
-        ss[r] = __ldg(reinterpret_cast<const unsigned short*>(scales[r]) + (at >> 4) / per_scale);
-      }
+  __syncthreads();
+  const int64_t v0 = ((int64_t)blockIdx.x * kFewWarps + warp) * kFewIds;
+  if (v0 >= p.V) return;  // (nothing below waits for another warp)
+
+  const int n_stages = (p.k_steps + 1) / 2;
+  const int per_slot = p.group / 32;  // stages of codes that a slot of scales is for: 4, 2 or 1
+  const uint64_t policy = p.w_once ? l2_policy_evict_first() : l2_policy_evict_normal();
+  auto fetch = [&](int stage) {  // one lane
+    const uint32_t bar = bars + 8u * (uint32_t)(stage % kFewStages);
+    const bool with_scales = stage % per_slot == 0;
+    mbar_arrive_expect_tx(bar, (uint32_t)(kFewStageBytes + (with_scales ? kFewScaleBytes : 0)));
+    tma_load_2d_hint(code_ring + (uint32_t)(stage % kFewStages * kFewStageBytes), &tmap_w, stage * 128, (int)v0, bar, policy);
+    if (with_scales) {
+      const int slot = stage / per_slot;
+      tma_load_2d_hint(scale_ring + (uint32_t)(slot % kFewScaleSlots * kFewScaleBytes), &tmap_s, slot * 8, (int)v0, bar, policy);
     }
   };
-#pragma unroll
-  for (int i = 0; i < kFewDepth; ++i)
-    if (i < p.k_steps) fetch(i, c[i], s[i]);
-  int shift[2], id_exp[2];
+  if (lane == 0)
+    for (int s = 0; s < kFewStages && s < n_stages; ++s) fetch(s);
+  // ids of this lane's two rows of the MMA: neighbours among the 16 bytes that eight lanes read at once lie in different halves
+  // of the swizzled 128-byte lines
+  const int at0 = ((g & 1) << 2) | (g >> 1);
+  const int64_t spitch = w4_scale_pitch(p.d, p.group);
+  float2 by[2];
+  int id_exp[2];
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    uint32_t top = fold_row(scales[r], t, 4, (int)(spitch / 8), 0u);
+    const __nv_bfloat16* scales = p.scales + min(v0 + at0 + 8 * r, (int64_t)p.V - 1) * spitch;
+    uint32_t top = fold_row(scales, t, 4, (int)(spitch / 8), 0u);
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     id_exp[r] = scale_exponent(top);
-    shift[r] = 10 - id_exp[r];
+    by[r] = scale_factors(id_exp[r]);
   }
   grid_wait();  // h comes from the kernel before
-  const uint4* h = reinterpret_cast<const uint4*>(p.h16) + g * 4 + t;  // [block][word][token][lane]
+  // [block][word][token][lane]; lanes without a token read another one's, for columns that nobody looks at
+  const uint4* h[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) h[n] = reinterpret_cast<const uint4*>(p.h16) + min(n * 8 + g, p.T - 1) * 4 + t;
   const int h_word = p.T * 4;
   float acc[NT][4] = {};
   const __half2 minus24 = __float2half2_rn(-24.f);
-  for (int s0 = 0; s0 < p.k_steps; s0 += kFewDepth) {
+  const ConvertBits k = convert_bits();
+  // One step: the codes and scales of both ids, and h, of which `words` words are there.
+  auto take = [&](const uint4 c0, const uint4 c1, const uint32_t s0, const uint32_t s1, auto words) {
+    constexpr int W = decltype(words)::value;
+    uint4 b[NT][W];
 #pragma unroll
-    for (int i = 0; i < kFewDepth; ++i) {
-      const int step = s0 + i;
-      if (step < p.k_steps) {
-        const int words = p.half_last && step == p.k_steps - 1 ? 2 : 4;
-        uint4 b[NT][4];
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+      for (int w = 0; w < W; ++w) b[n][w] = h[n][w * h_word];
+      h[n] += 4 * h_word;
+    }
+    const __half2 scale[2] = {normal_scale(s0, by[0]), normal_scale(s1, by[1])};
+    const __half2 offset[2] = {__hmul2(scale[0], minus24), __hmul2(scale[1], minus24)};
+    const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w};
+    const uint32_t w1[4] = {c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            b[n][w] = w < words && n * 8 + g < p.T ? h[((int64_t)step * 4 + w) * h_word + n * 32] : make_uint4(0u, 0u, 0u, 0u);
-        __half2 scale[2], offset[2];
+    for (int w = 0; w < W; ++w) {
+      uint32_t a[4], a8[4];
+      convert_word(w0[w], scale[0], offset[0], k, a);
+      convert_word(w1[w], scale[1], offset[1], k, a8);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          scale[r] = normal_scale(s[i][r], shift[r]);
-          offset[r] = __hmul2(scale[r], minus24);
-        }
-        const uint32_t w0[4] = {c[i][0].x, c[i][0].y, c[i][0].z, c[i][0].w};
-        const uint32_t w1[4] = {c[i][1].x, c[i][1].y, c[i][1].z, c[i][1].w};
-        if (step + kFewDepth < p.k_steps) fetch(step + kFewDepth, c[i], s[i]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t a[4], a8[4];
-          convert_word(w0[w], scale[0], offset[0], a);
-          convert_word(w1[w], scale[1], offset[1], a8);
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            mma_f16(acc[n], a[0], a8[0], a[1], a8[1], b[n][w].x, b[n][w].y);
-            mma_f16(acc[n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
-          }
-        }
+      for (int n = 0; n < NT; ++n) {
+        mma_f16(acc[n], a[0], a8[0], a[1], a8[1], b[n][w].x, b[n][w].y);
+        mma_f16(acc[n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
       }
     }
+  };
+  // of a stage: the line of this lane's ids, chunk `c` of eight; the scale of chunk c (32 codes)
+  const uint32_t line = code_ring + (uint32_t)(at0 * 128), swizzle = (uint32_t)at0;
+  const int scale_shift = p.group == 128 ? 2 : p.group == 64 ? 1 : 0;
+  auto scale_at = [&](int chunk) {  // of the row
+    const int i = chunk >> scale_shift;
+    return scale_ring + (uint32_t)((i >> 3) % kFewScaleSlots * kFewScaleBytes + (i & 7) * 2 + at0 * 16);
+  };
+  bool ok = true;
+  const int whole = (p.k_steps - (p.half_last ? 1 : 0)) / 2;  // stages of two whole steps
+  int slot = 0;
+  uint32_t phase = 0;
+  for (int i = 0; i < whole; ++i) {
+    ok = __all_sync(0xffffffffu, mbar_wait_cta(bars + 8u * (uint32_t)slot, phase, false, abort_flag));
+    if (!ok) break;
+    const uint32_t from = line + (uint32_t)(slot * kFewStageBytes);
+    const uint32_t x0 = from + (((uint32_t)t ^ swizzle) << 4), x1 = from + (((uint32_t)(t + 4) ^ swizzle) << 4);
+    const uint4 c00 = ld_shared_16(x0), c01 = ld_shared_16(x0 + 1024), c10 = ld_shared_16(x1), c11 = ld_shared_16(x1 + 1024);
+    const uint32_t y0 = scale_at(8 * i + t), y1 = scale_at(8 * i + 4 + t);
+    const uint32_t s00 = ld_shared_2(y0), s01 = ld_shared_2(y0 + 128), s10 = ld_shared_2(y1), s11 = ld_shared_2(y1 + 128);
+    __syncwarp();
+    if (lane == 0 && i + kFewStages < n_stages) fetch(i + kFewStages);
+    take(c00, c01, s00, s01, std::integral_constant<int, 4>());
+    take(c10, c11, s10, s11, std::integral_constant<int, 4>());
+    if (++slot == kFewStages) { slot = 0; phase ^= 1u; }
+  }
+  if (ok && whole < n_stages) {  // a whole step, a half one, or both
+    ok = __all_sync(0xffffffffu, mbar_wait_cta(bars + 8u * (uint32_t)slot, phase, false, abort_flag));
+    const uint32_t from = line + (uint32_t)(slot * kFewStageBytes);
+    int step = 2 * whole;
+    if (ok && step < p.k_steps - (p.half_last ? 1 : 0)) {
+      const uint32_t x = from + (((uint32_t)t ^ swizzle) << 4), y = scale_at(4 * step + t);
+      take(ld_shared_16(x), ld_shared_16(x + 1024), ld_shared_2(y), ld_shared_2(y + 128), std::integral_constant<int, 4>());
+      ++step;
+    }
+    if (ok && step < p.k_steps) {
+      const int chunk = (step & 1) * 4 + (t >> 1);  // of the stage; this lane's half of it
+      const uint32_t x = from + (((uint32_t)chunk ^ swizzle) << 4) + (uint32_t)(t & 1) * 8, y = scale_at(4 * step + (t >> 1));
+      const uint2 c0 = ld_shared_8(x), c1 = ld_shared_8(x + 1024);
+      take(make_uint4(c0.x, c0.y, 0u, 0u), make_uint4(c1.x, c1.y, 0u, 0u), ld_shared_2(y), ld_shared_2(y + 128),
+           std::integral_constant<int, 2>());
+    }
+  }
+  if (!ok) {  // a wait ran out: what was not computed is NaN; copies in flight get time to land
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) { }
+    if (lane == 0 && p.device_status != nullptr) *p.device_status = kStatusTimeout;
   }
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int token = n * 8 + 2 * t + (j & 1);
-      const int64_t v = v0 + g + (j >> 1) * 8;
+      const int64_t v = v0 + at0 + (j >> 1) * 8;
+      const float value = ok ? acc[n][j] : __int_as_float(0x7FC00000);
       if (token < p.T && v < p.V)
         static_cast<OUT*>(p.logits)[(int64_t)token * p.ld + v] =
-            from_float<OUT>(times_power(acc[n][j], id_exp[j >> 1] + p.token_exp[token]));
+            from_float<OUT>(times_power(value, id_exp[j >> 1] + p.token_exp[token]));
     }
 }
 
@@ -550,6 +625,7 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     const int64_t spitch = w4_scale_pitch(p.d, p.group);
     const int n8 = (int)(spitch / 8);
     const __half2 minus24 = __float2half2_rn(-24.f);
+    const ConvertBits bits = convert_bits();
     int stage = 0;
     uint32_t phase = 0, step0 = 0;  // steps of the tiles before
     uint4 c[4];
@@ -579,7 +655,7 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       ok = fetch();
     }
     while (more && ok) {
-      const int shift = 10 - scale_exponent(top);
+      const float2 by = scale_factors(scale_exponent(top));
       more = walk.next(vt, tt);
       next_scales = more ? scales_of(vt) : scales;
       // the next tile's largest scale, eight scales a stage of codes: there are no more of them than stages
@@ -600,7 +676,7 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
               uint32_t four[4];
-              convert_word(half == 0 ? (w == 0 ? c[t].x : c[t].y) : (w == 0 ? c[t].z : c[t].w), s[t], off[t], four);
+              convert_word(half == 0 ? (w == 0 ? c[t].x : c[t].y) : (w == 0 ? c[t].z : c[t].w), s[t], off[t], bits, four);
 #pragma unroll
               for (int q = 0; q < 4; ++q) out[8 * (2 * w + (q >> 1)) + 4 * (q & 1) + t] = four[q];
             }
@@ -620,7 +696,7 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const uint32_t two = t < 2 ? here.x : here.y;
-            s[t] = normal_scale((t & 1) == 0 ? two & 0xFFFFu : two >> 16, shift);
+            s[t] = normal_scale((t & 1) == 0 ? two : two >> 16, by);
             off[t] = __hmul2(s[t], minus24);
           }
           convert(0);
@@ -799,13 +875,17 @@ cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& 
                         : launch_typed<float>(tokens_per_tile, w, h, h_last, out, p, grid, stream);
 }
 
-cudaError_t launch_w4_few(int dtype, const W4LogitsParams& p, cudaStream_t stream) {
+template <int NT, typename OUT>
+static cudaError_t launch_few(const CUtensorMap& w, const CUtensorMap& s, const W4LogitsParams& p, cudaStream_t stream) {
+  const cudaError_t e = cudaFuncSetAttribute(w4_few<NT, OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+  if (e != cudaSuccess) return e;
   const int grid = (int)((p.V + (int64_t)kFewIds * kFewWarps - 1) / (kFewIds * kFewWarps));
+  return launch_after_prepare(p, w4_few<NT, OUT>, grid, 32 * kFewWarps, kFewSmem, stream, w, s, p);
+}
+cudaError_t launch_w4_few(int dtype, const CUtensorMap& w, const CUtensorMap& s, const W4LogitsParams& p, cudaStream_t stream) {
   if (dtype == kBf16)
-    return p.T <= 8 ? launch_after_prepare(p, w4_few<1, __nv_bfloat16>, grid, 32 * kFewWarps, 0, stream, p)
-                    : launch_after_prepare(p, w4_few<2, __nv_bfloat16>, grid, 32 * kFewWarps, 0, stream, p);
-  return p.T <= 8 ? launch_after_prepare(p, w4_few<1, float>, grid, 32 * kFewWarps, 0, stream, p)
-                  : launch_after_prepare(p, w4_few<2, float>, grid, 32 * kFewWarps, 0, stream, p);
+    return p.T <= 8 ? launch_few<1, __nv_bfloat16>(w, s, p, stream) : launch_few<2, __nv_bfloat16>(w, s, p, stream);
+  return p.T <= 8 ? launch_few<1, float>(w, s, p, stream) : launch_few<2, float>(w, s, p, stream);
 }
 
 }  // namespace difr

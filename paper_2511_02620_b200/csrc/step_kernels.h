@@ -43,7 +43,6 @@ cudaError_t launch_w4_dequantize(const W4ConvertParams& p, int dtype, cudaStream
 
 struct W4LogitsParams : LogitTiles {
   const __nv_bfloat16* h;  // [T][ldh]
-  const unsigned char* codes;
   const __nv_bfloat16* scales;
   __half* h16;             // [T][h16_pitch], workspace: h as the tensor cores take it
   int* token_exp;          // [T], workspace: what the epilogue takes back of it
@@ -54,7 +53,8 @@ struct W4LogitsParams : LogitTiles {
   bool few;                // launch_w4_few: only the sizes, buffers and strides of the tiles' part are used
 };
 constexpr int kW4Few = 16;  // tokens
-cudaError_t launch_w4_few(int dtype, const W4LogitsParams& p, cudaStream_t stream);
+// maps: codes in boxes of 128 bytes x 16 rows, scales in boxes of 8 x 16 rows
+cudaError_t launch_w4_few(int dtype, const CUtensorMap& w, const CUtensorMap& s, const W4LogitsParams& p, cudaStream_t stream);
 // `tokens_per_tile`: 32, 64, 128 or 256; maps: codes, h16, h16 for the last token tile, logits (used with tile_stores only).
 cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
                              const CUtensorMap& h_last, const CUtensorMap& out, const W4LogitsParams& p, int grid,
