@@ -55,13 +55,13 @@ bool rows_tmap(CUtensorMap* map, const void* base, CUtensorMapDataType type, int
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Scales: boxes of eight of sixteen rows.
+// Scales: boxes of eight of kW4FewIds rows.
 bool scales_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t spitch) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const cuuint64_t dims[2] = {(cuuint64_t)spitch, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)(spitch * 2)};
-  const cuuint32_t box[2] = {8, 16};
+  const cuuint32_t box[2] = {8, kW4FewIds};
   const cuuint32_t estr[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
@@ -195,11 +195,12 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
   p.h16 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + w4_exponent_bytes(T));
   p.ldh = ldh; p.d = (int)d; p.group = group; p.h16_pitch = (int)h16_pitch;
   p.k_steps = (int)((d + 127) / 128);
+  p.h_vec = vector_rows(h, ldh, DIFR_BF16);
   p.half_last = d - (int64_t)(p.k_steps - 1) * 128 <= 64;
   p.few = T <= kW4Few;
   CUtensorMap tw, th, th_last, tout;
   if (p.few) {
-    if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, 16) || !scales_tmap(&th, W_scales, V, w4_scale_pitch(d, group)))
+    if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, kW4FewIds) || !scales_tmap(&th, W_scales, V, w4_scale_pitch(d, group)))
       return DIFR_ERR_CUDA;
     return launch_w4_few(dtype, tw, th, p, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
   }

@@ -16,7 +16,7 @@
 // Two kernels, by the number of tokens alone; both take the vocabulary as the MMA's M side, read W once per token tile and
 // give the same bits (an MMA adds the same sixteen products in either).
 //
-// Up to 16 tokens, `w4_few`: a warp takes 16 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, three
+// Up to 16 tokens, `w4_few`: a warp takes 32 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, two
 // stages of two steps ahead, and meets nobody.
 //
 // More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
@@ -119,42 +119,60 @@ __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr) {
 // A row of h as fp16 times 2^e, e = 14 - exponent of its largest value, in pairs in the order of k told above, zeros to whole
 // 64; and -10 - e, the token's share of what the epilogue takes back.  A row with a NaN or an infinity is NaN.  For
 // `w4_few` the 16 bytes of a word's four pairs lie together: [block][word][token][lane].
-constexpr int kPrepareThreads = 256;
-__global__ void __launch_bounds__(kPrepareThreads) w4_prepare(const W4LogitsParams p) {
-  __shared__ uint32_t part[kPrepareThreads / 32];
+// One CTA a token, a thread eight values at a time; the second reading finds them in L1.
+constexpr int kPrepareMax = 1024;
+__device__ __forceinline__ void load_eight(uint32_t (&v)[4], const unsigned short* h, int k, int d, bool vec) {
+  if (vec && k + 8 <= d) {
+    const uint4 q = *reinterpret_cast<const uint4*>(h + k);
+    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = (k + 2 * i < d ? h[k + 2 * i] : 0u) | (k + 2 * i + 1 < d ? (uint32_t)h[k + 2 * i + 1] << 16 : 0u);
+  }
+}
+__global__ void __launch_bounds__(kPrepareMax) w4_prepare(const W4LogitsParams p) {
+  __shared__ uint32_t part[kPrepareMax / 32];
   grid_release();
   const int64_t token = blockIdx.x;
   const unsigned short* h = reinterpret_cast<const unsigned short*>(p.h) + token * p.ldh;
-  const int d = p.d;
+  const int d = p.d, eights = p.h16_pitch / 8;
   uint32_t top = 0;  // magnitudes of bf16 compare like their bits, and a NaN's or an infinity's are above every number's
-  for (int k = threadIdx.x; k < d; k += kPrepareThreads) top = max(top, (uint32_t)h[k] & 0x7FFFu);
+  for (int i = threadIdx.x; i < eights; i += blockDim.x) {
+    uint32_t v[4];
+    load_eight(v, h, i * 8, d, p.h_vec);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = max(top, max(v[j] & 0x7FFFu, (v[j] >> 16) & 0x7FFFu));
+  }
   top = __reduce_max_sync(0xffffffffu, top);
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kPrepareThreads / 32; ++w) top = max(top, part[w]);
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) top = max(top, part[w]);
   const bool broken = top >= 0x7F80u;
   const int e = broken || top == 0u ? 0 : 14 - (max((int)(top >> 7), 1) - 127);
   const float f1 = __int_as_float((127 + e / 2) << 23), f2 = __int_as_float((127 + e - e / 2) << 23);  // (|e| <= 141)
   if (threadIdx.x == 0) p.token_exp[token] = -10 - e;
-  __half2* out = reinterpret_cast<__half2*>(p.h16);
-  for (int i = threadIdx.x; i < p.h16_pitch / 2; i += kPrepareThreads) {
-    const int block = i >> 6, in = i & 63;
-    int w, q, t;
-    int64_t to;
-    if (p.few) {
-      q = in & 3; t = (in >> 2) & 3; w = in >> 4;
-      to = ((((int64_t)block * 4 + w) * p.T + token) * 4 + t) * 4 + q;
-    } else {
-      t = in & 3; q = ((in >> 2) & 1) + ((in >> 3) & 1) * 2; w = in >> 4;
-      to = token * (p.h16_pitch / 2) + i;
+  for (int i = threadIdx.x; i < eights; i += blockDim.x) {
+    uint32_t v[4], pair[4];
+    load_eight(v, h, i * 8, d, p.h_vec);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {  // values q and q + 4
+      const uint32_t a = (q & 1) ? v[q >> 1] & 0xFFFF0000u : v[q >> 1] << 16;
+      const uint32_t b = (q & 1) ? v[2 + (q >> 1)] & 0xFFFF0000u : v[2 + (q >> 1)] << 16;
+      __half2 two = __floats2half2_rn(__uint_as_float(a) * f1 * f2, __uint_as_float(b) * f1 * f2);
+      if (broken) two = __half2half2(__ushort_as_half((unsigned short)0x7FFF));
+      pair[q] = *reinterpret_cast<uint32_t*>(&two);
     }
-    const int k = block * 128 + (p.half_last && block == p.k_steps - 1 ? 16 : 32) * t + 8 * w + q;
-    const float a = k < d ? __uint_as_float((uint32_t)h[k] << 16) * f1 * f2 : 0.f;
-    const float b = k + 4 < d ? __uint_as_float((uint32_t)h[k + 4] << 16) * f1 * f2 : 0.f;
-    __half2 two = __floats2half2_rn(a, b);
-    if (broken) two = __half2half2(__ushort_as_half((unsigned short)0x7FFF));
-    out[to] = two;
+    const int block = i >> 4, in = i & 15;
+    const bool half = p.half_last && block == p.k_steps - 1;
+    const int t = half ? in >> 1 : in >> 2, w = half ? in & 1 : in & 3;
+    if (p.few) {
+      reinterpret_cast<uint4*>(p.h16)[(((int64_t)block * 4 + w) * p.T + token) * 4 + t] = make_uint4(pair[0], pair[1], pair[2], pair[3]);
+    } else {
+      uint32_t* to = reinterpret_cast<uint32_t*>(p.h16) + token * (p.h16_pitch / 2) + block * 64 + 16 * w + t;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) to[8 * (q >> 1) + 4 * (q & 1)] = pair[q];
+    }
   }
 }
 
@@ -257,9 +275,9 @@ __device__ __forceinline__ void take_back(uint32_t (&r)[N], int id_exp, int mine
 }
 
 // ------------------------------------------------------------------ up to 16 tokens
-constexpr int kFewWarps = 4, kFewIds = 16;
-constexpr int kFewStages = 3, kFewStageBytes = kFewIds * 128;      // codes of two steps of 16 ids
-constexpr int kFewScaleSlots = 4, kFewScaleBytes = kFewIds * 16;   // eight scales of 16 ids
+constexpr int kFewWarps = 2, kFewIds = kW4FewIds, kFewTiles = kFewIds / 16;
+constexpr int kFewStages = 2, kFewStageBytes = kFewIds * 128;          // codes of two steps
+constexpr int kFewScaleSlots = 4, kFewScaleBytes = kFewIds * 16;       // eight scales of each id
 constexpr int kFewWarpBytes = kFewStages * kFewStageBytes + kFewScaleSlots * kFewScaleBytes;
 constexpr int kFewSmem = kFewWarps * kFewWarpBytes + kFewWarps * kFewStages * 8 + 1024;  // + barriers, alignment
 
@@ -268,11 +286,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint2 ld_shared_8(uint32_t addr) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-  return v;
 }
 __device__ __forceinline__ uint32_t ld_shared_2(uint32_t addr) {
   uint16_t v;
@@ -309,28 +322,32 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
   if (v0 >= p.V) return;  // (nothing below waits for another warp)
 
   const int n_stages = (p.k_steps + 1) / 2;
-  const int per_slot = p.group / 32;  // stages of codes that a slot of scales is for: 4, 2 or 1
+  const int scale_shift = p.group == 128 ? 2 : p.group == 64 ? 1 : 0;  // a scale is for 2^shift chunks of 32 codes
   const uint64_t policy = p.w_once ? l2_policy_evict_first() : l2_policy_evict_normal();
-  auto fetch = [&](int stage) {  // one lane
-    const uint32_t bar = bars + 8u * (uint32_t)(stage % kFewStages);
-    const bool with_scales = stage % per_slot == 0;
-    mbar_arrive_expect_tx(bar, (uint32_t)(kFewStageBytes + (with_scales ? kFewScaleBytes : 0)));
-    tma_load_2d_hint(code_ring + (uint32_t)(stage % kFewStages * kFewStageBytes), &tmap_w, stage * 128, (int)v0, bar, policy);
-    if (with_scales) {
-      const int slot = stage / per_slot;
-      tma_load_2d_hint(scale_ring + (uint32_t)(slot % kFewScaleSlots * kFewScaleBytes), &tmap_s, slot * 8, (int)v0, bar, policy);
+  int next = 0, next_slot = 0;  // stage to fetch, its place
+  auto fetch = [&]() {
+    if (lane == 0) {
+      const uint32_t bar = bars + 8u * (uint32_t)next_slot;
+      // (a slot of eight scales is for 2^shift stages)
+      const int slot = next >> scale_shift;
+      const bool with_scales = slot << scale_shift == next;
+      mbar_arrive_expect_tx(bar, (uint32_t)(kFewStageBytes + (with_scales ? kFewScaleBytes : 0)));
+      tma_load_2d_hint(code_ring + (uint32_t)(next_slot * kFewStageBytes), &tmap_w, next * 128, (int)v0, bar, policy);
+      if (with_scales)
+        tma_load_2d_hint(scale_ring + (uint32_t)(slot % kFewScaleSlots * kFewScaleBytes), &tmap_s, slot * 8, (int)v0, bar, policy);
     }
+    ++next;
+    if (++next_slot == kFewStages) next_slot = 0;
   };
-  if (lane == 0)
-    for (int s = 0; s < kFewStages && s < n_stages; ++s) fetch(s);
+  for (int s = 0; s < kFewStages && s < n_stages; ++s) fetch();
   // ids of this lane's two rows of the MMA: neighbours among the 16 bytes that eight lanes read at once lie in different halves
   // of the swizzled 128-byte lines
   const int at0 = ((g & 1) << 2) | (g >> 1);
   const int64_t spitch = w4_scale_pitch(p.d, p.group);
-  float2 by[2];
-  int id_exp[2];
+  float2 by[2 * kFewTiles];
+  int id_exp[2 * kFewTiles];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < 2 * kFewTiles; ++r) {
     const __nv_bfloat16* scales = p.scales + min(v0 + at0 + 8 * r, (int64_t)p.V - 1) * spitch;
     uint32_t top = fold_row(scales, t, 4, (int)(spitch / 8), 0u);
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -340,45 +357,57 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
   }
   grid_wait();  // h comes from the kernel before
   // [block][word][token][lane]; lanes without a token read another one's, for columns that nobody looks at
-  const uint4* h[NT];
+  const unsigned char* h[NT];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) h[n] = reinterpret_cast<const uint4*>(p.h16) + min(n * 8 + g, p.T - 1) * 4 + t;
-  const int h_word = p.T * 4;
-  float acc[NT][4] = {};
+  for (int n = 0; n < NT; ++n) h[n] = reinterpret_cast<const unsigned char*>(p.h16) + (min(n * 8 + g, p.T - 1) * 4 + t) * 16;
+  const uint32_t h_word = (uint32_t)p.T * 64u;
+  float acc[kFewTiles][NT][4] = {};
   const __half2 minus24 = __float2half2_rn(-24.f);
   const ConvertBits k = convert_bits();
-  // One step: the codes and scales of both ids, and h, of which `words` words are there.
-  auto take = [&](const uint4 c0, const uint4 c1, const uint32_t s0, const uint32_t s1, auto words) {
+  // One step: codes and scales of this lane's ids, and h, of which `words` words are there.
+  auto take = [&](const uint4 (&c)[2 * kFewTiles], const uint32_t (&s)[2 * kFewTiles], auto words) {
     constexpr int W = decltype(words)::value;
     uint4 b[NT][W];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
-      for (int w = 0; w < W; ++w) b[n][w] = h[n][w * h_word];
+      for (int w = 0; w < W; ++w) b[n][w] = *reinterpret_cast<const uint4*>(h[n] + w * h_word);
       h[n] += 4 * h_word;
     }
-    const __half2 scale[2] = {normal_scale(s0, by[0]), normal_scale(s1, by[1])};
-    const __half2 offset[2] = {__hmul2(scale[0], minus24), __hmul2(scale[1], minus24)};
-    const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w};
-    const uint32_t w1[4] = {c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      uint32_t a[4], a8[4];
-      convert_word(w0[w], scale[0], offset[0], k, a);
-      convert_word(w1[w], scale[1], offset[1], k, a8);
+    for (int m = 0; m < kFewTiles; ++m) {
+      const __half2 scale0 = normal_scale(s[2 * m], by[2 * m]), scale1 = normal_scale(s[2 * m + 1], by[2 * m + 1]);
+      const __half2 offset0 = __hmul2(scale0, minus24), offset1 = __hmul2(scale1, minus24);
+      const uint32_t w0[4] = {c[2 * m].x, c[2 * m].y, c[2 * m].z, c[2 * m].w};
+      const uint32_t w1[4] = {c[2 * m + 1].x, c[2 * m + 1].y, c[2 * m + 1].z, c[2 * m + 1].w};
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        mma_f16(acc[n], a[0], a8[0], a[1], a8[1], b[n][w].x, b[n][w].y);
-        mma_f16(acc[n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
+      for (int w = 0; w < W; ++w) {
+        uint32_t a[4], a8[4];
+        convert_word(w0[w], scale0, offset0, k, a);
+        convert_word(w1[w], scale1, offset1, k, a8);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          mma_f16(acc[m][n], a[0], a8[0], a[1], a8[1], b[n][w].x, b[n][w].y);
+          mma_f16(acc[m][n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
+        }
       }
     }
   };
-  // of a stage: the line of this lane's ids, chunk `c` of eight; the scale of chunk c (32 codes)
+  // of a stage: the line of this lane's first id (the others 8 lines further each), 16 bytes for each of eight chunks of 32
+  // codes; of a slot of scales its first id's
   const uint32_t line = code_ring + (uint32_t)(at0 * 128), swizzle = (uint32_t)at0;
-  const int scale_shift = p.group == 128 ? 2 : p.group == 64 ? 1 : 0;
-  auto scale_at = [&](int chunk) {  // of the row
-    const int i = chunk >> scale_shift;
-    return scale_ring + (uint32_t)((i >> 3) % kFewScaleSlots * kFewScaleBytes + (i & 7) * 2 + at0 * 16);
+  const uint32_t scale_line = scale_ring + (uint32_t)(at0 * 16);
+  uint4 c[2 * kFewTiles];
+  uint32_t s[2 * kFewTiles];
+  auto load = [&](uint32_t stage_line, int chunk, uint32_t row_chunk) {
+    const uint32_t x = stage_line + (((uint32_t)chunk ^ swizzle) << 4);
+    const uint32_t i = row_chunk >> scale_shift;
+    const uint32_t y = scale_line + (i >> 3) % kFewScaleSlots * kFewScaleBytes + (i & 7u) * 2u;
+#pragma unroll
+    for (int r = 0; r < 2 * kFewTiles; ++r) {
+      c[r] = ld_shared_16(x + 1024u * (uint32_t)r);
+      s[r] = ld_shared_2(y + 128u * (uint32_t)r);
+    }
   };
   bool ok = true;
   const int whole = (p.k_steps - (p.half_last ? 1 : 0)) / 2;  // stages of two whole steps
@@ -388,14 +417,12 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
     ok = __all_sync(0xffffffffu, mbar_wait_cta(bars + 8u * (uint32_t)slot, phase, false, abort_flag));
     if (!ok) break;
     const uint32_t from = line + (uint32_t)(slot * kFewStageBytes);
-    const uint32_t x0 = from + (((uint32_t)t ^ swizzle) << 4), x1 = from + (((uint32_t)(t + 4) ^ swizzle) << 4);
-    const uint4 c00 = ld_shared_16(x0), c01 = ld_shared_16(x0 + 1024), c10 = ld_shared_16(x1), c11 = ld_shared_16(x1 + 1024);
-    const uint32_t y0 = scale_at(8 * i + t), y1 = scale_at(8 * i + 4 + t);
-    const uint32_t s00 = ld_shared_2(y0), s01 = ld_shared_2(y0 + 128), s10 = ld_shared_2(y1), s11 = ld_shared_2(y1 + 128);
+    load(from, t, (uint32_t)(8 * i + t));
+    take(c, s, std::integral_constant<int, 4>());
+    load(from, t + 4, (uint32_t)(8 * i + 4 + t));
     __syncwarp();
-    if (lane == 0 && i + kFewStages < n_stages) fetch(i + kFewStages);
-    take(c00, c01, s00, s01, std::integral_constant<int, 4>());
-    take(c10, c11, s10, s11, std::integral_constant<int, 4>());
+    if (next < n_stages) fetch();
+    take(c, s, std::integral_constant<int, 4>());
     if (++slot == kFewStages) { slot = 0; phase ^= 1u; }
   }
   if (ok && whole < n_stages) {  // a whole step, a half one, or both
@@ -403,16 +430,20 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
     const uint32_t from = line + (uint32_t)(slot * kFewStageBytes);
     int step = 2 * whole;
     if (ok && step < p.k_steps - (p.half_last ? 1 : 0)) {
-      const uint32_t x = from + (((uint32_t)t ^ swizzle) << 4), y = scale_at(4 * step + t);
-      take(ld_shared_16(x), ld_shared_16(x + 1024), ld_shared_2(y), ld_shared_2(y + 128), std::integral_constant<int, 4>());
+      load(from, t, (uint32_t)(4 * step + t));
+      take(c, s, std::integral_constant<int, 4>());
       ++step;
     }
-    if (ok && step < p.k_steps) {
-      const int chunk = (step & 1) * 4 + (t >> 1);  // of the stage; this lane's half of it
-      const uint32_t x = from + (((uint32_t)chunk ^ swizzle) << 4) + (uint32_t)(t & 1) * 8, y = scale_at(4 * step + (t >> 1));
-      const uint2 c0 = ld_shared_8(x), c1 = ld_shared_8(x + 1024);
-      take(make_uint4(c0.x, c0.y, 0u, 0u), make_uint4(c1.x, c1.y, 0u, 0u), ld_shared_2(y), ld_shared_2(y + 128),
-           std::integral_constant<int, 2>());
+    if (ok && step < p.k_steps) {  // lanes t and t + 1 share a chunk, eight bytes each
+      load(from, (step & 1) * 4 + (t >> 1), (uint32_t)(4 * step + (t >> 1)));
+      if (t & 1) {
+#pragma unroll
+        for (int r = 0; r < 2 * kFewTiles; ++r) {
+          c[r].x = c[r].z;
+          c[r].y = c[r].w;
+        }
+      }
+      take(c, s, std::integral_constant<int, 2>());
     }
   }
   if (!ok) {  // a wait ran out: what was not computed is NaN; copies in flight get time to land
@@ -423,13 +454,18 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int token = n * 8 + 2 * t + (j & 1);
-      const int64_t v = v0 + at0 + (j >> 1) * 8;
-      const float value = ok ? acc[n][j] : __int_as_float(0x7FC00000);
-      if (token < p.T && v < p.V)
-        static_cast<OUT*>(p.logits)[(int64_t)token * p.ld + v] =
-            from_float<OUT>(times_power(value, id_exp[j >> 1] + p.token_exp[token]));
+    for (int j = 0; j < 2; ++j) {
+      const int token = n * 8 + 2 * t + j;
+      if (token < p.T) {
+        const int token_exp = p.token_exp[token];
+        OUT* out = static_cast<OUT*>(p.logits) + (int64_t)token * p.ld;
+#pragma unroll
+        for (int r = 0; r < 2 * kFewTiles; ++r) {
+          const int64_t v = v0 + at0 + 8 * r;
+          const float value = ok ? acc[r >> 1][n][2 * (r & 1) + j] : __int_as_float(0x7FC00000);
+          if (v < p.V) out[v] = from_float<OUT>(times_power(value, id_exp[r] + token_exp));
+        }
+      }
     }
 }
 
@@ -829,7 +865,8 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
 template <typename... P, typename... A>
 static cudaError_t launch_after_prepare(const W4LogitsParams& p, void (*kernel)(P...), int grid, int threads, int smem,
                                         cudaStream_t stream, const A&... args) {
-  w4_prepare<<<p.T, kPrepareThreads, 0, stream>>>(p);
+  const int eights = p.h16_pitch / 8;
+  w4_prepare<<<p.T, eights >= kPrepareMax ? kPrepareMax : (eights + 31) / 32 * 32, 0, stream>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg;

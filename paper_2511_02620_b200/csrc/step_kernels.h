@@ -49,11 +49,13 @@ struct W4LogitsParams : LogitTiles {
   int64_t ldh;
   int d, group, h16_pitch;
   int k_steps;             // of 128 values
+  bool h_vec;              // h's rows start on 16-byte boundaries
   bool half_last;          // the last one has 64 at most
   bool few;                // launch_w4_few: only the sizes, buffers and strides of the tiles' part are used
 };
-constexpr int kW4Few = 16;  // tokens
-// maps: codes in boxes of 128 bytes x 16 rows, scales in boxes of 8 x 16 rows
+constexpr int kW4Few = 16;     // tokens
+constexpr int kW4FewIds = 32;  // ids of a warp
+// maps: codes in boxes of 128 bytes x kW4FewIds rows, scales in boxes of 8 x kW4FewIds rows
 cudaError_t launch_w4_few(int dtype, const CUtensorMap& w, const CUtensorMap& s, const W4LogitsParams& p, cudaStream_t stream);
 // `tokens_per_tile`: 32, 64, 128 or 256; maps: codes, h16, h16 for the last token tile, logits (used with tile_stores only).
 cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
