@@ -241,15 +241,20 @@ __device__ __forceinline__ ConvertBits convert_bits() {
   asm volatile("mov.b32 %0, 0x4E004E00;" : "=r"(b.magic));
   return b;
 }
-__device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 offset, ConvertBits k, uint32_t* out) {
-  const uint32_t at[4] = {w * 64u, w * 4u, w >> 2, w >> 6};
+// Pairs 2 e and 2 e + 1 of a word.
+__device__ __forceinline__ void convert_half(uint32_t w, int e, __half2 scale, __half2 offset, ConvertBits k, uint32_t* out) {
+  const uint32_t at[2] = {e == 0 ? w * 64u : w >> 2, e == 0 ? w * 4u : w >> 6};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     uint32_t bits;
     asm("lop3.b32 %0, %1, %2, %3, 0x6A;" : "=r"(bits) : "r"(at[i]), "r"(k.mask), "r"(k.magic));  // (a & b) ^ c
     const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&bits), scale, offset);
     out[i] = *reinterpret_cast<const uint32_t*>(&v);
   }
+}
+__device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 offset, ConvertBits k, uint32_t* out) {
+  convert_half(w, 0, scale, offset, k, out);
+  convert_half(w, 1, scale, offset, k, out + 2);
 }
 
 // x times 2^e, e from -276 to 230: three factors where one does not do, the rounding of the last to a subnormal apart exact.
@@ -346,14 +351,21 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
   const int64_t spitch = w4_scale_pitch(p.d, p.group);
   float2 by[2 * kFewTiles];
   int id_exp[2 * kFewTiles];
+  {
+    const int n8 = (int)(spitch / 8);
+    auto scale_row = [&](int r) { return p.scales + min(v0 + at0 + 8 * r, (int64_t)p.V - 1) * spitch; };
+    uint4 some[2 * kFewTiles];  // (all rows' first loads before the first is looked at)
 #pragma unroll
-  for (int r = 0; r < 2 * kFewTiles; ++r) {
-    const __nv_bfloat16* scales = p.scales + min(v0 + at0 + 8 * r, (int64_t)p.V - 1) * spitch;
-    uint32_t top = fold_row(scales, t, 4, (int)(spitch / 8), 0u);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    id_exp[r] = scale_exponent(top);
-    by[r] = scale_factors(id_exp[r]);
+    for (int r = 0; r < 2 * kFewTiles; ++r)
+      some[r] = t < n8 ? __ldg(reinterpret_cast<const uint4*>(scale_row(r)) + t) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int r = 0; r < 2 * kFewTiles; ++r) {
+      uint32_t top = fold_row(scale_row(r), t + 4, 4, n8, fold_scales(some[r], 0u));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      id_exp[r] = scale_exponent(top);
+      by[r] = scale_factors(id_exp[r]);
+    }
   }
   grid_wait();  // h comes from the kernel before
   // [block][word][token][lane]; lanes without a token read another one's, for columns that nobody looks at
