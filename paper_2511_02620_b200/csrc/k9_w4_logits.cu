@@ -51,7 +51,6 @@ constexpr int kW4TmemCols = 512;
 constexpr int kW4Step = 128;        // values of k
 constexpr int kW4SlotCols = 64;     // of a step: 128 fp16 a lane
 constexpr int kW4CodeBytes = 128 * 128;  // a stage of codes: two steps of 128 ids
-constexpr int kW4Ring = 8;          // barriers of steps
 
 template <int BN>
 struct W4Tile {
@@ -61,7 +60,7 @@ struct W4Tile {
   static constexpr int bar_bytes = 1024;
   static constexpr int out_buffers = BN == 256 ? 3 : 0;
   static constexpr int out_bytes = 2 * out_buffers * kLogitOutBytes;
-  static constexpr int h_stages = BN == 256 ? 4 : 8;
+  static constexpr int h_stages = BN == 256 ? 4 : BN == 128 ? 5 : BN == 64 ? 6 : 8;
   static constexpr int fit = (227 * 1024 - 1024 - bar_bytes - out_bytes - h_stages * h_bytes) / kW4CodeBytes;
   static constexpr int c_stages = fit > 12 ? 12 : fit;
   static constexpr int smem_bytes = h_stages * h_bytes + c_stages * kW4CodeBytes + out_bytes + bar_bytes + 1024;
@@ -76,7 +75,7 @@ struct W4Tile {
   static constexpr int chunks = BN / chunk;
   static constexpr int shared_loads = shared_cols / (2 * chunk);
   static_assert(c_stages >= 3 && slots >= 2, "pipeline depth");
-  static_assert(slots <= kW4Ring && h_stages <= kW4Ring, "a step's barriers are waited for before their next turn");
+  static_assert((slots & (slots - 1)) == 0, "steps are counted modulo 2^32");
 };
 
 // Instruction descriptor: dense, fp32 accumulator, fp16 A and B, both K-major.
@@ -109,6 +108,10 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// An arrival that publishes no memory of this thread.  (A releasing one waits for every load that the thread has under way.)
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar_cluster_addr) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+}
 __device__ __forceinline__ uint4 ld_shared_16(uint32_t addr) {
   uint4 v;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
@@ -494,24 +497,26 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   uint8_t* smem = smem_raw + (smem_base - raw_addr);
 
   // Both CTAs of a pair lay out their barriers at the same offsets.
-  //   full[g % 8]  of step g, first CTA's copy is used: 1 arrival (its producer of h) + the bytes of both CTAs' loads, one
-  //                arrival per conversion warp of the step, of both CTAs
-  //   done[g % 8]  of step g, each CTA's own copy: 1 arrival, the commit of its MMAs, delivered to both
-  //   c_full[s]    own: 1 arrival + the bytes of the CTA's codes;  c_empty[s] own: one arrival per conversion warp
+  //   h_full[s]   first CTA's copy is used: 1 arrival (its producer) + the bytes of both CTAs' loads
+  //   h_empty[s]  each CTA's own copy: 1 arrival, the commit of the MMAs that read the stage, delivered to both
+  //   c_full[s]   own: 1 arrival + the bytes of the CTA's codes;  c_empty[s] own: one arrival per conversion warp
+  //   a_full[s]   first CTA's copy is used: one arrival per conversion warp of the step, of both CTAs
+  //   a_empty[s]  each CTA's own copy: the commit of the MMAs that read the slot, delivered to both
   //   acc_full[a], acc_free[a]  as in the microscaled product
-  constexpr int HS = Tl::h_stages, CS = Tl::c_stages, AS = Tl::slots, R = kW4Ring;
+  constexpr int HS = Tl::h_stages, CS = Tl::c_stages, AS = Tl::slots;
   const uint32_t h_base = smem_base, c_base = smem_base + HS * Tl::h_bytes;
   uint8_t* out_pieces = smem + HS * Tl::h_bytes + CS * kW4CodeBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(out_pieces + Tl::out_bytes);
   const uint32_t bar0 = smem_u32(bars);
-  auto full = [&](uint32_t g) { return bar0 + 8u * (g % R); };
-  auto done = [&](uint32_t g) { return bar0 + 8u * (R + g % R); };
-  auto turn = [&](uint32_t g) { return (g / R) & 1u; };  // phase of a step's barriers
-  auto c_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * R + s); };
-  auto c_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * R + CS + s); };
-  auto acc_full = [&](int a) { return bar0 + 8u * (uint32_t)(2 * R + 2 * CS + a); };
-  auto acc_free = [&](int a) { return bar0 + 8u * (uint32_t)(2 * R + 2 * CS + 2 + a); };
-  constexpr int kBars = 2 * R + 2 * CS + 4;
+  auto h_full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+  auto h_empty = [&](int s) { return bar0 + 8u * (uint32_t)(HS + s); };
+  auto c_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + s); };
+  auto c_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + CS + s); };
+  auto a_full = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + s); };
+  auto a_empty = [&](int s) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + AS + s); };
+  auto acc_full = [&](int a) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + 2 * AS + a); };
+  auto acc_free = [&](int a) { return bar0 + 8u * (uint32_t)(2 * HS + 2 * CS + 2 * AS + 2 + a); };
+  constexpr int kBars = 2 * HS + 2 * CS + 2 * AS + 4;
   static_assert(kBars * 8 + 8 <= Tl::bar_bytes, "barrier block");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -523,13 +528,17 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   const int n_pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
-    for (uint32_t g = 0; g < R; ++g) {
-      mbar_init(full(g), 1 + kW4CvtWarps);
-      mbar_init(done(g), 1);
+    for (int s = 0; s < HS; ++s) {
+      mbar_init(h_full(s), 1);
+      mbar_init(h_empty(s), 1);
     }
     for (int s = 0; s < CS; ++s) {
       mbar_init(c_full(s), 1);
       mbar_init(c_empty(s), kW4CvtWarps);
+    }
+    for (int s = 0; s < AS; ++s) {
+      mbar_init(a_full(s), kW4CvtWarps);  // four warps of a step, of two CTAs
+      mbar_init(a_empty(s), 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full(a), 1);
@@ -561,8 +570,9 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     // ------------------------------------------------------------ TMA of h
     grid_wait();
     const uint64_t keep = l2_policy_evict_last();
-    const uint32_t full0_base = map_to_cta(full(0), 0);
-    uint32_t g = 0;  // step
+    const uint32_t full0_base = map_to_cta(h_full(0), 0);
+    int stage = 0;
+    uint32_t phase = 0;
     bool ok = true;
     int vt, tt;
     while (ok && walk.next(vt, tt)) {
@@ -570,17 +580,18 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int half = last ? p.last_tokens / 2 : BN / 2;
       const void* tmap_tokens = last ? &tmap_h_last : &tmap_h;
       const int h_row = tt * BN + (int)cta * half;
-      for (int k = 0; k < p.k_steps; ++k, ++g) {
-        if (g >= HS && !__all_sync(0xffffffffu, mbar_wait(done(g - HS), turn(g - HS), abort_flag))) { ok = false; break; }
+      for (int k = 0; k < p.k_steps; ++k) {
+        if (!__all_sync(0xffffffffu, mbar_wait(h_empty(stage), phase ^ 1u, abort_flag))) { ok = false; break; }
         if (elect_one()) {
           // (the second box of the last step may lie behind the row: it reads zeros)
-          if (cta == 0) mbar_arrive_expect_tx(full(g), 2u * 2u * (uint32_t)half * 128u);
-          const uint32_t full0 = full0_base + 8u * (g % R);
-          const uint32_t dst = h_base + (g % HS) * (uint32_t)Tl::h_bytes;
+          if (cta == 0) mbar_arrive_expect_tx(h_full(stage), 2u * 2u * (uint32_t)half * 128u);
+          const uint32_t full0 = full0_base + 8u * (uint32_t)stage;
+          const uint32_t dst = h_base + (uint32_t)(stage * Tl::h_bytes);
           tma_load_2d_pair(dst, tmap_tokens, k * kW4Step, h_row, full0, keep);
           tma_load_2d_pair(dst + Tl::h_box, tmap_tokens, k * kW4Step + 64, h_row, full0, keep);
         }
         __syncwarp();
+        if (++stage == HS) { stage = 0; phase ^= 1u; }
       }
     }
   } else if (warp == 3) {
@@ -609,9 +620,8 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     if (cta == 0) {
       const uint64_t desc0 = umma_desc_k_major_sw128(h_base);
       const uint32_t desc_hi = (uint32_t)(desc0 >> 32), desc_lo0 = (uint32_t)desc0;
-      int acc = 0;
-      uint32_t g = 0, n_tile = 0;
-      bool seen = false;
+      int stage = 0, slot = 0, acc = 0;
+      uint32_t phase = 0, slot_phase = 0, n_tile = 0;
       bool ok = true;
       int vt, tt;
       for (; ok && walk.next(vt, tt); ++n_tile) {
@@ -631,31 +641,31 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
         }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * Tl::acc_stride);
+        // (a last token tile narrower than the others has its boxes closer together in the stage all the same)
         uint32_t accumulate = 0;
-        for (int k = 0; k < p.k_steps; ++k, ++g) {
-          if (!__all_sync(0xffffffffu, mbar_wait_cta(full(g), turn(g), seen, abort_flag))) { ok = false; break; }
-          // a look at the next step: its answer is there by the time it is needed
-          seen = mbar_peek_cta(full(g + 1), turn(g + 1));
+        for (int k = 0; k < p.k_steps; ++k) {
+          if (!__all_sync(0xffffffffu, mbar_wait(h_full(stage), phase, abort_flag))) { ok = false; break; }
+          if (!__all_sync(0xffffffffu, mbar_wait(a_full(slot), slot_phase, abort_flag))) { ok = false; break; }
           tc_fence_after();
-          const uint32_t b_lo = desc_lo0 + (((g % HS) * (uint32_t)Tl::h_bytes) >> 4);
-          const uint32_t a_tmem = tmem_base + (uint32_t)Tl::slot_col0 + (g % AS) * kW4SlotCols;
-          const bool whole = !p.half_last || k + 1 < p.k_steps;
+          const int n_mma = p.half_last && k + 1 == p.k_steps ? 4 : 8;
+          const uint32_t b_lo = desc_lo0 + ((uint32_t)(stage * Tl::h_bytes) >> 4);
+          const uint32_t a_tmem = tmem_base + (uint32_t)(Tl::slot_col0 + slot * kW4SlotCols);
           if (elect_one()) {
-            // (a narrow last token tile has its second box at the same place)
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk, ((uint64_t)desc_hi << 32) | (b_lo + 2u * (uint32_t)kk), idesc,
-                                 kk == 0 ? accumulate : 1u);
-            if (whole) {
-#pragma unroll
-              for (int kk = 4; kk < 8; ++kk)
-                umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk,
-                                   ((uint64_t)desc_hi << 32) | (b_lo + (Tl::h_box >> 4) + 2u * (uint32_t)(kk & 3)), idesc, 1u);
+            for (int kk = 0; kk < kW4Step / 16; ++kk) {
+              if (kk < n_mma) {
+                const uint64_t b_desc =
+                    ((uint64_t)desc_hi << 32) | (b_lo + (uint32_t)(kk >> 2) * (Tl::h_box >> 4) + 2u * (uint32_t)(kk & 3));
+                umma_f16_tmem_pair(d_tmem, a_tmem + 8u * (uint32_t)kk, b_desc, idesc, kk == 0 ? accumulate : 1u);
+              }
             }
-            umma_commit_pair(done(g), 3);
+            umma_commit_pair(h_empty(stage), 3);
+            umma_commit_pair(a_empty(slot), 3);
           }
           __syncwarp();
           accumulate = 1;
+          if (++stage == HS) { stage = 0; phase ^= 1u; }
+          if (++slot == AS) { slot = 0; slot_phase ^= 1u; }
         }
         if (ok && elect_one()) umma_commit_pair(acc_full(acc), 3);
         __syncwarp();
@@ -669,102 +679,78 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
     const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
     const int r = quarter * 32 + lane;  // row of the CTA's 128
     const uint32_t row_smem = c_base + (uint32_t)r * 128u, swizzle = (uint32_t)(r & 7);
-    const uint32_t full0_base = map_to_cta(full(0), 0);
+    const uint32_t full0_base = map_to_cta(a_full(0), 0);
     const int64_t spitch = w4_scale_pitch(p.d, p.group);
-    const int n8 = (int)(spitch / 8);
     const __half2 minus24 = __float2half2_rn(-24.f);
     const ConvertBits bits = convert_bits();
     int stage = 0;
     uint32_t phase = 0, step0 = 0;  // steps of the tiles before
-    uint4 c[4];
-    // this thread's codes of the next stage, one ahead of the conversion
-    auto fetch = [&]() {
-      if (!__all_sync(0xffffffffu, mbar_wait_cta(c_full(stage), phase, false, abort_flag))) return false;
-      const uint32_t from = row_smem + (uint32_t)(stage * kW4CodeBytes);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(odd * 4 + j)) ^ swizzle) << 4));
-      __syncwarp();
-      if (lane == 0) mbar_arrive(c_empty(stage));
-      if (++stage == CS) { stage = 0; phase ^= 1u; }
-      return true;
-    };
-    auto scales_of = [&](int vt) {
-      return p.scales + (int64_t)min(vt * kLogitPairM + (int)cta * 128 + r, p.V - 1) * spitch;
-    };
+    bool ok = true;
     int vt, tt;
-    bool more = walk.next(vt, tt), ok = true;
-    const __nv_bfloat16 *scales = nullptr, *next_scales = nullptr;
-    uint32_t top = 0;
-    uint2 raw = make_uint2(0u, 0u);
-    if (more) {
-      scales = scales_of(vt);
-      if (odd < p.k_steps) raw = load_step_scales(scales, odd, p.group);
-      top = fold_row(scales, 0, 1, n8, 0u);
-      ok = fetch();
-    }
-    while (more && ok) {
-      const float2 by = scale_factors(scale_exponent(top));
-      more = walk.next(vt, tt);
-      next_scales = more ? scales_of(vt) : scales;
-      // the next tile's largest scale, eight scales a stage of codes: there are no more of them than stages
-      uint4 some = make_uint4(0u, 0u, 0u, 0u);
-      top = 0u;
+    while (ok && walk.next(vt, tt)) {
+      const int v = min(vt * kLogitPairM + (int)cta * 128 + r, p.V - 1);
+      const __nv_bfloat16* scales = p.scales + (int64_t)v * spitch;
+      const float2 by = scale_factors(scale_exponent(fold_row(scales, 0, 1, (int)(spitch / 8), 0u)));
+      uint2 raw = odd < p.k_steps ? load_step_scales(scales, odd, p.group) : make_uint2(0u, 0u);
       for (int k = 0; k < c_steps; ++k) {
         const int step = 2 * k + odd;
-        const bool mine = step < p.k_steps, half_step = p.half_last && step == p.k_steps - 1;
-        top = fold_scales(some, top);
-        if (k < n8) some = __ldg(reinterpret_cast<const uint4*>(next_scales) + k);
-        const uint32_t g = step0 + (uint32_t)step;
-        const uint32_t to = tmem_base + lane_addr + (uint32_t)Tl::slot_col0 + (g % AS) * kW4SlotCols;
-        uint32_t out[32];
-        __half2 s[4], off[4];
-        auto convert = [&](int half) {  // words 2 half and 2 half + 1 of the four chunks
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(c_full(stage), phase, false, abort_flag))) { ok = false; break; }
+        if (step < p.k_steps) {
+          const uint32_t from = row_smem + (uint32_t)(stage * kW4CodeBytes);
+          uint4 c[4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              uint32_t four[4];
-              convert_word(half == 0 ? (w == 0 ? c[t].x : c[t].y) : (w == 0 ? c[t].z : c[t].w), s[t], off[t], bits, four);
-#pragma unroll
-              for (int q = 0; q < 4; ++q) out[8 * (2 * w + (q >> 1)) + 4 * (q & 1) + t] = four[q];
-            }
-          }
-        };
-        if (mine) {
+          for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(odd * 4 + j)) ^ swizzle) << 4));
+          const bool half_step = p.half_last && step == p.k_steps - 1;
           uint2 here = spread_step_scales(raw, p.group);
+          if (step + 2 < p.k_steps) raw = load_step_scales(scales, step + 2, p.group);
           if (half_step) {  // lane t of mma.sync: the 16 codes at 16 t
             here = make_uint2(__byte_perm(here.x, 0, 0x1010), __byte_perm(here.x, 0, 0x3232));
             c[3].x = c[1].z; c[3].y = c[1].w;
             c[2].x = c[1].x; c[2].y = c[1].y;
             c[1].x = c[0].z; c[1].y = c[0].w;
           }
-          const bool in_tile = step + 2 < p.k_steps;
-          if (in_tile || (more && odd < p.k_steps))
-            raw = load_step_scales(in_tile ? scales : next_scales, in_tile ? step + 2 : odd, p.group);
+          __half2 s[4], off[4];
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const uint32_t two = t < 2 ? here.x : here.y;
             s[t] = normal_scale((t & 1) == 0 ? two : two >> 16, by);
             off[t] = __hmul2(s[t], minus24);
           }
-          convert(0);
-          if (g >= AS && !__all_sync(0xffffffffu, mbar_wait_cta(done(g - AS), turn(g - AS), false, abort_flag))) { ok = false; break; }
-          tc_fence_after();
-          tmem_st_32x32(to, out);
-          if (!half_step) convert(1);
-        }
-        if ((k + 1 < c_steps || more) && !fetch()) { ok = false; break; }
-        if (mine) {
-          if (!half_step) tmem_st_32x32(to + 32u, out);
+          const uint32_t g = step0 + (uint32_t)step;
+          const uint32_t slot = g % (uint32_t)AS, slot_phase = (g / (uint32_t)AS) & 1u;
+          const uint32_t to = tmem_base + lane_addr + (uint32_t)Tl::slot_col0 + slot * kW4SlotCols;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {  // words 2 half and 2 half + 1 of the four chunks
+            uint32_t out[32];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+#pragma unroll
+              for (int w = 0; w < 2; ++w) {
+                uint32_t four[4];
+                convert_word(half == 0 ? (w == 0 ? c[t].x : c[t].y) : (w == 0 ? c[t].z : c[t].w), s[t], off[t], bits, four);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) out[8 * (2 * w + (q >> 1)) + 4 * (q & 1) + t] = four[q];
+              }
+            }
+            if (half == 0) {
+              if (!__all_sync(0xffffffffu, mbar_wait_cta(a_empty((int)slot), slot_phase ^ 1u, false, abort_flag))) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+            }
+            tmem_st_32x32(to + 32u * (uint32_t)half, out);  // (the second half of a half step: columns that no MMA reads)
+          }
+          if (!ok) break;
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive_cluster_nofence(full0_base + 8u * (g % R));  // (TMEM writes are ordered by the fence above)
+          if (lane == 0) mbar_arrive_cluster_relaxed(full0_base + 8u * slot);  // (TMEM writes are ordered by the fence above)
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(c_empty(stage));
+        if (++stage == CS) { stage = 0; phase ^= 1u; }
       }
-      top = fold_scales(some, top);
-      if (ok && c_steps < n8) top = fold_row(next_scales, c_steps, 1, n8, top);
-      scales = next_scales;
       step0 += (uint32_t)p.k_steps;
     }
   } else if (warp >= kW4EpiWarp0) {
