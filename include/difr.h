@@ -583,7 +583,7 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
  *   r = max(p_m - q_m, 0), or p_m where that is zero everywhere, or p of the last row where none was refused
  *
  * so that the tokens are distributed as the target's.  A filter is applied by the caller: ids at -infinity have no
- * probability.  What decides is computed in fp64; p_draft is within 2^-16 of the definition's, relative.  Two kernels.
+ * probability.  What decides is computed in fp64; p_draft is within 2^-16 of the definition's, relative.
  */
 typedef struct {
   const void* logits;           /* [n_drafts + B, V] of type `dtype`, row stride ld >= V elements */

@@ -217,7 +217,7 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
 
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {
   if (B < 1 || n_drafts < 0 || V < 1 || B > kMaxRows || n_drafts > kMaxRows || !verify_supported(B, n_drafts, V)) return 0;
-  return (size_t)(n_drafts + B) * (size_t)verify_chunks(V, 4) * sizeof(float4);
+  return ((size_t)(n_drafts + B) * (size_t)verify_chunks(V, 4) + (size_t)B) * sizeof(float4);
 }
 
 difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_drafts, int64_t V, const difr_drafts_out* out,
@@ -240,7 +240,7 @@ difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_draft
   VerifyParams p;
   memset(&p, 0, sizeof p);
   p.chunks = (int)verify_chunks(V, elem_bytes(in->dtype));
-  if (!out->workspace || out->workspace_bytes < (size_t)(n_drafts + B) * (size_t)p.chunks * sizeof(float4))
+  if (!out->workspace || out->workspace_bytes < difr_verify_workspace_bytes(B, n_drafts, V))
     return DIFR_ERR_WORKSPACE;
   int pairs = 0;
   const difr_status ds = device_pairs(&pairs);
@@ -249,7 +249,8 @@ difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_draft
   p.accept_words = in->accept_words; p.sample_words = in->sample_words;
   p.temperatures = in->temperatures; p.temperature = in->temperature;
   p.tokens = out->tokens; p.n_accepted = out->n_accepted; p.p_draft = out->p_draft; p.status = out->status;
-  p.records = static_cast<float4*>(out->workspace);
+  p.picks = static_cast<float4*>(out->workspace);
+  p.records = p.picks + B;
   p.ld = in->ld; p.ld_probs = in->ld_draft;
   p.B = (int)B; p.n_drafts = (int)n_drafts; p.V = (int)V; p.max_drafts = in->max_drafts;
   return launch_verify_drafts(p, in->dtype, reinterpret_cast<cudaStream_t>(stream)) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;

@@ -5,25 +5,25 @@
 //   the next token is the first id i with sum over k <= i of r(k) > nu sum of r,
 //   r = max(p_m - q_m, 0) (p_m itself where that is zero everywhere), or p_n where nothing was refused
 //
-// Two kernels.  `draft_rows` reads every row once, a CTA a chunk of it, and leaves (largest logit, its first id, sum of
-// exponentials) per chunk in fp32: bound by the logits' bytes.  `draft_decide`, a cluster of CTAs per request, joins the
-// records, walks the drafts, and samples the row it ends at: ids are split into contiguous ranges of CTAs and warps, sums
-// are taken in fp64 and the warp whose range holds the target sum walks it once more.  Whole numbers hang on these
-// comparisons, so what decides is in fp64: exponentials of the sampled row, and the row sum of a draft whose acceptance lies
-// within fp32's error of the border, which the cluster then takes again.
-#include <cooperative_groups.h>
+// Five kernels.  `draft_rows` reads every row once, a CTA a chunk of it, and leaves (largest logit, sum of exponentials, first
+// id of the largest) per chunk in fp32: bound by the logits' bytes.  `draft_merge`, a CTA a request, joins the records and
+// walks the drafts.  Of the row a request ends at `draft_sums` takes the sums of chunks of ids, of the exponentials first where a
+// residual needs the row's sum before it can be added up, and `draft_pick` finds the token in the chunk that holds the target.
+// Whole numbers hang on these comparisons, so what decides is in fp64: exponentials of the sampled row, and the row sum of a
+// draft whose acceptance lies within fp32's error of the border, which `draft_merge` then takes again.  (As one kernel with a
+// cluster of CTAs a request, the sampling spent its time at the clusters' barriers: 151 us and more for 192 requests of 151936
+// ids.)
 #include <cuda_runtime.h>
 #include <string.h>
 
 #include "mx_device.cuh"
 #include "step_kernels.h"
 
-namespace cg = cooperative_groups;
-
 namespace difr {
 
 constexpr int kRowThreads = 256, kRowVecs = kVerifyChunkVecs / kRowThreads;
-constexpr int kDecideThreads = 512, kDecideWarps = kDecideThreads / 32;
+constexpr int kMergeThreads = 256;
+constexpr int kSumThreads = 256, kSumWarps = kSumThreads / 32, kSumIds = 8192;  // ids of a chunk of sums
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 // Relative error allowed for a row sum from fp32 terms: an exponent is off by 2^-23 times itself (terms beyond 2^-40 of the
 // sum do not count), ex2 by 2^-22, sums of 1024 vectors by a few 2^-24: under 2^-17 in all.
@@ -46,16 +46,57 @@ __device__ __forceinline__ int request_of_row(const int32_t* offsets, int B, int
   return lo;
 }
 
+// Sixteen bytes of logits as they lie in memory: a thread keeps four of them, unpacked where they are used, so that 2048
+// threads fit an SM.
 template <typename X>
-struct LogitVec {
-  static constexpr int n = 16 / (int)sizeof(X);
-  X e[n];
+struct LogitVec;
+template <>
+struct LogitVec<float> {
+  static constexpr int n = 4;
+  static constexpr uint32_t none = 0xFF800000u;  // -infinity
+  static __device__ __forceinline__ float get(const uint4& q, int i) {
+    return __uint_as_float(i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w);
+  }
+  static __device__ __forceinline__ float largest(const uint4& q) {
+    return max_nan(max_nan(get(q, 0), get(q, 1)), max_nan(get(q, 2), get(q, 3)));
+  }
+};
+template <typename H2>
+__device__ __forceinline__ H2 as_pair(uint32_t w) { return *reinterpret_cast<const H2*>(&w); }
+__device__ __forceinline__ uint32_t vec_word(const uint4& q, int i) { return i == 0 ? q.x : i == 1 ? q.y : i == 2 ? q.z : q.w; }
+template <>
+struct LogitVec<__nv_bfloat16> {
+  static constexpr int n = 8;
+  static constexpr uint32_t none = 0xFF80FF80u;
+  static __device__ __forceinline__ float get(const uint4& q, int i) {
+    const uint32_t w = vec_word(q, i >> 1);
+    return __uint_as_float((i & 1) ? w & 0xFFFF0000u : w << 16);
+  }
+  static __device__ __forceinline__ float largest(const uint4& q) {
+    using H2 = __nv_bfloat162;
+    const H2 m = __hmax2_nan(__hmax2_nan(as_pair<H2>(q.x), as_pair<H2>(q.y)), __hmax2_nan(as_pair<H2>(q.z), as_pair<H2>(q.w)));
+    return max_nan(__low2float(m), __high2float(m));
+  }
+};
+template <>
+struct LogitVec<__half> {
+  static constexpr int n = 8;
+  static constexpr uint32_t none = 0xFC00FC00u;
+  static __device__ __forceinline__ float get(const uint4& q, int i) {
+    const __half2 h = as_pair<__half2>(vec_word(q, i >> 1));
+    return (i & 1) ? __high2float(h) : __low2float(h);
+  }
+  static __device__ __forceinline__ float largest(const uint4& q) {
+    using H2 = __half2;
+    const H2 m = __hmax2_nan(__hmax2_nan(as_pair<H2>(q.x), as_pair<H2>(q.y)), __hmax2_nan(as_pair<H2>(q.z), as_pair<H2>(q.w)));
+    return max_nan(__low2float(m), __high2float(m));
+  }
 };
 
 template <typename X>
-__global__ void __launch_bounds__(kRowThreads) draft_rows(const VerifyParams p) {
-  using V16 = LogitVec<X>;
-  constexpr int N = V16::n;
+__global__ void __launch_bounds__(kRowThreads, 8) draft_rows(const VerifyParams p) {
+  using L = LogitVec<X>;
+  constexpr int N = L::n;
   __shared__ float2 part[kRowThreads / 32];
   __shared__ int part_id[kRowThreads / 32];
   const int64_t row = blockIdx.x;
@@ -63,40 +104,51 @@ __global__ void __launch_bounds__(kRowThreads) draft_rows(const VerifyParams p) 
   const X* l = static_cast<const X*>(p.logits) + row * p.ld;
   // vectors lie on 16-byte boundaries of memory: the first one of a row may begin before it
   const int before = (int)((reinterpret_cast<uintptr_t>(l) & 15u) / sizeof(X));
-  float v[kRowVecs][N];
+  const int first = chunk * kVerifyChunkVecs * N + (int)threadIdx.x * N - before;  // of this thread; kRowThreads N further each
+  uint4 v[kRowVecs];
   const float none = __int_as_float(0xFF800000);
 #pragma unroll
   for (int k = 0; k < kRowVecs; ++k) {
-    const int64_t at = ((int64_t)chunk * kRowVecs + k) * kRowThreads + threadIdx.x;
-    const int64_t e0 = at * N - before;
+    const int e0 = first + k * kRowThreads * N;
     if (e0 >= 0 && e0 + N <= p.V) {
-      const uint4 raw = __ldg(reinterpret_cast<const uint4*>(l + e0));
-      const V16 vec = *reinterpret_cast<const V16*>(&raw);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[k][i] = (float)vec.e[i];
+      v[k] = __ldg(reinterpret_cast<const uint4*>(l + e0));
     } else {
+      uint32_t w[4] = {L::none, L::none, L::none, L::none};
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[k][i] = e0 + i >= 0 && e0 + i < p.V ? (float)l[e0 + i] : none;
+      for (int i = 0; i < N; ++i) {
+        if (e0 + i < 0 || e0 + i >= p.V) continue;
+        if constexpr (sizeof(X) == 4) {
+          w[i] = reinterpret_cast<const uint32_t*>(l)[e0 + i];
+        } else {
+          const uint32_t one = reinterpret_cast<const uint16_t*>(l)[e0 + i];
+          w[i >> 1] = (i & 1) ? (w[i >> 1] & 0xFFFFu) | one << 16 : (w[i >> 1] & 0xFFFF0000u) | one;
+        }
+      }
+      v[k] = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
   float temperature = p.temperature;
   if (p.temperatures != nullptr) temperature = p.temperatures[request_of_row(p.offsets, p.B, row)];
-  float m = none;
+  float m = L::largest(v[0]);
 #pragma unroll
-  for (int k = 0; k < kRowVecs; ++k)
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = max_nan(m, v[k][i]);
+  for (int k = 1; k < kRowVecs; ++k) m = max_nan(m, L::largest(v[k]));
 #pragma unroll
   for (int s = 16; s >= 1; s >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, s));
   float sum = 0.f;
   int id = 0x7fffffff;
+  const float c = temperature > 0.f ? fminf((float)kLog2e / temperature, 3.4e38f) : 0.f;
   if (temperature > 0.f) {
-    const float c = fminf((float)kLog2e / temperature, 3.4e38f);
     if (m > none) {  // (also false for NaN, which decides by itself)
+      float2 s2 = make_float2(0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kRowVecs; ++k)
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum += ex2_approx((v[k][i] - m) * c);
+        for (int i = 0; i < N; i += 2) {
+          // (the difference first: a product of its own would round at the size of the logits)
+          const float2 z = fmul2(fadd2(make_float2(L::get(v[k], i), L::get(v[k], i + 1)), make_float2(-m, -m)), make_float2(c, c));
+          s2 = fadd2(s2, make_float2(ex2_approx(z.x), ex2_approx(z.y)));
+        }
+      sum = s2.x + s2.y;
     }
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
@@ -105,8 +157,7 @@ __global__ void __launch_bounds__(kRowThreads) draft_rows(const VerifyParams p) 
     for (int k = kRowVecs - 1; k >= 0; --k)
 #pragma unroll
       for (int i = N - 1; i >= 0; --i)
-        if (v[k][i] == m)
-          id = (int)((((int64_t)chunk * kRowVecs + k) * kRowThreads + threadIdx.x) * N - before + i);
+        if (L::get(v[k], i) == m) id = first + k * kRowThreads * N + i;
     id = __reduce_min_sync(0xffffffffu, id);
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -122,7 +173,6 @@ __global__ void __launch_bounds__(kRowThreads) draft_rows(const VerifyParams p) 
     m = mine.x;
 #pragma unroll
     for (int s = 4; s >= 1; s >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, s));
-    const float c = temperature > 0.f ? fminf((float)kLog2e / temperature, 3.4e38f) : 0.f;
     sum = mine.x > none ? mine.y * ex2_approx((mine.x - m) * c) : 0.f;
 #pragma unroll
     for (int s = 4; s >= 1; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
@@ -132,278 +182,373 @@ __global__ void __launch_bounds__(kRowThreads) draft_rows(const VerifyParams p) 
   }
 }
 
-// 2^y for y <= 0 in fp64 (0 below 2^-1000): 2^(n / 64) from the table, the rest by the series of exp, |f| <= ln 2 / 128, to
-// its fifth power: off by a few 2^-53.
+// 2^y for y <= 0 in fp64 (0 below 2^-1000): 2^(n / 256) from the table, the rest by the series of 2^f = exp(f ln 2), |f| <=
+// 2^-9, to its fourth power: off by 2^-54 and the roundings.
+constexpr int kExpTable = 256;
+__device__ __forceinline__ void fill_exp_table(double* table) {
+  for (int i = threadIdx.x; i < kExpTable; i += blockDim.x) table[i] = exp2((double)i / kExpTable);
+}
 __device__ __forceinline__ double exp2_neg(double y, const double* table) {
-  const double magic = 6755399441055744.0 / 64.0;  // 1.5 * 2^52 / 64: rounds to whole 64ths
+  const double magic = 6755399441055744.0 / kExpTable;  // 1.5 * 2^52 / 256: rounds to whole 256ths
   const double t = y + magic;
   const int n = __double2loint(t);
-  const double f = (y - (t - magic)) * kLn2;
-  double s = fma(f, 1.0 / 120.0, 1.0 / 24.0);
-  s = fma(f, s, 1.0 / 6.0);
-  s = fma(f, s, 0.5);
+  const double f = y - (t - magic);
+  constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4;
+  double s = fma(f, c4, c3);
+  s = fma(f, s, c2);
+  s = fma(f, s, c1);
   s = fma(f, s, 1.0);
-  s = fma(f, s, 1.0);
-  s *= table[n & 63];
-  s = __hiloint2double(__double2hiint(s) + ((n >> 6) << 20), __double2loint(s));
-  return y < -1000.0 ? 0.0 : s;
+  s *= table[n & (kExpTable - 1)];
+  // (the exponent goes into the upper word; y's, compared there too, is that of -1000 or beyond)
+  s = __hiloint2double(__double2hiint(s) + ((n >> 8) << 20), __double2loint(s));
+  return (uint32_t)__double2hiint(y) >= 0xC08F4000u ? 0.0 : s;
 }
 
 enum DraftState : int { kRefused = 0, kAccepted = 1, kNear = 2, kBroken = 3 };
 
+__device__ __forceinline__ double uniform(uint32_t word) { return ((double)word + 0.5) * (1.0 / 4294967296.0); }
+__device__ __forceinline__ double draft_q(const VerifyParams& p, int draft, int x) {
+  if (p.probs == nullptr) return 1.0;
+  return x >= 0 && x < p.V ? (double)p.probs[(int64_t)draft * p.ld_probs + x] : 0.0;
+}
+// The terms that a token is sampled by: exponentials of a row, one id left out or none, or what the draft leaves of the
+// probabilities.
 template <typename X>
-__global__ void __launch_bounds__(kDecideThreads) draft_decide(const VerifyParams p) {
-  __shared__ double table[64];
-  __shared__ double warp_sums[kDecideWarps];
-  __shared__ double cta_sums[2];
+struct SampledRow {
+  const X* row;
+  const float* q_row;  // null: exponentials
+  const double* table;
+  double m, c, inv_z;
+  int without;         // -1: none
+
+  __device__ __forceinline__ double exponential(float l) const { return exp2_neg(((double)l - m) * c, table); }
+  __device__ __forceinline__ double term(float l, float q) const {
+    const double e = exponential(l);
+    if (q_row == nullptr) return e;
+    const double r = fma(e, inv_z, -(double)q);
+    const int keep = ~(__double2hiint(r) >> 31);  // 0 where the draft has more
+    return __hiloint2double(__double2hiint(r) & keep, __double2loint(r) & keep);
+  }
+  // id i's logit (nothing outside the range) and draft probability (NaN: no probability is left of it)
+  __device__ __forceinline__ float logit(int i, bool in) const {
+    return in && i != without ? (float)row[i] : __int_as_float(0xFF800000);
+  }
+  __device__ __forceinline__ float draft(int i, bool in) const {
+    const float q = q_row != nullptr && in ? q_row[i] : 0.f;
+    return q == q ? q : __int_as_float(0x7F800000);
+  }
+  // Sum over the ids from .. to, in all lanes of the warp.
+  __device__ __forceinline__ double sum(int from, int to) const {
+    constexpr int U = 8;
+    const int lane = threadIdx.x & 31;
+    double acc = 0.0;
+    for (int i0 = from + lane; i0 < to; i0 += 32 * U) {
+      float l[U], q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) l[u] = logit(i0 + 32 * u, i0 + 32 * u < to);
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u] = draft(i0 + 32 * u, i0 + 32 * u < to);
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc += term(l[u], q[u]);  // (0 behind the range)
+    }
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) acc += shfl_xor_double(acc, s);
+    return acc;
+  }
+};
+
+// Of a request: what is sampled, by mode.
+enum PickMode : int { kPickNone = 0, kPickRow = 1, kPickWithout = 2, kPickResidual = 3 };
+
+__device__ __forceinline__ double scale_of(float temperature) { return kLog2e / (double)temperature; }
+__device__ __forceinline__ float temperature_of(const VerifyParams& p, int b) {
+  return p.temperatures != nullptr ? p.temperatures[b] : p.temperature;
+}
+
+// Joins the records of a request's rows, a warp a row, and walks its drafts.
+template <typename X>
+__global__ void __launch_bounds__(kMergeThreads) draft_merge(const VerifyParams p) {
+  __shared__ double table[kExpTable];
+  __shared__ double warp_sums[kMergeThreads / 32];
   __shared__ float row_max[kVerifyMaxDrafts + 1];
   __shared__ int row_id[kVerifyMaxDrafts + 1];
   __shared__ int state[kVerifyMaxDrafts + 1];
-  cg::cluster_group cluster = cg::this_cluster();
-  const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int b = blockIdx.x / ranks;
+  const int b = blockIdx.x;
   const float none = __int_as_float(0xFF800000);
-  if (threadIdx.x < 64) table[threadIdx.x] = exp2((double)threadIdx.x / 64.0);
-  grid_wait();
-
+  fill_exp_table(table);
   const int o0 = p.offsets[b], o1 = p.offsets[b + 1];
-  const float temperature = p.temperatures != nullptr ? p.temperatures[b] : p.temperature;
+  const float temperature = temperature_of(p, b);
+  __syncthreads();
+  grid_wait();
+  grid_release();
   uint32_t status = 0;
   if (o0 < 0 || o1 < o0 || o1 > p.n_drafts || o1 - o0 > p.max_drafts) status |= kDraftBadOffsets;
   if (!(temperature >= 0.f) || temperature > 3.4e38f) status |= kDraftBadTemperature;
   int32_t* tokens = p.tokens + (int64_t)b * (p.max_drafts + 1);
-  if (status != 0) {  // the same in the whole cluster
-    if (rank == 0) {
-      for (int j = threadIdx.x; j <= p.max_drafts; j += kDecideThreads) tokens[j] = -1;
-      if (threadIdx.x == 0) {
-        p.n_accepted[b] = 0;
-        if (p.status != nullptr) p.status[b] = status;
+  int m = 0, mode = kPickNone;
+  if (status == 0) {  // the same in the whole CTA
+    const int n = o1 - o0;
+    const int64_t row0 = (int64_t)o0 + b;
+    const bool greedy = temperature == 0.f;
+    const double c = greedy ? 0.0 : scale_of(temperature);
+    const X* logits = static_cast<const X*>(p.logits);
+    int broken_ids = 0;
+    for (int j = warp; j <= n; j += kMergeThreads / 32) {
+      const float4* rec = p.records + (row0 + j) * p.chunks;
+      const int x = j < n ? p.drafted[o0 + j] : -1;
+      const bool known = x >= 0 && x < p.V;
+      const float lx = known ? (float)logits[(row0 + j) * p.ld + x] : 0.f;
+      const double bound = j < n ? uniform(p.accept_words[o0 + j]) * draft_q(p, o0 + j, x) : 0.0;
+      float top = none;
+      for (int k = lane; k < p.chunks; k += 32) top = max_nan(top, rec[k].x);
+#pragma unroll
+      for (int s = 16; s >= 1; s >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, s));
+      const bool fine = top > none && top < -none;
+      double sum = 0.0;
+      int id = 0x7fffffff;
+      for (int k = lane; k < p.chunks; k += 32) {
+        const float4 r = rec[k];
+        if (r.x > none) sum += (double)r.y * exp2_neg(((double)r.x - (double)top) * c, table);
+        if (r.x == top) id = min(id, __float_as_int(r.z));
+      }
+#pragma unroll
+      for (int s = 16; s >= 1; s >>= 1) sum += shfl_xor_double(sum, s);
+      id = __reduce_min_sync(0xffffffffu, id);
+      int st = fine ? kRefused : kBroken;
+      double pd = __longlong_as_double(0x7FF8000000000000LL);
+      if (j < n) {
+        if (!known) broken_ids = 1;
+        if (fine) {
+          pd = !known ? 0.0 : greedy ? (x == id ? 1.0 : 0.0) : exp2_neg(((double)lx - (double)top) * c, table) / sum;
+          if (bound < pd) st = kAccepted;
+          if (!greedy && known && fabs(bound - pd) <= kNearBorder * pd) st = kNear;
+        }
+        if (lane == 0 && p.p_draft != nullptr) p.p_draft[o0 + j] = (float)pd;
+      }
+      if (lane == 0) {
+        row_max[j] = top;
+        row_id[j] = id;
+        state[j] = st;
       }
     }
+    broken_ids = __syncthreads_or(broken_ids);
+    if (broken_ids) status |= kDraftBadToken;
+    bool broken = false;
+    for (; m < n; ++m) {
+      int st = state[m];
+      if (st == kNear) {
+        const SampledRow<X> r = {logits + (row0 + m) * p.ld, nullptr, table, (double)row_max[m], c, 1.0, -1};
+        const int per_warp = (p.V + kMergeThreads / 32 - 1) / (kMergeThreads / 32);
+        const int from = min(p.V, warp * per_warp);
+        const double acc = r.sum(from, min(p.V, from + per_warp));
+        __syncthreads();
+        if (lane == 0) warp_sums[warp] = acc;
+        __syncthreads();
+        double z = 0.0;
+        for (int w = 0; w < kMergeThreads / 32; ++w) z += warp_sums[w];
+        const int x = p.drafted[o0 + m];
+        st = uniform(p.accept_words[o0 + m]) * draft_q(p, o0 + m, x) < r.exponential((float)r.row[x]) / z ? kAccepted : kRefused;
+      }
+      if (st == kAccepted) continue;
+      broken = st == kBroken;
+      break;
+    }
+    if (m == n) broken = state[n] == kBroken;
+    if (broken) status |= kDraftBadRow;
+    for (int j = threadIdx.x; j <= p.max_drafts; j += kMergeThreads)
+      tokens[j] = j < m ? p.drafted[o0 + j] : j == m && greedy && !broken ? row_id[m] : -1;
+    if (!greedy && !broken) mode = m == n ? kPickRow : p.probs == nullptr ? kPickWithout : kPickResidual;
+    if (threadIdx.x == 0) p.picks[b] = make_float4(row_max[m], __int_as_float(mode), __int_as_float(m), 0.f);
+  } else {
+    for (int j = threadIdx.x; j <= p.max_drafts; j += kMergeThreads) tokens[j] = -1;
+    if (threadIdx.x == 0) p.picks[b] = make_float4(0.f, __int_as_float(kPickNone), __int_as_float(0), 0.f);
+  }
+  if (threadIdx.x == 0) {
+    p.n_accepted[b] = m;
+    if (p.status != nullptr) p.status[b] = status;
+  }
+}
+
+// The row that request b samples; its sums of chunks lie where the records of its rows did, (exponentials, terms) each.
+template <typename X>
+__device__ __forceinline__ SampledRow<X> sampled_row(const VerifyParams& p, int b, float4 pick, const double* table, double2** sums) {
+  const int o0 = p.offsets[b], m = __float_as_int(pick.z), mode = __float_as_int(pick.y);
+  const int64_t row0 = (int64_t)o0 + b;
+  *sums = reinterpret_cast<double2*>(p.records + row0 * p.chunks);
+  const int x = mode == kPickWithout ? p.drafted[o0 + m] : -1;
+  return {static_cast<const X*>(p.logits) + (row0 + m) * p.ld,
+          mode == kPickResidual ? p.probs + (int64_t)(o0 + m) * p.ld_probs : nullptr, table, (double)pick.x,
+          scale_of(temperature_of(p, b)), 1.0, x >= 0 && x < p.V ? x : -1};
+}
+// The row's sum, the same in all lanes of all warps: the chunks' in their order by lanes, then the lanes'.
+__device__ __forceinline__ double sum_of_chunks(const double2* sums, int n) {
+  double z = 0.0;
+  for (int k = threadIdx.x & 31; k < n; k += 32) z += sums[k].x;
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) z += shfl_xor_double(z, s);
+  return z;
+}
+
+// A chunk's sum.  TERMS: of the terms; otherwise of the exponentials, where a residual needs them.
+template <typename X, bool TERMS>
+__global__ void __launch_bounds__(kSumThreads, 4) draft_sums(const VerifyParams p) {
+  __shared__ double table[kExpTable];
+  __shared__ double warp_sums[kSumWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = p.first_request + blockIdx.y, chunk = blockIdx.x, n_chunks = gridDim.x;
+  fill_exp_table(table);
+  __syncthreads();
+  grid_wait();
+  grid_release();
+  const float4 pick = p.picks[b];
+  const int mode = __float_as_int(pick.y);
+  if (TERMS ? mode == kPickNone : mode != kPickResidual) return;
+  double2* sums;
+  SampledRow<X> r = sampled_row<X>(p, b, pick, table, &sums);
+  if (!TERMS)
+    r.q_row = nullptr;
+  else if (mode == kPickResidual)
+    r.inv_z = 1.0 / sum_of_chunks(sums, n_chunks);
+  const int first = chunk * kSumIds + warp * (kSumIds / kSumWarps);
+  const double acc = r.sum(min(first, p.V), min(first + kSumIds / kSumWarps, p.V));
+  if (lane == 0) warp_sums[warp] = acc;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int w = 0; w < kSumWarps; ++w) s += warp_sums[w];
+    if (TERMS) sums[chunk].y = s; else sums[chunk].x = s;
+  }
+}
+
+// The token: the chunk that holds the target sum, in it the warp's range, which all warps share out once more, and in that the
+// warp that walks its part.  Each time the last range with a sum at all where rounding has the target beyond every one.
+template <typename X>
+__global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) {
+  __shared__ double table[kExpTable];
+  __shared__ double warp_sums[2][kSumWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = blockIdx.x;
+  const int n_chunks = (p.V + kSumIds - 1) / kSumIds;
+  fill_exp_table(table);
+  __syncthreads();
+  grid_wait();
+  const float4 pick = p.picks[b];
+  const int mode = __float_as_int(pick.y), m = __float_as_int(pick.z);
+  if (mode == kPickNone) return;
+  double2* sums;
+  SampledRow<X> r = sampled_row<X>(p, b, pick, table, &sums);
+  int32_t* token = p.tokens + (int64_t)b * (p.max_drafts + 1) + m;
+  double total = 0.0;
+  for (int k = 0; k < n_chunks; ++k) total += sums[k].y;
+  const bool left = total > 0.0;
+  if (!left && mode == kPickWithout) {  // all of the probability was the drafted token's
+    if (threadIdx.x == 0) *token = r.without;
     return;
   }
-  const int n = o1 - o0;
-  const int64_t row0 = (int64_t)o0 + b;
-  const bool greedy = temperature == 0.f;
-  const double c = greedy ? 0.0 : kLog2e / (double)temperature;
-  const X* logits = static_cast<const X*>(p.logits);
-  __syncthreads();
-
-  auto uniform = [](uint32_t word) { return ((double)word + 0.5) * (1.0 / 4294967296.0); };
-  auto draft_q = [&](int j, int x) {
-    if (p.probs == nullptr) return 1.0;
-    return x >= 0 && x < p.V ? (double)p.probs[(int64_t)(o0 + j) * p.ld_probs + x] : 0.0;
-  };
-  // Every CTA of the cluster joins the records of all rows for itself, a warp a row.
-  int broken_ids = 0;
-  for (int j = warp; j <= n; j += kDecideWarps) {
-    const float4* rec = p.records + (row0 + j) * p.chunks;
-    float m = none;
-    for (int k = lane; k < p.chunks; k += 32) m = max_nan(m, rec[k].x);
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, s));
-    const bool fine = m > none && m < -none;
-    double sum = 0.0;
-    int id = 0x7fffffff;
-    for (int k = lane; k < p.chunks; k += 32) {
-      const float4 r = rec[k];
-      if (r.x > none) sum += (double)r.y * exp2_neg(((double)r.x - (double)m) * c, table);
-      if (r.x == m) id = min(id, __float_as_int(r.z));
-    }
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) sum += shfl_xor_double(sum, s);
-    id = __reduce_min_sync(0xffffffffu, id);
-    int st = kBroken;
-    double pd = __longlong_as_double(0x7FF8000000000000LL);
-    if (j < n) {
-      const int x = p.drafted[o0 + j];
-      const bool known = x >= 0 && x < p.V;
-      if (!known) broken_ids = 1;
-      if (fine) {
-        if (!known)
-          pd = 0.0;
-        else if (greedy)
-          pd = x == id ? 1.0 : 0.0;
-        else
-          pd = exp2_neg(((double)(float)logits[(row0 + j) * p.ld + x] - (double)m) * c, table) / sum;
-        const double bound = uniform(p.accept_words[o0 + j]) * draft_q(j, x);
-        st = bound < pd ? kAccepted : kRefused;
-        if (!greedy && known && fabs(bound - pd) <= kNearBorder * pd) st = kNear;
-      }
-      if (rank == 0 && lane == 0 && p.p_draft != nullptr) p.p_draft[o0 + j] = (float)pd;
-    } else if (fine) {
-      st = kRefused;
-    }
-    if (lane == 0) {
-      row_max[j] = m;
-      row_id[j] = id;
-      state[j] = st;
-    }
+  if (!left) {  // the draft leaves nothing: the target's own probabilities
+    r.q_row = nullptr;
+    total = 0.0;
+    for (int k = 0; k < n_chunks; ++k) total += sums[k].x;
+  } else if (mode == kPickResidual) {
+    r.inv_z = 1.0 / sum_of_chunks(sums, n_chunks);
   }
-  broken_ids = __syncthreads_or(broken_ids);
-  if (broken_ids) status |= kDraftBadToken;
-
-  // contiguous ranges of ids: of the CTAs, inside them of the warps
-  const int per_cta = (p.V + ranks - 1) / ranks, first = min(p.V, rank * per_cta), last = min(p.V, first + per_cta);
-  const int per_warp = (last - first + kDecideWarps - 1) / kDecideWarps;
-  const int w_first = min(last, first + warp * per_warp), w_last = min(last, w_first + per_warp);
-  // what is summed: exponentials of a row, or what the draft leaves of its probabilities
-  const X* row = nullptr;
-  const float* q_row = nullptr;
-  double m64 = 0.0, inv_z = 1.0;
-  int without = -1;
-  auto term = [&](float l, float q) {
-    const double e = exp2_neg(((double)l - m64) * c, table);
-    return q_row != nullptr ? fmax(fma(e, inv_z, -(double)q), 0.0) : e;
-  };
-  int turn = 0;
-  double total = 0.0, before = 0.0;  // of the cluster; of the CTAs before this one
-  auto take_sums = [&]() {
-    constexpr int U = 8;
-    double acc = 0.0;
-    for (int i0 = w_first + lane; i0 < w_last; i0 += 32 * U) {
-      float l[U], q[U];
+  const double target = uniform(p.sample_words[b]) * total;
+  int from = 0, to = p.V;
+  double run = 0.0;
+#pragma unroll 1
+  for (int level = 0; level < 3; ++level) {
+    const int part = level == 0 ? kSumIds : (to - from + kSumWarps - 1) / kSumWarps;
+    const int parts = level == 0 ? n_chunks : kSumWarps;
+    if (level > 0) {
+      const int p_first = min(to, from + warp * part);
+      const double acc = r.sum(p_first, min(to, p_first + part));
+      if (lane == 0) warp_sums[level - 1][warp] = acc;
+      __syncthreads();
+    }
+    int found = -1;
+    double found_run = run;
+    for (int w = 0; w < parts; ++w) {
+      const double s = level == 0 ? (left ? sums[w].y : sums[w].x) : warp_sums[level - 1][w];
+      if (s > 0.0 && (found < 0 || run <= target)) {
+        found = w;
+        found_run = run;
+      }
+      run += s;
+    }
+    from = min(to, from + max(found, 0) * part);
+    to = min(to, from + part);
+    run = found_run;
+    if (level == 2 && warp != found) from = to;  // one warp walks
+  }
+  int at = -1;
+  constexpr int U = 4;  // neighbours a lane
+  for (int i0 = from; i0 < to; i0 += 32 * U) {
+    double v[U], own = 0.0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + lane * U + u;
+      v[u] = r.term(r.logit(i, i < to), r.draft(i, i < to));
+      own += v[u];
+    }
+    double scan = own;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const double o = __shfl_up_sync(0xffffffffu, scan, s);
+      if (lane >= s) scan += o;
+    }
+    // the first lane that passes the target, or the last one with anything so far
+    const unsigned hit = __ballot_sync(0xffffffffu, own > 0.0 && run + scan > target);
+    const unsigned some = __ballot_sync(0xffffffffu, own > 0.0);
+    if (some != 0) {
+      int mine = -1;
+      double s = run + scan - own;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = i0 + 32 * u;
-        l[u] = i < w_last && i != without ? (float)row[i] : none;
-        q[u] = q_row != nullptr && i < w_last ? q_row[i] : 0.f;
+        if (v[u] > 0.0 && (mine < 0 || !(s > target))) mine = i0 + lane * U + u;
+        s += v[u];
       }
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (i0 + 32 * u < w_last) acc += term(l[u], q[u]);
+      at = __shfl_sync(0xffffffffu, mine, hit != 0 ? __ffs(hit) - 1 : 31 - __clz(some));
     }
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) acc += shfl_xor_double(acc, s);
-    if (lane == 0) warp_sums[warp] = acc;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double s = 0.0;
-      for (int w = 0; w < kDecideWarps; ++w) s += warp_sums[w];
-      cta_sums[turn] = s;
-    }
-    cluster.sync();
-    total = before = 0.0;
-    for (int r = 0; r < ranks; ++r) {
-      const double s = *cluster.map_shared_rank(&cta_sums[turn], r);
-      if (r < rank) before += s;
-      total += s;
-    }
-    turn ^= 1;
-  };
-  auto set_row = [&](int j) {
-    row = logits + (row0 + j) * p.ld;
-    m64 = (double)row_max[j];
-    q_row = nullptr;
-    without = -1;
-  };
+    if (hit != 0) break;
+    run += __shfl_sync(0xffffffffu, scan, 31);
+  }
+  if (lane == 0 && from < to) *token = at;
+}
 
-  int m = 0;
-  bool broken = false;
-  for (; m < n; ++m) {
-    int st = state[m];
-    if (st == kNear) {
-      set_row(m);
-      take_sums();
-      const int x = p.drafted[o0 + m];
-      st = uniform(p.accept_words[o0 + m]) * draft_q(m, x) < exp2_neg(((double)(float)row[x] - m64) * c, table) / total
-               ? kAccepted : kRefused;
-    }
-    if (st == kAccepted) continue;
-    broken = st == kBroken;
-    break;
-  }
-  if (m == n) broken = state[n] == kBroken;
-  if (broken) status |= kDraftBadRow;
-  if (rank == 0) {
-    for (int j = threadIdx.x; j <= p.max_drafts; j += kDecideThreads)
-      if (j != m || broken) tokens[j] = j < m ? p.drafted[o0 + j] : -1;
-    if (threadIdx.x == 0) {
-      if (greedy && !broken) tokens[m] = row_id[m];
-      p.n_accepted[b] = m;
-      if (p.status != nullptr) p.status[b] = status;
-    }
-  }
-  if (!greedy && !broken) {
-    set_row(m);
-    if (m < n) {
-      const int x = p.drafted[o0 + m];
-      if (p.probs == nullptr) {
-        without = x >= 0 && x < p.V ? x : -1;
-      } else {
-        take_sums();
-        inv_z = 1.0 / total;
-        q_row = p.probs + (int64_t)(o0 + m) * p.ld_probs;
-      }
-    }
-    take_sums();
-    if (!(total > 0.0)) {  // the draft leaves nothing: the target's own probabilities
-      q_row = nullptr;
-      without = -1;
-      take_sums();
-    }
-    const double target = uniform(p.sample_words[b]) * total;
-    // the CTA whose range holds the target sum; the last one with a sum at all where rounding has it beyond every range
-    double mine = 0.0, after = 0.0;
-    for (int r = 0; r < ranks; ++r) {
-      const double s = *cluster.map_shared_rank(&cta_sums[turn ^ 1], r);
-      if (r == rank) mine = s;
-      if (r > rank) after += s;
-    }
-    if (mine > 0.0 && before <= target && (target < before + mine || after == 0.0)) {
-      double w_before = before, w_after = 0.0;
-      for (int w = 0; w < warp; ++w) w_before += warp_sums[w];
-      for (int w = warp + 1; w < kDecideWarps; ++w) w_after += warp_sums[w];
-      const double own = warp_sums[warp];
-      if (own > 0.0 && w_before <= target && (target < w_before + own || w_after == 0.0)) {
-        // this warp's range once more, 32 ids at a time
-        double run = w_before;
-        int found = -1, last_id = -1;
-        for (int i0 = w_first; i0 < w_last && found < 0; i0 += 32) {
-          const int i = i0 + lane;
-          const bool in = i < w_last;
-          const double v = in ? term(i != without ? (float)row[i] : none, q_row != nullptr ? q_row[i] : 0.f) : 0.0;
-          double scan = v;
-#pragma unroll
-          for (int s = 1; s < 32; s <<= 1) {
-            const double o = __shfl_up_sync(0xffffffffu, scan, s);
-            if (lane >= s) scan += o;
-          }
-          const unsigned hit = __ballot_sync(0xffffffffu, in && v > 0.0 && run + scan > target);
-          const unsigned some = __ballot_sync(0xffffffffu, v > 0.0);
-          if (hit != 0) found = i0 + __ffs(hit) - 1;
-          if (some != 0) last_id = i0 + 31 - __clz(some);
-          run += __shfl_sync(0xffffffffu, scan, 31);
-        }
-        if (lane == 0) tokens[m] = found >= 0 ? found : last_id;
-      }
-    }
-  }
-  cluster.sync();  // (the sums of this CTA may still be read)
+template <typename X>
+static cudaError_t launch_next(void (*kernel)(const VerifyParams), dim3 grid, int threads, const VerifyParams& p, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  memset(&attr, 0, sizeof attr);
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 template <typename X>
 static cudaError_t launch_typed(const VerifyParams& p, cudaStream_t stream) {
   draft_rows<X><<<dim3((unsigned)(p.n_drafts + p.B), (unsigned)p.chunks), kRowThreads, 0, stream>>>(p);
   cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  constexpr int ranks = 8;
-  cudaLaunchConfig_t cfg;
-  memset(&cfg, 0, sizeof cfg);
-  cfg.gridDim = dim3((unsigned)(p.B * ranks), 1, 1);
-  cfg.blockDim = dim3(kDecideThreads, 1, 1);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[2];
-  memset(attr, 0, sizeof attr);
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = ranks;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, draft_decide<X>, p);
+  if (e == cudaSuccess) e = launch_next<X>(draft_merge<X>, dim3((unsigned)p.B), kMergeThreads, p, stream);
+  if (p.temperatures == nullptr && p.temperature == 0.f) return e;  // greedy: done
+  const unsigned chunks = (unsigned)((p.V + kSumIds - 1) / kSumIds);
+  // (a grid's second dimension holds 65535: requests beyond that in further launches)
+  for (int b0 = 0; b0 < p.B && e == cudaSuccess; b0 += 65535) {
+    VerifyParams q = p;
+    q.first_request = b0;
+    const dim3 grid(chunks, (unsigned)(p.B - b0 < 65535 ? p.B - b0 : 65535));
+    if (p.probs != nullptr) e = launch_next<X>(draft_sums<X, false>, grid, kSumThreads, q, stream);
+    if (e == cudaSuccess) e = launch_next<X>(draft_sums<X, true>, grid, kSumThreads, q, stream);
+  }
+  if (e == cudaSuccess) e = launch_next<X>(draft_pick<X>, dim3((unsigned)p.B), kSumThreads, p, stream);
+  return e;
 }
 
 cudaError_t launch_verify_drafts(const VerifyParams& p, int dtype, cudaStream_t stream) {

@@ -75,9 +75,11 @@ struct VerifyParams {
   float* p_draft;                // [n_drafts], nullable
   uint32_t* status;              // [B], nullable
   float4* records;               // [n_drafts + B][chunks]: largest logit, sum of exponentials, first id of the largest
+  float4* picks;                 // [B]: largest logit of the row to sample, how it is sampled, accepted drafts
   int64_t ld, ld_probs;
   float temperature;
   int B, n_drafts, V, max_drafts, chunks;
+  int first_request;             // of a launch
 };
 constexpr int kVerifyMaxDrafts = 255;
 constexpr int kVerifyChunkVecs = 1024;  // 16-byte vectors of logits per record

@@ -74,7 +74,7 @@ def test_structs_have_the_headers_layout():
 
 def test_sizes_of_the_verification():
     size = difr.difr_verify_workspace_bytes
-    assert size(1, 0, 1) == 16 and size(2, 3, 4096) == 5 * 2 * 16 and size(2, 3, 4090) == 5 * 16
+    assert size(1, 0, 1) == 2 * 16 and size(2, 3, 4096) == (5 * 2 + 2) * 16 and size(2, 3, 4090) == (5 + 2) * 16
     for bad in ((0, 0, 10), (1, -1, 10), (1, 0, 0), (1, 0, (1 << 28) + 1), (1, 1 << 30, 10), ((1 << 27) + 1, 0, 10)):
         assert size(*bad) == 0
 
