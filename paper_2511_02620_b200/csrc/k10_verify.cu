@@ -219,41 +219,80 @@ struct SampledRow {
   const float* q_row;  // null: exponentials
   const double* table;
   double m, c, inv_z;
-  int without;         // -1: none
+  int without;         // -1: none; exponentials only
 
   __device__ __forceinline__ double exponential(float l) const { return exp2_neg(((double)l - m) * c, table); }
+  template <bool RES>
   __device__ __forceinline__ double term(float l, float q) const {
     const double e = exponential(l);
-    if (q_row == nullptr) return e;
+    if (!RES) return e;
     const double r = fma(e, inv_z, -(double)q);
-    const int keep = ~(__double2hiint(r) >> 31);  // 0 where the draft has more
-    return __hiloint2double(__double2hiint(r) & keep, __double2loint(r) & keep);
+    return r > 0.0 ? r : 0.0;  // (0 for a NaN too)
   }
-  // id i's logit (nothing outside the range) and draft probability (NaN: no probability is left of it)
-  __device__ __forceinline__ float logit(int i, bool in) const {
-    return in && i != without ? (float)row[i] : __int_as_float(0xFF800000);
-  }
-  __device__ __forceinline__ float draft(int i, bool in) const {
-    const float q = q_row != nullptr && in ? q_row[i] : 0.f;
-    return q == q ? q : __int_as_float(0x7F800000);
-  }
-  // Sum over the ids from .. to, in all lanes of the warp.
-  __device__ __forceinline__ double sum(int from, int to) const {
-    constexpr int U = 8;
+  // Eight ids of each lane from i0 on, 32 apart; what is behind the range has no probability.
+  struct Some {
+    float l[8], q[8];
+  };
+  template <bool RES>
+  __device__ __forceinline__ void load(Some& s, int i0, int to) const {
     const int lane = threadIdx.x & 31;
+    if (i0 + 256 <= to) {
+      const X* l = row + i0 + lane;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s.l[u] = (float)l[32 * u];
+      if (RES) {
+        const float* q = q_row + i0 + lane;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s.q[u] = q[32 * u];
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + lane + 32 * u;
+        s.l[u] = i < to ? (float)row[i] : __int_as_float(0xFF800000);
+        if (RES) s.q[u] = i < to ? q_row[i] : 0.f;
+      }
+    }
+    if (!RES && (unsigned)(without - i0) < 256u) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + lane + 32 * u == without) s.l[u] = __int_as_float(0xFF800000);
+    }
+  }
+  template <bool RES>
+  __device__ __forceinline__ double terms(const Some& s) const {
+    double a = 0.0, b = 0.0;
+#pragma unroll
+    for (int u = 0; u < 8; u += 2) {
+      a += term<RES>(s.l[u], s.q[u]);
+      b += term<RES>(s.l[u + 1], s.q[u + 1]);
+    }
+    return a + b;
+  }
+  // Sum over the ids from .. to, in all lanes of the warp; the next ids are under way while some are worked on.  `first` holds
+  // the first ones.
+  template <bool RES>
+  __device__ __forceinline__ double sum(int from, int to, Some& first) const {
     double acc = 0.0;
-    for (int i0 = from + lane; i0 < to; i0 += 32 * U) {
-      float l[U], q[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) l[u] = logit(i0 + 32 * u, i0 + 32 * u < to);
-#pragma unroll
-      for (int u = 0; u < U; ++u) q[u] = draft(i0 + 32 * u, i0 + 32 * u < to);
-#pragma unroll
-      for (int u = 0; u < U; ++u) acc += term(l[u], q[u]);  // (0 behind the range)
+    for (int i0 = from; i0 < to; i0 += 512) {
+      Some second;
+      if (i0 + 256 < to) load<RES>(second, i0 + 256, to);
+      acc += terms<RES>(first);
+      if (i0 + 512 < to) load<RES>(first, i0 + 512, to);
+      if (i0 + 256 < to) acc += terms<RES>(second);
     }
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) acc += shfl_xor_double(acc, s);
     return acc;
+  }
+  template <bool RES>
+  __device__ __forceinline__ double sum(int from, int to) const {
+    Some first;
+    load<RES>(first, from, to);
+    return sum<RES>(from, to, first);
+  }
+  __device__ __forceinline__ double sum(int from, int to) const {
+    return q_row != nullptr ? sum<true>(from, to) : sum<false>(from, to);
   }
 };
 
@@ -392,7 +431,7 @@ __device__ __forceinline__ double sum_of_chunks(const double2* sums, int n) {
 
 // A chunk's sum.  TERMS: of the terms; otherwise of the exponentials, where a residual needs them.
 template <typename X, bool TERMS>
-__global__ void __launch_bounds__(kSumThreads, 4) draft_sums(const VerifyParams p) {
+__global__ void __launch_bounds__(kSumThreads, 3) draft_sums(const VerifyParams p) {
   __shared__ double table[kExpTable];
   __shared__ double warp_sums[kSumWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -406,12 +445,17 @@ __global__ void __launch_bounds__(kSumThreads, 4) draft_sums(const VerifyParams 
   if (TERMS ? mode == kPickNone : mode != kPickResidual) return;
   double2* sums;
   SampledRow<X> r = sampled_row<X>(p, b, pick, table, &sums);
-  if (!TERMS)
-    r.q_row = nullptr;
-  else if (mode == kPickResidual)
+  if (!TERMS) r.q_row = nullptr;
+  const int from = min(chunk * kSumIds + warp * (kSumIds / kSumWarps), p.V), to = min(from + kSumIds / kSumWarps, p.V);
+  typename SampledRow<X>::Some some;
+  double acc;
+  if (TERMS && mode == kPickResidual) {
+    r.template load<true>(some, from, to);  // (under way before the row's sum is put together)
     r.inv_z = 1.0 / sum_of_chunks(sums, n_chunks);
-  const int first = chunk * kSumIds + warp * (kSumIds / kSumWarps);
-  const double acc = r.sum(min(first, p.V), min(first + kSumIds / kSumWarps, p.V));
+    acc = r.template sum<true>(from, to, some);
+  } else {
+    acc = r.template sum<false>(from, to);
+  }
   if (lane == 0) warp_sums[warp] = acc;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -439,8 +483,17 @@ __global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) 
   double2* sums;
   SampledRow<X> r = sampled_row<X>(p, b, pick, table, &sums);
   int32_t* token = p.tokens + (int64_t)b * (p.max_drafts + 1) + m;
-  double total = 0.0;
-  for (int k = 0; k < n_chunks; ++k) total += sums[k].y;
+  // (lanes take the chunks' sums, so that their loads go out together; the row's sum is the one that the residual was taken by)
+  double total = 0.0, z = 0.0;
+  for (int k = lane; k < n_chunks; k += 32) {
+    total += sums[k].y;
+    z += sums[k].x;
+  }
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) {
+    total += shfl_xor_double(total, s);
+    z += shfl_xor_double(z, s);
+  }
   const bool left = total > 0.0;
   if (!left && mode == kPickWithout) {  // all of the probability was the drafted token's
     if (threadIdx.x == 0) *token = r.without;
@@ -448,28 +501,51 @@ __global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) 
   }
   if (!left) {  // the draft leaves nothing: the target's own probabilities
     r.q_row = nullptr;
-    total = 0.0;
-    for (int k = 0; k < n_chunks; ++k) total += sums[k].x;
+    total = z;
   } else if (mode == kPickResidual) {
-    r.inv_z = 1.0 / sum_of_chunks(sums, n_chunks);
+    r.inv_z = 1.0 / z;
   }
   const double target = uniform(p.sample_words[b]) * total;
   int from = 0, to = p.V;
   double run = 0.0;
-#pragma unroll 1
-  for (int level = 0; level < 3; ++level) {
-    const int part = level == 0 ? kSumIds : (to - from + kSumWarps - 1) / kSumWarps;
-    const int parts = level == 0 ? n_chunks : kSumWarps;
-    if (level > 0) {
-      const int p_first = min(to, from + warp * part);
-      const double acc = r.sum(p_first, min(to, p_first + part));
-      if (lane == 0) warp_sums[level - 1][warp] = acc;
-      __syncthreads();
+  {
+    // 32 chunks at a time: the last with a sum that begins at or before the target
+    double before = 0.0;
+    int chunk = 0;
+    bool any = false;
+    for (int k0 = 0; k0 < n_chunks; k0 += 32) {
+      const int k = k0 + lane;
+      const double own = k < n_chunks ? (left ? sums[k].y : sums[k].x) : 0.0;
+      double scan = own;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const double o = __shfl_up_sync(0xffffffffu, scan, s);
+        if (lane >= s) scan += o;
+      }
+      const double begin = before + scan - own;
+      const unsigned some = __ballot_sync(0xffffffffu, own > 0.0), good = __ballot_sync(0xffffffffu, own > 0.0 && begin <= target);
+      if (good != 0 || (!any && some != 0)) {
+        const int who = good != 0 ? 31 - __clz(good) : __ffs(some) - 1;
+        chunk = k0 + who;
+        run = __shfl_sync(0xffffffffu, begin, who);
+        any = true;
+      }
+      before += __shfl_sync(0xffffffffu, scan, 31);
     }
+    from = chunk * kSumIds;
+    to = min(p.V, from + kSumIds);
+  }
+#pragma unroll 1
+  for (int level = 0; level < 2; ++level) {
+    const int part = (to - from + kSumWarps - 1) / kSumWarps;
+    const int p_first = min(to, from + warp * part);
+    const double acc = r.sum(p_first, min(to, p_first + part));
+    if (lane == 0) warp_sums[level][warp] = acc;
+    __syncthreads();
     int found = -1;
     double found_run = run;
-    for (int w = 0; w < parts; ++w) {
-      const double s = level == 0 ? (left ? sums[w].y : sums[w].x) : warp_sums[level - 1][w];
+    for (int w = 0; w < kSumWarps; ++w) {
+      const double s = warp_sums[level][w];
       if (s > 0.0 && (found < 0 || run <= target)) {
         found = w;
         found_run = run;
@@ -479,7 +555,7 @@ __global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) 
     from = min(to, from + max(found, 0) * part);
     to = min(to, from + part);
     run = found_run;
-    if (level == 2 && warp != found) from = to;  // one warp walks
+    if (level == 1 && warp != found) from = to;  // one warp walks
   }
   int at = -1;
   constexpr int U = 4;  // neighbours a lane
@@ -488,7 +564,8 @@ __global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) 
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + lane * U + u;
-      v[u] = r.term(r.logit(i, i < to), r.draft(i, i < to));
+      const float l = i < to && i != r.without ? (float)r.row[i] : __int_as_float(0xFF800000);
+      v[u] = r.q_row != nullptr ? r.template term<true>(l, i < to ? r.q_row[i] : 0.f) : r.template term<false>(l, 0.f);
       own += v[u];
     }
     double scan = own;
