@@ -431,7 +431,7 @@ __device__ __forceinline__ double sum_of_chunks(const double2* sums, int n) {
 
 // A chunk's sum.  TERMS: of the terms; otherwise of the exponentials, where a residual needs them.
 template <typename X, bool TERMS>
-__global__ void __launch_bounds__(kSumThreads, 3) draft_sums(const VerifyParams p) {
+__global__ void __launch_bounds__(kSumThreads, 4) draft_sums(const VerifyParams p) {
   __shared__ double table[kExpTable];
   __shared__ double warp_sums[kSumWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;

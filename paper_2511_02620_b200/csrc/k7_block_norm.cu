@@ -17,9 +17,10 @@
 
 namespace difr {
 
-// A thread holds VPT vectors of x, of the residual and of the gate: registers for two CTAs of 512 threads only with one.
+// A thread holds VPT vectors of x, of the residual and of the gate.  Two (fp32: one) and at most 64 registers a thread: 65536 x
+// 2048 in bf16 with a gate per channel took 206 us, 219 without the limit, 224 at four vectors, 266 at one.
 template <typename X, int VPT, int FMT, bool GATE, bool AL>
-__global__ void __launch_bounds__(kNormMaxThreads, VPT == 1 ? 2 : 1) block_norm(const BlockNormParams p) {
+__global__ void __launch_bounds__(kNormMaxThreads, VPT <= 2 ? 2 : 1) block_norm(const BlockNormParams p) {
   __shared__ double part[4][kNormMaxThreads / 32];
   __shared__ uint4 stage_all[AL ? 1 : kNormMaxThreads * sizeof(X) / 2];  // 256 elements per warp
   X* stage = reinterpret_cast<X*>(stage_all) + (AL ? 0 : (threadIdx.x >> 5) * 256);
@@ -49,7 +50,8 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 1 ? 2 : 1) block_norm(
     finish_row(r, fr, res, t, tpr, p.d, stage);
     if (GATE) finish_row(g, fg, gate, t, tpr, p.d, stage);
     X* to = static_cast<X*>(p.residual_out) + row * p.ld_residual_out;
-    const float2 alpha = make_float2(p.alpha, p.alpha), beta = make_float2(p.beta, p.beta);
+    const float2 beta = make_float2(p.beta, p.beta);
+    const float scale = f.y * p.alpha;  // (one product less per value: alpha goes with the root)
     const float2 offset = make_float2(p.weight_offset, p.weight_offset);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
@@ -64,10 +66,12 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT == 1 ? 2 : 1) block_norm(
         float2 a = v[j].pair(i);
         if (post != nullptr) {
           if (f.x != 1.f) a = fmul2(a, make_float2(f.x, f.x));
-          a = fmul2(fmul2(a, make_float2(f.y, f.y)), fadd2(w[0].pair(i), offset));
+          a = fmul2(fmul2(a, make_float2(scale, scale)), fadd2(w[0].pair(i), offset));
+        } else {
+          a = fmul2(a, make_float2(scale, scale));
         }
         if (GATE) a = fmul2(a, g[j].pair(i));
-        v[j].set_pair(i, ffma2(alpha, a, fmul2(beta, r[j].pair(i))));
+        v[j].set_pair(i, ffma2(beta, r[j].pair(i), a));
       }
       if (p.residual_out != nullptr) store_row<X, AL>(v[j], to, j * tpr + t, p.d, stage);
     }
@@ -104,9 +108,9 @@ static void launch_vec(const BlockNormParams& p, unsigned grid, int threads, cud
 
 template <typename X>
 static cudaError_t launch_typed(BlockNormParams p, cudaStream_t stream) {
-  // Vectors per thread by the row alone, so that a row's result does not depend on its batch: the final norm's choice.
+  // Vectors per thread by the row alone, so that a row's result does not depend on its batch.
   const int nvec = (p.d + 127) / 128 * 16;  // to whole scale words
-  int vpt = !p.vec ? 1 : sizeof(X) == 4 ? 2 : 4;
+  int vpt = !p.vec ? 1 : sizeof(X) == 4 ? 1 : 2;
   while (vpt > 1 && nvec <= 32 * vpt / 2) vpt /= 2;
   while ((nvec + vpt - 1) / vpt > kNormMaxThreads) vpt *= 2;
   if (!p.vec && vpt == 4) vpt = 8;  // (not built: rows of more than 8192 off the 16-byte boundaries)

@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kW4Warps * 32) w4_quantize(const W4ConvertPara
     const float scale = __uint_as_float(bits << 16);
     const bool number = bits != 0u && bits != 0x7FC0u;
     const float inv = number ? 1.f / scale : 0.f;
-    const float half = 0.5f * scale, below = __uint_as_float(__float_as_uint(half) - (number ? 1u : 0u));
+    const uint32_t half = __float_as_uint(0.5f * scale);
     uint32_t word = 0;
 #pragma unroll
     for (int i = 3; i >= 0; --i) {
@@ -84,9 +84,10 @@ __global__ void __launch_bounds__(kW4Warps * 32) w4_quantize(const W4ConvertPara
       const float2 q = fadd2(t, make_float2(-12582912.f, -12582912.f));
       const float2 r = ffma2(q, make_float2(-scale, -scale), v[i]);
       const uint32_t a = opaque_bits(t.x), b = opaque_bits(t.y);
-      const float ha = (a & 1u) ? below : half, hb = (b & 1u) ? below : half;
-      const uint32_t ca = a + (fabsf(r.x) > ha ? (r.x > 0.f ? 1u : ~0u) : 0u);
-      const uint32_t cb = b + (fabsf(r.y) > hb ? (r.y > 0.f ? 1u : ~0u) : 0u);
+      // (a tie moves away from an odd integer: half of the scale less its last bit; magnitudes compare like their bits)
+      const uint32_t ra = opaque_bits(r.x), rb = opaque_bits(r.y);
+      const uint32_t ca = a + ((ra & 0x7FFFFFFFu) > half - (a & 1u) ? (uint32_t)((int)ra >> 31) | 1u : 0u);
+      const uint32_t cb = b + ((rb & 0x7FFFFFFFu) > half - (b & 1u) ? (uint32_t)((int)rb >> 31) | 1u : 0u);
       word = (word << 8) | ((cb & 15u) << 4) | (ca & 15u);
     }
     if (!number) word = 0u;
