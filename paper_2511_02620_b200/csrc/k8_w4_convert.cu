@@ -36,6 +36,44 @@ __device__ __forceinline__ uint32_t opaque_bits(float x) {
   return r;
 }
 
+// Codes of eight 16-bit values.  A quotient of 16-bit numbers that is no tie is at least 2^-14 away from one, so quotients a
+// little too small and a little too large round to the same integer except at ties, where they round to both neighbours.  On
+// 1.5 * 2^23 the sum of the two holds the integer in the same bits one exponent higher, where a unit is 2: the addition itself
+// rounds a tie's odd sum to the even neighbour.  The eight integers + 8 are then digits of a number to the base 16.
+__device__ __forceinline__ uint32_t codes_of_halves(const float2 (&v)[4], float inv) {
+  const float2 small = make_float2(inv * (1.f - 0x1p-22f), inv * (1.f - 0x1p-22f));
+  const float2 large = make_float2(inv * (1.f + 0x1p-22f), inv * (1.f + 0x1p-22f));
+  const float2 magic = make_float2(12582912.f, 12582912.f);
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 3; i >= 0; --i) {
+    const float2 u = fadd2(ffma2(v[i], small, magic), ffma2(v[i], large, magic));
+    word = (word * 16u + opaque_bits(u.y)) * 16u + opaque_bits(u.x);
+  }
+  constexpr uint32_t base = 0x4BC00000u - 8u;  // the bits of 2 * 1.5 * 2^23, and the 8 that is added to each
+  return (word - base * 0x11111111u) ^ 0x88888888u;
+}
+// Codes of eight fp32 values, whose quotients may lie next to a tie.  1.5 * 2^23: the sum's last bits are the integer nearest
+// to value * inv; what is left of the value, which is exact, shows where inv's rounding took the wrong side of a border, and the
+// ties.
+__device__ __forceinline__ uint32_t codes_of_floats(const float2 (&v)[4], float inv, float scale) {
+  const uint32_t half = __float_as_uint(0.5f * scale);
+  uint32_t word = 0;
+#pragma unroll
+  for (int i = 3; i >= 0; --i) {
+    const float2 t = ffma2(v[i], make_float2(inv, inv), make_float2(12582912.f, 12582912.f));
+    const float2 q = fadd2(t, make_float2(-12582912.f, -12582912.f));
+    const float2 r = ffma2(q, make_float2(-scale, -scale), v[i]);
+    const uint32_t a = opaque_bits(t.x), b = opaque_bits(t.y);
+    // (a tie moves away from an odd integer: half of the scale less its last bit; magnitudes compare like their bits)
+    const uint32_t ra = opaque_bits(r.x), rb = opaque_bits(r.y);
+    const uint32_t ca = a + ((ra & 0x7FFFFFFFu) > half - (a & 1u) ? (uint32_t)((int)ra >> 31) | 1u : 0u);
+    const uint32_t cb = b + ((rb & 0x7FFFFFFFu) > half - (b & 1u) ? (uint32_t)((int)rb >> 31) | 1u : 0u);
+    word = (word << 8) | ((cb & 15u) << 4) | (ca & 15u);
+  }
+  return word;
+}
+
 template <typename X, int GROUP, bool AL>
 __global__ void __launch_bounds__(kW4Warps * 32) w4_quantize(const W4ConvertParams p) {
   __shared__ uint4 stage_all[AL ? 1 : kW4Warps * 32 * sizeof(X) / 2];
@@ -72,25 +110,7 @@ __global__ void __launch_bounds__(kW4Warps * 32) w4_quantize(const W4ConvertPara
     const uint32_t bits = w4_scale_bits(m);
     const float scale = __uint_as_float(bits << 16);
     const bool number = bits != 0u && bits != 0x7FC0u;
-    const float inv = number ? 1.f / scale : 0.f;
-    const uint32_t half = __float_as_uint(0.5f * scale);
-    uint32_t word = 0;
-#pragma unroll
-    for (int i = 3; i >= 0; --i) {
-      // 1.5 * 2^23: the sum's last bits are the integer nearest to value * inv; what is left of the value, which is
-      // exact, shows where inv's rounding took the wrong side of a border, and the ties
-      const float2 magic = make_float2(12582912.f, 12582912.f);
-      const float2 t = ffma2(v[i], make_float2(inv, inv), magic);
-      const float2 q = fadd2(t, make_float2(-12582912.f, -12582912.f));
-      const float2 r = ffma2(q, make_float2(-scale, -scale), v[i]);
-      const uint32_t a = opaque_bits(t.x), b = opaque_bits(t.y);
-      // (a tie moves away from an odd integer: half of the scale less its last bit; magnitudes compare like their bits)
-      const uint32_t ra = opaque_bits(r.x), rb = opaque_bits(r.y);
-      const uint32_t ca = a + ((ra & 0x7FFFFFFFu) > half - (a & 1u) ? (uint32_t)((int)ra >> 31) | 1u : 0u);
-      const uint32_t cb = b + ((rb & 0x7FFFFFFFu) > half - (b & 1u) ? (uint32_t)((int)rb >> 31) | 1u : 0u);
-      word = (word << 8) | ((cb & 15u) << 4) | (ca & 15u);
-    }
-    if (!number) word = 0u;
+    const uint32_t word = !number ? 0u : sizeof(X) == 2 ? codes_of_halves(v, 1.f / scale) : codes_of_floats(v, 1.f / scale, scale);
     if (vec < nvec) codes[vec] = word;
     if (vec < nvec_scales && (lane & (GROUP / 8 - 1)) == 0)
       scales[vec / (GROUP / 8)] = __ushort_as_bfloat16((unsigned short)bits);
