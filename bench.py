@@ -774,6 +774,20 @@ def time_variants(difr, h, W, tokens, seeds, pos, temperature, sigma, T, d, V, i
         calls[f"mx_quantize_head_{bits}_bits"] = lambda Wq=Wq: difr.difr_mx_quantize(W, Wq)
         calls[f"mx_logits_{bits}_bits_4096_rows"] = lambda hq=hq, Wq=Wq: difr.difr_mx_logits(hq, Wq, logits,
                                                                                              out.device_status)
+    # the norms around the last block, the head as 4-bit integers with group scales, and the verification of drafted tokens
+    out_norm = difr.NormOut(h=torch.empty_like(x), residual=stream)
+    calls["block_norm_4096_rows"] = lambda: difr.difr_block_norm(x, stream, gain, 1e-6, out_norm, post_weight=gain)
+    W4 = difr.W4Tensor.allocate(V, d, 128)
+    ws4 = torch.empty(difr.difr_w4_workspace_bytes(rows, d), dtype=torch.uint8, device="cuda")
+    calls["w4_quantize_head"] = lambda: difr.difr_w4_quantize(W, W4)
+    calls["w4_logits_4096_rows"] = lambda: difr.difr_w4_logits(h[:rows], W4, logits, ws4, out.device_status)
+    calls["w4_logits_one_row"] = lambda: difr.difr_w4_logits(h[:1], W4, logits[:1], ws4, out.device_status)
+    drafts, requests = rows - rows // 8, rows // 8  # up to 7 drafted tokens a request
+    words = torch.arange(rows, dtype=torch.int32, device="cuda") * 0x9E3779B + 12345
+    offsets = torch.arange(requests + 1, dtype=torch.int32, device="cuda") * 7
+    picked = difr.DraftOut.allocate(requests, drafts, 7, V)
+    calls["verify_drafts_4096_rows"] = lambda: difr.difr_verify_drafts(
+        logits, tokens[:drafts], offsets, words[:drafts], words[:requests], temperature, picked)
     res = {}
     calls["score_gm"]()
     for name, fn in calls.items():

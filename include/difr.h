@@ -564,7 +564,13 @@ difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t gr
 /*
  * logits[t, v] = h[t, :] . W[v, :] with h bf16 [T, d] (row stride ldh >= d) and W [V, d] in 4 bits, accumulated in fp32;
  * `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or DIFR_BF16.  Any T from 1, any V from 1, any d.
- * The logits of a row of h with a NaN or an infinity are NaN, and so are those of an id with such a scale.
+ * The tensor cores add 16 exact products per step and drop low bits there: the tests hold the fp32 sums within (steps + 2)
+ * 2^-23 sum |h W| of the exact ones; they lie 4e-6 of their size nearer to zero at d = 4096.  Values below 2^-31 of the
+ * largest of their row of h, or whose scale is below 2^-27 of the largest of their id, lose bits below 2^-39 (2^-35) of that
+ * largest; scales below 2^-126 count as zero.  The logits of a row of h with a NaN or an infinity are NaN, and so are those of
+ * an id with such a scale.  A row's logits are the same bits whatever other rows the batch holds.
+ * `workspace`: 16-byte aligned scratch; calls that may run at the same time need one each.  `device_status` as in difr_out,
+ * optional: a wait that runs out also leaves NaN in the place of every logit that was not computed.
  */
 size_t difr_w4_workspace_bytes(int64_t T, int64_t d);  /* scratch bytes of a call; 0 for sizes the library rejects */
 difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, const void* W_scales, int32_t group, int64_t T,
@@ -611,7 +617,7 @@ typedef struct {
   size_t workspace_bytes;
 } difr_drafts_out;
 /* Scratch bytes for the sizes of a call, whatever its type; 0 for sizes the library rejects
- * (B < 1, n_drafts < 0, V < 1 or > 2^28, more than 2^30 rows). */
+ * (B < 1, n_drafts < 0, V < 1 or > 2^27, more than 2^30 rows). */
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V);
 /* B == 0 returns DIFR_OK without launching. */
 difr_status difr_verify_drafts(const difr_drafts* in, int64_t B, int64_t n_drafts, int64_t V, const difr_drafts_out* out,

@@ -74,7 +74,7 @@ int64_t verify_chunks(int64_t V, int elem) {
   return ((V + 2 * (n - 1)) / n + kVerifyChunkVecs - 1) / kVerifyChunkVecs;
 }
 bool verify_supported(int64_t B, int64_t n_drafts, int64_t V) {
-  return n_drafts + B <= kMaxRows && V <= ((int64_t)1 << 28) && B <= ((int64_t)1 << 27);
+  return n_drafts + B <= kMaxRows && V <= ((int64_t)1 << 27) && B <= ((int64_t)1 << 27);
 }
 
 }  // namespace

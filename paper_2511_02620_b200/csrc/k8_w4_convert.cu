@@ -5,7 +5,7 @@
 //
 // Laid out like the microscaled conversions: a warp takes a part of a row, a lane 8 consecutive values at a time; a group is
 // 4, 8 or 16 neighbouring lanes, its maximum two to four shuffles away.  Both directions are bound by their bytes as long as
-// few instructions are spent per value.
+// few instructions are spent per value: 128256 x 4096 in bf16 takes 276 us to codes, 520 with the way back (409 of bytes).
 #include <cuda_runtime.h>
 
 #include "step_kernels.h"

@@ -17,21 +17,22 @@
 // give the same bits (an MMA adds the same sixteen products in either).
 //
 // Up to 16 tokens, `w4_few`: a warp takes 32 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, two
-// stages of two steps ahead, and meets nobody.
+// stages of two steps ahead, and meets nobody.  One token x 128256 x 4096 takes 64 us (43 of bytes), 16 tokens 81; a step of 16
+// ids is 167 instructions, 13 of them for each word of codes that becomes fp16.  (The other kernel took 115 for one token.)
 //
 // More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
 // run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads and converts its own 128 ids and loads
 // half of the tile's tokens, and the pair's first CTA issues the MMAs.  A step is 128 values of k: 64 TMEM columns of
 // converted weights (a slot), a stage of h; a stage of codes is two steps.  TMEM: two accumulators and the slots; with BN =
-// 256 the accumulators overlap by 128 columns, which the epilogue reads first.  (An MMA of few tokens takes as long as one of
-// 128, 64 clocks: a step 512, where a step's bytes take 360.  Hence the other kernel.)
+// 256 the accumulators overlap by 128 columns, which the epilogue reads first.  4096 tokens x 128256 x 4096 take 2730 us in
+// short runs (1.57 PFLOP/s), 3117 sustained under the power cap (1.38); 64 tokens 114, which is about 1000 clocks at 1965 MHz for each step of seven tiles.  Which of conversion, TMEM store
+// and MMA sets that was not measured.
 // Warps: 0 TMA of h, 1 MMA, 2 TMEM allocation, 3 TMA of codes, 4..11 epilogue (two per lane quarter, half of the tile's columns
 // each), 12..19 conversion (two per lane quarter, even and odd steps).
 //
-// The order of k.  In mma.sync lane t of four holds, of a block of 128 values, the 32 at 32 t, and MMA 2 w + e / 2 .. adds
-// pairs q = 0, 1 (then 2, 3) of all four lanes' words w = 0 .. 3.  TMEM columns and h follow that: pair q of word w of
-// lane t is column 8 (2 w + q / 2) + 4 (q & 1) + t of a step.  Where the last block has 64 values at most, lane t holds the 16
-// at 16 t, two words.
+// The order of k.  In mma.sync lane t of four holds, of a block of 128 values, the 32 at 32 t, four words, and an MMA adds pairs
+// q = 0 and 1, or 2 and 3, of all four lanes' words w.  TMEM columns and h follow that: pair q of word w of lane t is column
+// 8 (2 w + q / 2) + 4 (q & 1) + t of a step.  Where the last block has 64 values at most, lane t holds the 16 at 16 t, two words.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <string.h>

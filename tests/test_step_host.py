@@ -75,7 +75,7 @@ def test_structs_have_the_headers_layout():
 def test_sizes_of_the_verification():
     size = difr.difr_verify_workspace_bytes
     assert size(1, 0, 1) == 2 * 16 and size(2, 3, 4096) == (5 * 2 + 2) * 16 and size(2, 3, 4090) == (5 + 2) * 16
-    for bad in ((0, 0, 10), (1, -1, 10), (1, 0, 0), (1, 0, (1 << 28) + 1), (1, 1 << 30, 10), ((1 << 27) + 1, 0, 10)):
+    for bad in ((0, 0, 10), (1, -1, 10), (1, 0, 0), (1, 0, (1 << 27) + 1), (1, 1 << 30, 10), ((1 << 27) + 1, 0, 10)):
         assert size(*bad) == 0
 
 
@@ -108,7 +108,7 @@ def test_refusals_of_the_verification():
     assert verify(ld=99) == INVALID and verify(ld_draft=99) == INVALID and verify(ld_draft=99, draft_probs=None) == CUDA
     for t in (-1.0, float("nan"), float("inf")):
         assert verify(temperature=t) == INVALID and verify(temperature=t, temperatures=P) == CUDA
-    assert verify(V=(1 << 28) + 1, ld=1 << 29, ld_draft=1 << 29) == SHAPE and verify(B=1 << 28) == SHAPE
+    assert verify(V=(1 << 27) + 1, ld=1 << 29, ld_draft=1 << 29) == SHAPE and verify(B=1 << 28) == SHAPE
     assert verify(workspace=None) == WORKSPACE and verify(workspace_bytes=difr.difr_verify_workspace_bytes(3, 6, 100) - 1) == WORKSPACE
     assert verify(B=0, logits=None, offsets=None) == OK
 
