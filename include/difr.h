@@ -612,7 +612,8 @@ typedef struct {
   uint32_t* status;       /* [B], nullable.  bit0: a drafted id outside [0, V) (p = 0, refused); bit1: the row it ended at has
                              a NaN, +infinity or no finite logit (no next token: -1); bit2: offsets descend, leave
                              [0, n_drafts] or hold more than max_drafts; bit3: unusable temperature (2, 3: nothing accepted,
-                             all tokens -1) */
+                             all tokens -1).  Where bit2 stands at a request because offsets descend, others may share rows
+                             and scratch: no access leaves the buffers, but their tokens are then not to be used */
   void* workspace;        /* >= difr_verify_workspace_bytes, 16-byte aligned; scratch */
   size_t workspace_bytes;
 } difr_drafts_out;
