@@ -608,7 +608,8 @@ typedef struct {
 typedef struct {
   int32_t* tokens;        /* [B, max_drafts + 1]: the accepted drafts, the next token, -1 in the rest */
   int32_t* n_accepted;    /* [B] */
-  float* p_draft;         /* [n_drafts], nullable: p_j(x_j) of every drafted token, those behind a refusal too */
+  float* p_draft;         /* [n_drafts], nullable: p_j(x_j) of every drafted token, those behind a refusal too; NaN where its
+                             row is broken (bit1's reasons) or no request with usable offsets and temperature holds it */
   uint32_t* status;       /* [B], nullable.  bit0: a drafted id outside [0, V) (p = 0, refused); bit1: the row it ended at has
                              a NaN, +infinity or no finite logit (no next token: -1); bit2: offsets descend, leave
                              [0, n_drafts] or hold more than max_drafts; bit3: unusable temperature (2, 3: nothing accepted,

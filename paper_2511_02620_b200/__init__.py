@@ -761,7 +761,7 @@ class DraftOut:
     """Output tensors and workspace of difr_verify_drafts (mirrors `difr_drafts_out`); p_draft and status may be None."""
     tokens: "object"      # int32 [B, max_drafts + 1]: accepted drafts, the next token, -1 in the rest
     n_accepted: "object"  # int32 [B]
-    p_draft: "object"     # float [n_drafts]: the target's probability of every drafted token
+    p_draft: "object"     # float [n_drafts]: the target's probability of every drafted token, NaN where there is none
     status: "object"      # int32 [B] (uint32 bits)
     workspace: "object"   # uint8 [difr_verify_workspace_bytes(B, n_drafts, V)]
 

@@ -1,0 +1,42 @@
+"""Edges of a decoding step's operators on the GPU, against the plain 64-bit statements in step_reference.py."""
+import math
+
+import pytest
+import torch
+
+import paper_2511_02620_b200 as difr
+from test_gpu_step import check_verify, make_drafts, run_verify
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ verification of drafted tokens
+def outputs_that_held_something(s):
+    B, D, V = s["sample"].numel(), s["drafted"].numel(), s["logits"].shape[1]
+    out = difr.DraftOut.allocate(B, D, s["K"], V)
+    for x in (out.tokens, out.n_accepted, out.status):
+        x.fill_(-77)
+    out.p_draft.fill_(0.25)  # an ordinary probability, such as an earlier call's
+    return out
+
+
+def test_probabilities_of_drafts_that_are_not_looked_at():
+    """Requests with an unusable temperature or too many drafts, drafts of no request: NaN, whatever the buffer held."""
+    s = make_drafts(6, 3, 100, "f32", True, 1.0, seed=30, ragged=False)
+    s["t"] = torch.tensor([1.0, math.nan, -1.0, math.inf, 0.0, 2.0])
+    out = check_verify(s, run_verify(s, outputs_that_held_something(s)))
+    assert torch.equal(torch.isnan(out.p_draft).cpu(), torch.tensor([0, 1, 1, 1, 0, 0]).bool().repeat_interleave(3))
+    s = make_drafts(6, 3, 100, "bf16", False, 1.0, seed=31, ragged=False)
+    s["offsets"] = torch.tensor([2, 3, 3, 12, 13, 15, 17], dtype=torch.int32)
+    out = check_verify(s, run_verify(s, outputs_that_held_something(s)))
+    assert out.status.tolist() == [0, 0, 4, 0, 0, 0]
+    nan = torch.tensor([i < 2 or 3 <= i < 12 or i >= 17 for i in range(18)])
+    assert torch.equal(torch.isnan(out.p_draft).cpu(), nan)
+
+
+def test_probabilities_of_drafts_where_offsets_descend():
+    """No entry keeps what the buffer held."""
+    s = make_drafts(6, 4, 100, "f32", True, 1.0, seed=10, ragged=False)
+    s["offsets"] = torch.tensor([0, 4, 2, 8, 30, -1, 3], dtype=torch.int32)
+    out = run_verify(s, outputs_that_held_something(s))
+    assert not torch.any(out.p_draft == 0.25)
