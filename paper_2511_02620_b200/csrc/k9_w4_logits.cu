@@ -261,10 +261,10 @@ __device__ __forceinline__ void convert_word(uint32_t w, __half2 scale, __half2 
   convert_half(w, 1, scale, offset, k, out + 2);
 }
 
-// x times 2^e, e from -276 to 230: three factors where one does not do, the rounding of the last to a subnormal apart exact.
+// x times 2^e, e from -276 to 230, rounded once: where 2^e is no normal number, by way of fp64.
 __device__ __forceinline__ float times_power(float x, int e) {
-  const int a = max(-120, min(120, e)), b = max(-120, min(120, e - a)), c = e - a - b;
-  return x * __int_as_float((127 + a) << 23) * __int_as_float((127 + b) << 23) * __int_as_float((127 + c) << 23);
+  if (e >= -126 && e <= 127) return x * __int_as_float((127 + e) << 23);
+  return (float)((double)x * __hiloint2double((1023 + e) << 20, 0));
 }
 // Takes the powers of two back: r[j] times 2^(ids's exponent + token's).  `mine`: the exponent of token t0 + lane.
 template <int N>

@@ -5,7 +5,8 @@ import pytest
 import torch
 
 import paper_2511_02620_b200 as difr
-from test_gpu_step import check_verify, make_drafts, run_verify
+import step_reference as ref
+from test_gpu_step import check_verify, make_drafts, run_verify, w4_logits
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +41,26 @@ def test_probabilities_of_drafts_where_offsets_descend():
     s["offsets"] = torch.tensor([0, 4, 2, 8, 30, -1, 3], dtype=torch.int32)
     out = run_verify(s, outputs_that_held_something(s))
     assert not torch.any(out.p_draft == 0.25)
+
+
+# ------------------------------------------------------------------ the product on 4-bit weights
+@pytest.mark.parametrize("e", [-140, -130, -127, -126, -125, -123, -121, -120])
+def test_w4_logits_below_the_normal_numbers_are_rounded_once(e):
+    """Sums of integers N, exact in fp32, times 2^(e - 30): the nearest fp32 number, whatever takes the powers of two back."""
+    V, d, group = 5000, 96, 32
+    g = torch.Generator().manual_seed(33)
+    eh, es = -40, e + 64  # exponents of the largest hidden state and of the largest scale: e = eh + es - 24
+    codes = torch.randint(-8, 8, (V, d), generator=g)
+    codes[:, :group] = 0
+    scales = torch.full((V, 3), 2.0 ** (es - 20))
+    scales[:, 0] = 2.0 ** es
+    c, s = ref.w4_pack(codes, scales, d, group)
+    W = difr.W4Tensor(c.cuda(), s.cuda(), group, V, d)
+    h = torch.randint(-255, 256, (300, d), generator=g).double() * 2.0 ** (eh - 34)
+    h[:, 0] = 2.0 ** eh
+    h = h.to(torch.bfloat16)
+    want = (h.double() @ ref.w4_values(c, s, d, group).T).float()
+    assert e < -126 or 0 < int((want.abs() < 2.0 ** -126).sum())
+    for T in (1, 16, 30, 60, 100, 300):
+        got = w4_logits(h[:T], W).cpu()
+        assert torch.equal(got, want[:T]), T
