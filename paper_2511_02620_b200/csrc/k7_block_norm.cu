@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT <= 2 ? 2 : 1) block_norm(
     if (GATE) finish_row(g, fg, gate, t, tpr, p.d, stage);
     X* to = static_cast<X*>(p.residual_out) + row * p.ld_residual_out;
     const float2 beta = make_float2(p.beta, p.beta);
-    const float scale = f.y * p.alpha;  // (one product less per value: alpha goes with the root)
+    const float2 alpha = make_float2(p.alpha, p.alpha);
     const float2 offset = make_float2(p.weight_offset, p.weight_offset);
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
@@ -67,12 +67,11 @@ __global__ void __launch_bounds__(kNormMaxThreads, VPT <= 2 ? 2 : 1) block_norm(
         float2 a = v[j].pair(i);
         if (post != nullptr) {
           if (f.x != 1.f) a = fmul2(a, make_float2(f.x, f.x));
-          a = fmul2(fmul2(a, make_float2(scale, scale)), fadd2(w[0].pair(i), offset));
-        } else {
-          a = fmul2(a, make_float2(scale, scale));
+          a = fmul2(fmul2(a, make_float2(f.y, f.y)), fadd2(w[0].pair(i), offset));
         }
         if (GATE) a = fmul2(a, g[j].pair(i));
-        v[j].set_pair(i, ffma2(beta, r[j].pair(i), a));
+        // (alpha last, as the formula has it: its product with the root or with x may leave fp32 where n does not)
+        v[j].set_pair(i, ffma2(beta, r[j].pair(i), fmul2(a, alpha)));
       }
       if (p.residual_out != nullptr) store_row<X, AL>(v[j], to, j * tpr + t, p.d, stage);
     }

@@ -6,7 +6,7 @@ import torch
 
 import paper_2511_02620_b200 as difr
 import step_reference as ref
-from test_gpu_step import check_verify, make_drafts, run_verify, w4_logits
+from test_gpu_step import block_inputs, check_h, check_stream, check_verify, make_drafts, run_block, run_verify, w4_logits
 
 pytestmark = pytest.mark.gpu
 
@@ -41,6 +41,26 @@ def test_probabilities_of_drafts_where_offsets_descend():
     s["offsets"] = torch.tensor([0, 4, 2, 8, 30, -1, 3], dtype=torch.int32)
     out = run_verify(s, outputs_that_held_something(s))
     assert not torch.any(out.p_draft == 0.25)
+
+
+# ------------------------------------------------------------------ block norm
+def test_block_norm_where_root_and_scale_leave_fp32_together():
+    """1 / rms times the block's scale is beyond fp32 on either side, gate and scale are, and the result is an ordinary number."""
+    d = 640
+    x, r, w, pw, g = block_inputs(6, d, "f32", "token")
+    x[:2] *= 1e-10
+    out = run_block(x[:2], r[:2] * 1e30, w, 1e-6, pw, 1e-24, scale=1e30)
+    check_stream(out.residual, x[:2], r[:2] * 1e30, "f32", pw, 1e-24, scale=1e30)
+    check_h(out.h, out.residual, w, 1e-6)
+    x[2:4] *= 1e30
+    out = run_block(x[2:4], r[2:4] * 1e-28, w, 1e-45, pw, 1e-6, g[2:4], scale=1e-28)
+    check_stream(out.residual, x[2:4], r[2:4] * 1e-28, "f32", pw, 1e-6, g[2:4], scale=1e-28)
+    check_h(out.h, out.residual, w, 1e-45)
+    x[4:] *= 1e20
+    for gate in (g[4:] * 1e-30, g[4:5] * 1e-30):
+        out = run_block(x[4:], r[4:] * 1e20, w, 1e-6, gate=gate, scale=1e30)
+        check_stream(out.residual, x[4:], r[4:] * 1e20, "f32", gate=gate, scale=1e30)
+        check_h(out.h, out.residual, w, 1e-6)
 
 
 # ------------------------------------------------------------------ the product on 4-bit weights
