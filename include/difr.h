@@ -567,7 +567,7 @@ difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t gr
  * The tensor cores add 16 exact products per step and drop low bits there: the tests hold the fp32 sums within (steps + 2)
  * 2^-23 sum |h W| of the exact ones; they lie 4e-6 of their size nearer to zero at d = 4096.  Values below 2^-31 of the
  * largest of their row of h, or whose scale is below 2^-27 of the largest of their id, lose bits below 2^-39 (2^-35) of that
- * largest; scales below 2^-126 count as zero.  The logits of a row of h with a NaN or an infinity are NaN, and so are those of
+ * largest; an id whose scales are all below 2^-126 has logits of zero.  The logits of a row of h with a NaN or an infinity are NaN, and so are those of
  * an id with such a scale.  A row's logits are the same bits whatever other rows the batch holds.
  * `workspace`: 16-byte aligned scratch; calls that may run at the same time need one each.  `device_status` as in difr_out,
  * optional: a wait that runs out also leaves NaN in the place of every logit that was not computed.

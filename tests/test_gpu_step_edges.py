@@ -6,7 +6,8 @@ import torch
 
 import paper_2511_02620_b200 as difr
 import step_reference as ref
-from test_gpu_step import block_inputs, check_h, check_stream, check_verify, make_drafts, run_block, run_verify, w4_logits
+from test_gpu_step import (block_inputs, check_h, check_stream, check_verify, check_w4_logits, make_drafts, randn, random_w4, run_block,
+                           run_verify, w4_logits)
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +85,20 @@ def test_w4_logits_below_the_normal_numbers_are_rounded_once(e):
     for T in (1, 16, 30, 60, 100, 300):
         got = w4_logits(h[:T], W).cpu()
         assert torch.equal(got, want[:T]), T
+
+
+def test_w4_scales_below_the_normal_numbers():
+    """Beside a larger scale of their id they count by their value, alone they count as zero."""
+    T, V, d, group = 20, 200, 96, 32
+    W, _ = random_w4(V, d, group, seed=36)
+    scales = torch.full((V, 8), 0.0)
+    scales[:, 0] = 1.5 * 2.0 ** -126
+    scales[:, 1], scales[:, 2] = 2.0 ** -127, -3 * 2.0 ** -131
+    scales[1::2, 0] = 2.0 ** -128
+    W.scales.copy_(scales.to(torch.bfloat16))
+    h = (randn(T, d, seed=37) * 2.0 ** 60).to(torch.bfloat16)
+    values = ref.w4_values(W.codes.cpu(), W.scales.cpu(), d, group)
+    for rows in (slice(0, T), slice(0, 3)):
+        got = w4_logits(h[rows], W)
+        check_w4_logits(got[:, ::2], h[rows], values[::2])
+        assert torch.all(got[:, 1::2] == 0)
