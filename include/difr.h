@@ -596,7 +596,8 @@ typedef struct {
   int64_t ld;
   int32_t dtype;                /* difr_dtype */
   int32_t max_drafts;           /* largest n_b, 0 .. 255 */
-  const float* draft_probs;     /* [n_drafts, V], row stride ld_draft >= V, nullable; NaN counts as no probability */
+  const float* draft_probs;     /* [n_drafts, V], row stride ld_draft >= V, nullable.  A NaN at the drafted token refuses it; one
+                                   anywhere in the refused draft's row takes all of that id's probability out of r */
   int64_t ld_draft;
   const int32_t* draft_tokens;  /* [n_drafts] */
   const int32_t* offsets;       /* [B + 1], from 0 to n_drafts */

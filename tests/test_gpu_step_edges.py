@@ -102,3 +102,20 @@ def test_w4_scales_below_the_normal_numbers():
         got = w4_logits(h[rows], W)
         check_w4_logits(got[:, ::2], h[rows], values[::2])
         assert torch.all(got[:, 1::2] == 0)
+
+
+def test_a_nan_among_the_drafts_probabilities():
+    """At the drafted token it refuses it, elsewhere in the refused draft's row its id is not sampled; an infinity does the same."""
+    V = 8
+    s = make_drafts(40, 1, V, "f32", True, 1.0, seed=38, ragged=False)
+    s["logits"][:] = 0.0
+    for bad in (math.nan, math.inf):
+        s["probs"][:] = 1e-3  # (as no distribution: every draft is accepted, and 7/8 or more of p is left where not)
+        s["probs"][:20, 3] = bad
+        s["probs"][20:, 5] = bad
+        s["drafted"][:20], s["drafted"][20:] = 3, 1
+        s["accept"][:] = -1
+        s["probs"][20:, 1] = 0.5  # refused by its probability
+        out = check_verify(s, run_verify(s, outputs_that_held_something(s)))
+        assert torch.all(out.n_accepted == 0)
+        assert not torch.any(out.tokens[:20, 0] == 3) and not torch.any(out.tokens[20:, 0] == 5)
