@@ -6,8 +6,8 @@ import torch
 
 import paper_2511_02620_b200 as difr
 import step_reference as ref
-from test_gpu_step import (block_inputs, check_h, check_stream, check_verify, check_w4_logits, make_drafts, randn, random_w4, run_block,
-                           run_verify, w4_logits)
+from test_gpu_step import (DTYPES, block_inputs, check_h, check_stream, check_verify, check_w4_logits, make_drafts, randn, random_w4,
+                           run_block, run_verify, w4_logits)
 
 pytestmark = pytest.mark.gpu
 
@@ -44,6 +44,52 @@ def test_probabilities_of_drafts_where_offsets_descend():
     assert not torch.any(out.p_draft == 0.25)
 
 
+def test_a_nan_among_the_drafts_probabilities():
+    """At the drafted token it refuses it, elsewhere in the refused draft's row its id is not sampled; an infinity does the same."""
+    V = 8
+    s = make_drafts(40, 1, V, "f32", True, 1.0, seed=38, ragged=False)
+    s["logits"][:] = 0.0
+    for bad in (math.nan, math.inf):
+        s["probs"][:] = 1e-3  # (as no distribution: every draft is accepted, and 7/8 or more of p is left where not)
+        s["probs"][:20, 3] = bad
+        s["probs"][20:, 5] = bad
+        s["drafted"][:20], s["drafted"][20:] = 3, 1
+        s["accept"][:] = -1
+        s["probs"][20:, 1] = 0.5  # refused by its probability
+        out = check_verify(s, run_verify(s, outputs_that_held_something(s)))
+        assert torch.all(out.n_accepted == 0)
+        assert not torch.any(out.tokens[:20, 0] == 3) and not torch.any(out.tokens[20:, 0] == 5)
+
+
+def test_more_requests_than_a_grid_holds():
+    """70000 requests, looked at in one call and in two; the last ones against the definition."""
+    B, K, V = 70000, 1, 9
+    g = torch.Generator().manual_seed(32)
+    n = torch.randint(0, K + 1, (B,), generator=g)
+    off = torch.cat([torch.zeros(1, dtype=torch.int64), n.cumsum(0)]).to(torch.int32)
+    D = int(off[-1])
+    words = lambda k: torch.randint(-2 ** 31, 2 ** 31, (k,), generator=g, dtype=torch.int64).to(torch.int32)
+    logits, probs = 2 * torch.randn(D + B, V, generator=g), torch.softmax(2 * torch.randn(D, V, generator=g), 1)
+    s = dict(logits=logits, drafted=torch.randint(0, V, (D,), generator=g).to(torch.int32), offsets=off, accept=words(D), sample=words(B),
+             t=torch.ones(B), K=K, probs=probs)
+
+    def part(b0, b1):
+        o0, o1 = int(off[b0]), int(off[b1])
+        return dict(logits=s["logits"][o0 + b0:o1 + b1], drafted=s["drafted"][o0:o1], offsets=off[b0:b1 + 1] - o0, accept=s["accept"][o0:o1],
+                    sample=s["sample"][b0:b1], t=s["t"][b0:b1], K=K, probs=None if s["probs"] is None else s["probs"][o0:o1])
+
+    for with_probs in (True, False):
+        if not with_probs:
+            s["probs"] = None
+        whole = run_verify(s)
+        for b0, b1 in ((0, 40000), (40000, B)):
+            out = run_verify(part(b0, b1))
+            assert torch.equal(out.tokens, whole.tokens[b0:b1]) and torch.equal(out.n_accepted, whole.n_accepted[b0:b1])
+        assert int(whole.status.abs().max()) == 0
+        check_verify(part(B - 300, B))
+        check_verify(part(65400, 65700))
+
+
 # ------------------------------------------------------------------ block norm
 def test_block_norm_where_root_and_scale_leave_fp32_together():
     """1 / rms times the block's scale is beyond fp32 on either side, gate and scale are, and the result is an ordinary number."""
@@ -62,6 +108,33 @@ def test_block_norm_where_root_and_scale_leave_fp32_together():
         out = run_block(x[4:], r[4:] * 1e20, w, 1e-6, gate=gate, scale=1e30)
         check_stream(out.residual, x[4:], r[4:] * 1e20, "f32", gate=gate, scale=1e30)
         check_h(out.h, out.residual, w, 1e-6)
+
+
+@pytest.mark.parametrize("dtype,d,ld", [("bf16", 1031, 1031), ("bf16", 1030, 1034), ("bf16", 1028, 1036), ("f16", 333, 341), ("f32", 1031, 1033),
+                                        ("f32", 2050, 2050), ("bf16", 70, 71), ("bf16", 9001, 9003)])
+@pytest.mark.parametrize("post", [True, False])
+def test_block_norm_in_place_of_rows_off_16_bytes(dtype, d, ld, post):
+    """The stream over the residual or over x, h over the other one (bf16), rows that go by way of shared memory."""
+    T = 37
+    x, r, w, pw, g = block_inputs(T, d, dtype, "token")
+    kw = dict(post_weight=pw.cuda() if post else None, gate=g.cuda(), scale=0.5)
+    place = lambda t: torch.as_strided(torch.full((T * ld + 8,), -3.0, dtype=t.dtype, device="cuda"), (T, d), (ld, 1)).copy_(t.cuda())
+    def call(stream_over):
+        xs, rs = place(x), place(r)
+        stream = {"apart": torch.as_strided(torch.empty(T * ld, dtype=x.dtype, device="cuda"), (T, d), (ld, 1)), "x": xs, "residual": rs}[stream_over]
+        h = torch.as_strided(torch.empty(T * ld, dtype=torch.bfloat16, device="cuda"), (T, d), (ld, 1))
+        if dtype == "bf16" and stream_over != "apart":
+            h = rs if stream_over == "x" else xs
+        difr.difr_block_norm(xs, rs, w.cuda(), 1e-6, difr.NormOut(h=h, residual=stream), **kw)
+        for t in (xs, rs):
+            assert torch.all(torch.as_strided(t, (T - 1, ld - d), (ld, 1), d) == -3.0)
+        return stream, h
+    stream, h = call("apart")
+    check_stream(stream.contiguous(), x, r, dtype, pw if post else None, 1e-6, g, scale=0.5)
+    check_h(h.contiguous(), stream.contiguous(), w, 1e-6)
+    for over in ("x", "residual"):
+        got = call(over)
+        assert torch.equal(got[0], stream) and torch.equal(got[1], h)
 
 
 # ------------------------------------------------------------------ the product on 4-bit weights
@@ -104,18 +177,26 @@ def test_w4_scales_below_the_normal_numbers():
         assert torch.all(got[:, 1::2] == 0)
 
 
-def test_a_nan_among_the_drafts_probabilities():
-    """At the drafted token it refuses it, elsewhere in the refused draft's row its id is not sampled; an infinity does the same."""
-    V = 8
-    s = make_drafts(40, 1, V, "f32", True, 1.0, seed=38, ragged=False)
-    s["logits"][:] = 0.0
-    for bad in (math.nan, math.inf):
-        s["probs"][:] = 1e-3  # (as no distribution: every draft is accepted, and 7/8 or more of p is left where not)
-        s["probs"][:20, 3] = bad
-        s["probs"][20:, 5] = bad
-        s["drafted"][:20], s["drafted"][20:] = 3, 1
-        s["accept"][:] = -1
-        s["probs"][20:, 1] = 0.5  # refused by its probability
-        out = check_verify(s, run_verify(s, outputs_that_held_something(s)))
-        assert torch.all(out.n_accepted == 0)
-        assert not torch.any(out.tokens[:20, 0] == 3) and not torch.any(out.tokens[20:, 0] == 5)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,d,group,ld", [(300, 10003, 513, 32, 10003), (300, 10003, 513, 64, 10004), (513, 10000, 1030, 128, 10000),
+                                            (513, 10003, 1749, 32, 10008), (300, 10002, 1749, 64, 10003), (300, 10003, 130, 128, 10008),
+                                            (700, 10003, 64, 32, 10008), (513, 10004, 2048, 64, 10008), (257, 10006, 1151, 32, 10008),
+                                            (300, 10001, 4033, 64, 10004)])
+def test_w4_logits_of_tiles_of_256_tokens(T, V, d, group, ld, out):
+    """Enough tiles for every pair of CTAs, so that they are 256 tokens wide: both ways out (rows on 16 bytes or not, ids that
+    end inside 16 bytes), even and odd numbers of steps, a last one of half the length."""
+    W, values = random_w4(V, d, group, seed=V + d)
+    h = randn(T, d, seed=d).to(torch.bfloat16)
+    check_w4_logits(w4_logits(h, W, DTYPES[out], ld), h, values)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("d", [1, 70, 130, 513, 1100, 1749, 2048])
+def test_w4_logits_are_the_same_bits_in_tiles_of_every_width(d, group):
+    """Rows alone and in batches that go through mma.sync (up to 16) and through tiles of 32, 64, 128 and 256 tokens."""
+    V = 10000
+    W, _ = random_w4(V, d, group, seed=34)
+    h = randn(300, d, seed=35).to(torch.bfloat16).cuda()
+    whole = w4_logits(h, W)
+    for t0, t1 in ((0, 1), (299, 300), (5, 13), (100, 116), (3, 23), (250, 282), (40, 100), (17, 145), (0, 299)):
+        assert torch.equal(w4_logits(h[t0:t1], W), whole[t0:t1]), (t0, t1)
