@@ -23,8 +23,8 @@
  *                difr_verify_drafts (drafted tokens against the target's logits, from given random words)
  *   sizes        difr_workspace_bytes, difr_filtered_workspace_bytes, difr_mx_codes_bytes, difr_mx_scales_bytes,
  *                difr_w4_codes_bytes, difr_w4_scales_bytes, difr_w4_workspace_bytes, difr_verify_workspace_bytes
- *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_debug_plan_override,
- *                difr_status_string, difr_version
+ *   aids         difr_logits, difr_philox, difr_selftest_wait, difr_selftest_mx_wait, difr_selftest_w4_wait,
+ *                difr_debug_plan_override, difr_status_string, difr_version
  *
  * Conventions
  *   - Plain C linkage, no exceptions, no global state visible to the caller.
@@ -657,6 +657,13 @@ difr_status difr_selftest_wait(int32_t* status2, int64_t limit_cycles, difr_stre
 difr_status difr_selftest_mx_wait(int32_t format, int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld,
                                   int32_t done_tiles, int64_t limit_cycles, int32_t* device_status,
                                   difr_stream_t stream);
+
+/*
+ * Validation aid (version 311): the same of difr_w4_logits.  Up to 16 tokens a warp has one tile of 32 ids and no other: with
+ * done_tiles > 0 nothing is left to give up.
+ */
+difr_status difr_selftest_w4_wait(int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, int32_t done_tiles,
+                                  int64_t limit_cycles, int32_t* device_status, difr_stream_t stream);
 
 /*
  * Validation aid: overrides the work planner's choices for every later call of the process (0 = the planner's

@@ -25,7 +25,8 @@ EXPORTS = ("difr_workspace_bytes", "difr_filtered_workspace_bytes", "difr_score_
            "difr_mx_logits", "difr_block_norm", "difr_verify_workspace_bytes", "difr_verify_drafts",
            "difr_w4_codes_bytes", "difr_w4_scales_bytes", "difr_w4_quantize", "difr_w4_dequantize", "difr_w4_workspace_bytes",
            "difr_w4_logits",
-           "difr_selftest_wait", "difr_selftest_mx_wait", "difr_debug_plan_override", "difr_status_string", "difr_version")
+           "difr_selftest_wait", "difr_selftest_mx_wait", "difr_selftest_w4_wait",
+           "difr_debug_plan_override", "difr_status_string", "difr_version")
 STATIC_SCRATCH_BYTES = 16 << 20  # DIFR_STATIC_SCRATCH_BYTES
 DIFR_BF16, DIFR_F16, DIFR_F32 = 0, 1, 2
 DIFR_MX8, DIFR_MX4 = 8, 4
@@ -168,6 +169,8 @@ def lib() -> ctypes.CDLL:
         L.difr_verify_drafts.argtypes = [ctypes.POINTER(_CDrafts), i64, i64, i64, ctypes.POINTER(_CDraftsOut), v]
         L.difr_selftest_mx_wait.restype = ctypes.c_int
         L.difr_selftest_mx_wait.argtypes = [i32, i64, i64, i64, v, i32, i64, i32, i64, v, v]
+        L.difr_selftest_w4_wait.restype = ctypes.c_int
+        L.difr_selftest_w4_wait.argtypes = [i64, i64, i64, v, i32, i64, i32, i64, v, v]
         _lib = L
     return _lib
 
@@ -749,6 +752,15 @@ def difr_w4_logits(h, W: W4Tensor, logits, workspace, device_status=None, stream
     _call("difr_w4_logits", device, stream, h.data_ptr(), ldh, W.codes.data_ptr(), W.scales.data_ptr(), W.group, T, d, W.rows,
           logits.data_ptr(), dtype, ld, workspace.data_ptr(), workspace.numel(),
           None if device_status is None else device_status.data_ptr())
+    return logits
+
+
+def difr_selftest_w4_wait(d: int, logits, done_tiles: int, limit_cycles: int, device_status=None, stream=None):
+    """Validation aid: difr_w4_logits' way out where a wait runs out, without a product; see include/difr.h."""
+    dtype, ld, device = _matrix(logits, "logits", _WIDE_DTYPE)
+    _check_status_word(device_status, device)
+    _call("difr_selftest_w4_wait", device, stream, logits.shape[0], d, logits.shape[1], logits.data_ptr(), dtype, ld, done_tiles,
+          limit_cycles, None if device_status is None else device_status.data_ptr())
     return logits
 
 

@@ -68,6 +68,30 @@ bool scales_tmap(CUtensorMap* map, const void* base, int64_t rows, int64_t spitc
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+difr_status w4_product_checks(int64_t T, int64_t d, int64_t V, int32_t dtype, int64_t ld) {
+  if (dtype != DIFR_F32 && dtype != DIFR_BF16) return DIFR_ERR_INVALID_ARG;
+  if (T < 0 || d <= 0 || V <= 0 || ld < V) return DIFR_ERR_INVALID_ARG;
+  if (T > kMaxRows || d > kMaxD || V > kMaxRows || ld > kMaxLd) return DIFR_ERR_SHAPE;
+  return DIFR_OK;
+}
+
+// How a product of T >= 1 tokens is cut up: what of the kernel's parameters the sizes and the logits decide, tokens per tile, grid.
+difr_status w4_plan(int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, int32_t* device_status,
+                    W4LogitsParams* p, int* bn, int* grid) {
+  if (too_many_tiles(T, V, 32)) return DIFR_ERR_SHAPE;
+  int pairs = 0;
+  const difr_status ds = device_pairs(&pairs);
+  if (ds != DIFR_OK) return ds;
+  memset(p, 0, sizeof *p);
+  const int64_t h16_pitch = w4_h16_pitch(d);
+  plan_logit_tiles(T, V, h16_pitch * 2, V * w4_pitch_bytes(d), 32, logits, dtype, ld, device_status, pairs, p, bn, grid);
+  p->d = (int)d; p->h16_pitch = (int)h16_pitch;
+  p->k_steps = (int)((d + 127) / 128);
+  p->half_last = d - (int64_t)(p->k_steps - 1) * 128 <= 64;
+  p->few = T <= kW4Few;
+  return DIFR_OK;
+}
+
 // Records of a row: its vectors, of which the first may begin before the row.
 int64_t verify_chunks(int64_t V, int elem) {
   const int64_t n = 16 / elem;
@@ -170,34 +194,28 @@ size_t difr_w4_workspace_bytes(int64_t T, int64_t d) {
 difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, const void* W_scales, int32_t group, int64_t T,
                            int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, void* workspace,
                            size_t workspace_bytes, int32_t* device_status, difr_stream_t stream) {
-  if (!known_group(group) || (dtype != DIFR_F32 && dtype != DIFR_BF16)) return DIFR_ERR_INVALID_ARG;
-  if (T < 0 || d <= 0 || V <= 0 || ldh < d || ld < V) return DIFR_ERR_INVALID_ARG;
-  if (T > kMaxRows || d > kMaxD || V > kMaxRows || ldh > kMaxLd || ld > kMaxLd) return DIFR_ERR_SHAPE;
+  if (!known_group(group) || ldh < d) return DIFR_ERR_INVALID_ARG;
+  const difr_status st = w4_product_checks(T, d, V, dtype, ld);
+  if (st != DIFR_OK) return st;
+  if (ldh > kMaxLd) return DIFR_ERR_SHAPE;
   if (T == 0) return DIFR_OK;
   if (!h || !W_codes || !W_scales || !logits) return DIFR_ERR_INVALID_ARG;
   if (!aligned_to(h, 2) || !aligned16(W_codes) || !aligned16(W_scales) || !aligned_to(logits, elem_bytes(dtype)) ||
       !aligned_to(device_status, 4) || !aligned16(workspace))
     return DIFR_ERR_ALIGN;
   if (!workspace || workspace_bytes < difr_w4_workspace_bytes(T, d)) return DIFR_ERR_WORKSPACE;
-  if (too_many_tiles(T, V, 32)) return DIFR_ERR_SHAPE;
-  int pairs = 0;
-  const difr_status ds = device_pairs(&pairs);
-  if (ds != DIFR_OK) return ds;
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   W4LogitsParams p;
-  memset(&p, 0, sizeof p);
   int bn = 0, grid = 0;
+  const difr_status plan = w4_plan(T, d, V, logits, dtype, ld, device_status, &p, &bn, &grid);
+  if (plan != DIFR_OK) return plan;
   const int64_t pitch = w4_pitch_bytes(d), h16_pitch = w4_h16_pitch(d);
-  plan_logit_tiles(T, V, h16_pitch * 2, V * pitch, 32, logits, dtype, ld, device_status, pairs, &p, &bn, &grid);
   p.h = static_cast<const __nv_bfloat16*>(h);
   p.scales = static_cast<const __nv_bfloat16*>(W_scales);
   p.token_exp = static_cast<int*>(workspace);
   p.h16 = reinterpret_cast<__half*>(static_cast<char*>(workspace) + w4_exponent_bytes(T));
-  p.ldh = ldh; p.d = (int)d; p.group = group; p.h16_pitch = (int)h16_pitch;
-  p.k_steps = (int)((d + 127) / 128);
+  p.ldh = ldh; p.group = group;
   p.h_vec = vector_rows(h, ldh, DIFR_BF16);
-  p.half_last = d - (int64_t)(p.k_steps - 1) * 128 <= 64;
-  p.few = T <= kW4Few;
   CUtensorMap tw, th, th_last, tout;
   if (p.few) {
     if (!rows_tmap(&tw, W_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, V, pitch, kW4FewIds) || !scales_tmap(&th, W_scales, V, w4_scale_pitch(d, group)))
@@ -213,6 +231,23 @@ difr_status difr_w4_logits(const void* h, int64_t ldh, const void* W_codes, cons
   memset(&tout, 0, sizeof tout);
   if (p.tile_stores && !logits_tmap(&tout, logits, dtype, T, V, ld)) return DIFR_ERR_CUDA;
   return launch_w4_logits(bn, dtype, tw, th, th_last, tout, p, grid, s) == cudaSuccess ? DIFR_OK : DIFR_ERR_CUDA;
+}
+
+difr_status difr_selftest_w4_wait(int64_t T, int64_t d, int64_t V, void* logits, int32_t dtype, int64_t ld, int32_t done_tiles,
+                                  int64_t limit_cycles, int32_t* device_status, difr_stream_t stream) {
+  if (done_tiles < 0 || limit_cycles < 1 || limit_cycles > 1000000000LL) return DIFR_ERR_INVALID_ARG;
+  const difr_status st = w4_product_checks(T, d, V, dtype, ld);
+  if (st != DIFR_OK || T == 0) return st;
+  if (!logits) return DIFR_ERR_INVALID_ARG;
+  if (!aligned_to(logits, elem_bytes(dtype)) || !aligned_to(device_status, 4)) return DIFR_ERR_ALIGN;
+  W4LogitsParams p;
+  int bn = 0, grid = 0;
+  const difr_status plan = w4_plan(T, d, V, logits, dtype, ld, device_status, &p, &bn, &grid);
+  if (plan != DIFR_OK) return plan;
+  return launch_w4_wait_selftest(bn, dtype, p, done_tiles, (long long)limit_cycles, grid, reinterpret_cast<cudaStream_t>(stream)) ==
+                 cudaSuccess
+             ? DIFR_OK
+             : DIFR_ERR_CUDA;
 }
 
 size_t difr_verify_workspace_bytes(int64_t B, int64_t n_drafts, int64_t V) {

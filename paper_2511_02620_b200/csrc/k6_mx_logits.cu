@@ -351,38 +351,6 @@ mx_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
   if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
 }
 
-// The way out of the epilogue after waits that ran out, without a product: a CTA is the eight epilogue warps, its first
-// `done_tiles` tiles count as finished, and the barrier of the next one is never arrived at.  With tiles of 256 tokens one
-// warp of each half sees its barrier complete, so that it is the others that make it give up.
-template <int FMT, int BN, typename OUT>
-__global__ void __launch_bounds__(32 * kMxEpiWarps)
-mx_wait_selftest(const __grid_constant__ MxLogitsParams p, int done_tiles, long long limit_cycles) {
-  __shared__ uint64_t bars[2];  // never complete, complete
-  __shared__ int abort_word;
-  volatile int* abort_flag = &abort_word;
-  if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&bars[0]), 1);
-    mbar_init(smem_u32(&bars[1]), 1);
-    abort_word = 0;
-    mbar_fence_init();
-    mbar_arrive(smem_u32(&bars[1]));
-  }
-  __syncthreads();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int half = warp >> 2, quarter = warp & 3;
-  TileWalk walk(p, blockIdx.x >> 1, gridDim.x >> 1);
-  int vt, tt;
-  for (int k = 0; k <= done_tiles; ++k)
-    if (!walk.next(vt, tt)) return;  // all tiles of the pair are finished, in all of its threads
-  const bool ok = mbar_wait_cta(smem_u32(&bars[BN == 256 && quarter == 1 ? 1 : 0]), 0, false, abort_flag, limit_cycles);
-  __syncwarp();
-  const bool given_up = BN == 256 ? !named_barrier_and(1 + half, 128, ok) : !__all_sync(0xffffffffu, ok);
-  if (given_up)
-    fill_given_up<MxTile<FMT, BN>, OUT>(p, walk, vt, tt, done_tiles & 1, half, (int)(blockIdx.x & 1) * 128 + quarter * 32 + lane);
-  __syncthreads();
-  if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
-}
-
 // ------------------------------------------------------------------ launcher
 template <int FMT, int BN, typename OUT>
 static cudaError_t launch_tile(const CUtensorMap& w, const CUtensorMap& h, const CUtensorMap& hl, const CUtensorMap& sw,
@@ -432,13 +400,12 @@ cudaError_t launch_mx_logits(int fmt, int tokens_per_tile, int dtype, const CUte
 
 template <int FMT, typename OUT>
 static cudaError_t launch_selftest(int bn, const MxLogitsParams& p, int done, long long limit, int grid, cudaStream_t stream) {
-  constexpr int threads = 32 * kMxEpiWarps;
   switch (bn) {
-    case 16: mx_wait_selftest<FMT, 16, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
-    case 32: mx_wait_selftest<FMT, 32, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
-    case 64: mx_wait_selftest<FMT, 64, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
-    case 128: mx_wait_selftest<FMT, 128, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
-    default: mx_wait_selftest<FMT, 256, OUT><<<grid, threads, 0, stream>>>(p, done, limit); break;
+    case 16: logit_wait_selftest<MxTile<FMT, 16>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    case 32: logit_wait_selftest<MxTile<FMT, 32>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    case 64: logit_wait_selftest<MxTile<FMT, 64>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    case 128: logit_wait_selftest<MxTile<FMT, 128>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    default: logit_wait_selftest<MxTile<FMT, 256>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
   }
   return cudaGetLastError();
 }

@@ -308,6 +308,35 @@ __device__ __forceinline__ void tma_load_2d_hint(uint32_t dst_smem, const void* 
       : "memory");
 }
 
+// The first of the ids of lanes 4 g .. 4 g + 3 among the warp's, the others 8 further each.
+__device__ __forceinline__ int few_row(int g) { return ((g & 1) << 2) | (g >> 1); }
+// A lane's logits (ids v, v + 8 ..) on their way out.  Not ok: a wait ran out, they are NaN and copies in flight get time to land.
+template <int NT, typename OUT>
+__device__ __forceinline__ void few_finish(const W4LogitsParams& p, const float (&acc)[kFewTiles][NT][4],
+                                           const int (&id_exp)[2 * kFewTiles], bool ok, int64_t v_first, int t) {
+  if (!ok) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000LL) { }
+    if ((threadIdx.x & 31) == 0 && p.device_status != nullptr) *p.device_status = kStatusTimeout;
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int token = n * 8 + 2 * t + j;
+      if (token < p.T) {
+        const int token_exp = ok ? p.token_exp[token] : 0;
+        OUT* out = static_cast<OUT*>(p.logits) + (int64_t)token * p.ld;
+#pragma unroll
+        for (int r = 0; r < 2 * kFewTiles; ++r) {
+          const int64_t v = v_first + 8 * r;
+          const float value = ok ? acc[r >> 1][n][2 * (r & 1) + j] : __int_as_float(0x7FC00000);
+          if (v < p.V) out[v] = from_float<OUT>(times_power(value, id_exp[r] + token_exp));
+        }
+      }
+    }
+}
+
 // NT: tiles of eight tokens.
 template <int NT, typename OUT>
 __global__ void __launch_bounds__(32 * kFewWarps)
@@ -351,7 +380,7 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
   for (int s = 0; s < kFewStages && s < n_stages; ++s) fetch();
   // ids of this lane's two rows of the MMA: neighbours among the 16 bytes that eight lanes read at once lie in different halves
   // of the swizzled 128-byte lines
-  const int at0 = ((g & 1) << 2) | (g >> 1);
+  const int at0 = few_row(g);
   const int64_t spitch = w4_scale_pitch(p.d, p.group);
   float2 by[2 * kFewTiles];
   int id_exp[2 * kFewTiles];
@@ -465,27 +494,28 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
       take(c, s, std::integral_constant<int, 2>());
     }
   }
-  if (!ok) {  // a wait ran out: what was not computed is NaN; copies in flight get time to land
-    const long long t0 = clock64();
-    while (clock64() - t0 < 2000000LL) { }
-    if (lane == 0 && p.device_status != nullptr) *p.device_status = kStatusTimeout;
+  few_finish<NT, OUT>(p, acc, id_exp, ok, v0 + at0, t);
+}
+
+// What w4_few ends with where a wait runs out, without a product: its warps, the barrier of each never arrived at.
+template <int NT, typename OUT>
+__global__ void __launch_bounds__(32 * kFewWarps)
+w4_few_wait_selftest(const __grid_constant__ W4LogitsParams p, long long limit_cycles) {
+  __shared__ uint64_t bars[kFewWarps];
+  __shared__ int abort_word;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  if (threadIdx.x == 0) abort_word = 0;
+  if (lane == 0) {
+    mbar_init(smem_u32(&bars[warp]), 1);
+    mbar_fence_init();
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int token = n * 8 + 2 * t + j;
-      if (token < p.T) {
-        const int token_exp = p.token_exp[token];
-        OUT* out = static_cast<OUT*>(p.logits) + (int64_t)token * p.ld;
-#pragma unroll
-        for (int r = 0; r < 2 * kFewTiles; ++r) {
-          const int64_t v = v0 + at0 + 8 * r;
-          const float value = ok ? acc[r >> 1][n][2 * (r & 1) + j] : __int_as_float(0x7FC00000);
-          if (v < p.V) out[v] = from_float<OUT>(times_power(value, id_exp[r] + token_exp));
-        }
-      }
-    }
+  __syncthreads();
+  const int64_t v0 = ((int64_t)blockIdx.x * kFewWarps + warp) * kFewIds;
+  if (v0 >= p.V) return;
+  const bool ok = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bars[warp]), 0, false, &abort_word, limit_cycles));
+  const float acc[kFewTiles][NT][4] = {};
+  const int id_exp[2 * kFewTiles] = {};
+  few_finish<NT, OUT>(p, acc, id_exp, ok, v0 + few_row(g), t);
 }
 
 // ------------------------------------------------------------------ more tokens
@@ -925,6 +955,31 @@ cudaError_t launch_w4_few(int dtype, const CUtensorMap& w, const CUtensorMap& s,
   if (dtype == kBf16)
     return p.T <= 8 ? launch_few<1, __nv_bfloat16>(w, s, p, stream) : launch_few<2, __nv_bfloat16>(w, s, p, stream);
   return p.T <= 8 ? launch_few<1, float>(w, s, p, stream) : launch_few<2, float>(w, s, p, stream);
+}
+
+template <typename OUT>
+static cudaError_t launch_selftest(int bn, const W4LogitsParams& p, int done, long long limit, int grid, cudaStream_t stream) {
+  if (p.few) {
+    if (done > 0) return cudaSuccess;  // (a warp has one tile)
+    const int few_grid = (int)((p.V + (int64_t)kFewIds * kFewWarps - 1) / (kFewIds * kFewWarps));
+    if (p.T <= 8)
+      w4_few_wait_selftest<1, OUT><<<few_grid, 32 * kFewWarps, 0, stream>>>(p, limit);
+    else
+      w4_few_wait_selftest<2, OUT><<<few_grid, 32 * kFewWarps, 0, stream>>>(p, limit);
+    return cudaGetLastError();
+  }
+  switch (bn) {
+    case 32: logit_wait_selftest<W4Tile<32>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    case 64: logit_wait_selftest<W4Tile<64>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    case 128: logit_wait_selftest<W4Tile<128>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+    default: logit_wait_selftest<W4Tile<256>, OUT><<<grid, kLogitEpiThreads, 0, stream>>>(p, done, limit); break;
+  }
+  return cudaGetLastError();
+}
+cudaError_t launch_w4_wait_selftest(int tokens_per_tile, int dtype, const W4LogitsParams& p, int done_tiles,
+                                    long long limit_cycles, int grid, cudaStream_t stream) {
+  return dtype == kBf16 ? launch_selftest<__nv_bfloat16>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream)
+                        : launch_selftest<float>(tokens_per_tile, p, done_tiles, limit_cycles, grid, stream);
 }
 
 }  // namespace difr

@@ -148,4 +148,37 @@ __device__ __forceinline__ void fill_given_up(const LogitTiles& p, TileWalk& wal
   } while (walk.next(vt, tt));
 }
 
+// The way out of the epilogue after waits that ran out, without a product: a CTA is the eight epilogue warps, its first
+// `done_tiles` tiles count as finished, and the barrier of the next one is never arrived at.  With tiles of 256 tokens one
+// warp of each half sees its barrier complete, so that it is the others that make it give up.
+constexpr int kLogitEpiThreads = 256;
+template <typename Tl, typename OUT>
+__global__ void __launch_bounds__(kLogitEpiThreads)
+logit_wait_selftest(const __grid_constant__ LogitTiles p, int done_tiles, long long limit_cycles) {
+  __shared__ uint64_t bars[2];  // never complete, complete
+  __shared__ int abort_word;
+  volatile int* abort_flag = &abort_word;
+  if (threadIdx.x == 0) {
+    mbar_init(smem_u32(&bars[0]), 1);
+    mbar_init(smem_u32(&bars[1]), 1);
+    abort_word = 0;
+    mbar_fence_init();
+    mbar_arrive(smem_u32(&bars[1]));
+  }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int half = warp >> 2, quarter = warp & 3;
+  TileWalk walk(p, blockIdx.x >> 1, gridDim.x >> 1);
+  int vt, tt;
+  for (int k = 0; k <= done_tiles; ++k)
+    if (!walk.next(vt, tt)) return;  // all tiles of the pair are finished, in all of its threads
+  const bool ok = mbar_wait_cta(smem_u32(&bars[Tl::tokens == 256 && quarter == 1 ? 1 : 0]), 0, false, abort_flag, limit_cycles);
+  __syncwarp();
+  const bool given_up = Tl::tokens == 256 ? !named_barrier_and(1 + half, 128, ok) : !__all_sync(0xffffffffu, ok);
+  if (given_up)
+    fill_given_up<Tl, OUT>(p, walk, vt, tt, done_tiles & 1, half, (int)(blockIdx.x & 1) * 128 + quarter * 32 + lane);
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag && p.device_status != nullptr) *p.device_status = kStatusTimeout;
+}
+
 }  // namespace difr

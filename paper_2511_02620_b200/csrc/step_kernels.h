@@ -61,6 +61,9 @@ cudaError_t launch_w4_few(int dtype, const CUtensorMap& w, const CUtensorMap& s,
 cudaError_t launch_w4_logits(int tokens_per_tile, int dtype, const CUtensorMap& w, const CUtensorMap& h,
                              const CUtensorMap& h_last, const CUtensorMap& out, const W4LogitsParams& p, int grid,
                              cudaStream_t stream);
+// Validation aid: how the product of `p` ends where a wait runs out; nothing is computed.
+cudaError_t launch_w4_wait_selftest(int tokens_per_tile, int dtype, const W4LogitsParams& p, int done_tiles,
+                                    long long limit_cycles, int grid, cudaStream_t stream);
 
 struct VerifyParams {
   const void* logits;            // [n_drafts + B][ld]

@@ -200,3 +200,43 @@ def test_w4_logits_are_the_same_bits_in_tiles_of_every_width(d, group):
     whole = w4_logits(h, W)
     for t0, t1 in ((0, 1), (299, 300), (5, 13), (100, 116), (3, 23), (250, 282), (40, 100), (17, 145), (0, 299)):
         assert torch.equal(w4_logits(h[t0:t1], W), whole[t0:t1]), (t0, t1)
+
+
+@pytest.mark.parametrize("T,V,d,ld,out", [(1, 5003, 96, 5003, "f32"), (16, 9800, 300, 9808, "bf16"), (20, 50000, 96, 50000, "bf16"),
+                                          (40, 9800, 96, 9803, "bf16"), (300, 1100, 160, 1104, "f32"), (600, 9800, 160, 9800, "bf16"),
+                                          (600, 9801, 160, 9801, "f32"), (2700, 9800, 40000, 9800, "bf16")])
+def test_w4_logits_that_a_wait_keeps_from_being_computed_are_nan(T, V, d, ld, out):
+    """The way out of either kernel after waits that ran out, at every tile width: all logits but those of the finished tiles are
+    NaN, the status word says so, and the next call is as good as ever."""
+    buf = torch.full((T + 1, ld), -7.0, dtype=DTYPES[out], device="cuda")
+    part = buf[:T, :V]
+    few = T <= 16
+    width = 16 if few else 256 if T > 128 and (V + 255) // 256 * ((T + 255) // 256) > 37 else 128 if T > 64 else 64 if T > 32 else 32
+    left = []
+    for done in (0, 1, 2, 3, 1000):
+        buf.fill_(-7.0)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        difr.difr_selftest_w4_wait(d, part, done, 1_000_000, status)
+        nan = torch.isnan(part)
+        assert int(status.item()) == (-7 if bool(nan.any()) else 0)
+        assert torch.all(part[~nan] == -7.0)
+        assert torch.all(buf[:T, V:] == -7.0) and torch.all(buf[T:] == -7.0)
+        left.append(~nan)
+        buf.fill_(-7.0)
+        difr.difr_selftest_w4_wait(d, part, done, 1_000_000)  # no status word: the logits tell
+        assert torch.equal(torch.isnan(part), nan)
+    assert not left[0].any() and left[-1].all()
+    for less, more in zip(left, left[1:]):
+        new = more & ~less
+        assert not (less & ~more).any()
+        if few:
+            assert more.all()
+            continue
+        # whole tiles, at most one for every pair of the 74
+        pad = lambda x: torch.nn.functional.pad(x, (0, -V % 256, 0, -T % width)).view(-1, width, (V + 255) // 256, 256)
+        tiles = pad(new).any(3).any(1)
+        assert more.all() or int(tiles.sum()) <= 74
+        assert torch.equal(pad(new), pad(torch.ones_like(new)) & tiles.view(-1, 1, tiles.shape[1], 1))
+    W, values = random_w4(1000, 96, 32, seed=39)
+    h = randn(T, 96, seed=40).to(torch.bfloat16)
+    check_w4_logits(w4_logits(h, W), h, values)
