@@ -11,8 +11,8 @@ SOURCES = ["difr_api.cu", "difr_mx_api.cu", "k0_expand_seeds.cu", "k1_fused_scor
            "k2_filtered.cu", "k2_select.cu", "k3_detect.cu", "k4_norm.cu", "k5_mx_convert.cu", "k6_mx_logits.cu",
            "difr_step_api.cu", "k7_block_norm.cu", "k8_w4_convert.cu", "k9_w4_logits.cu",
            "k10_verify.cu"]
-HEADERS = ["difr_device.cuh", "difr_host.h", "difr_kernels.h", "difr_plan.h", "mx_device.cuh", "mx_kernels.h", "norm_device.cuh", "logit_plan.h", "logit_tiles.cuh",
-           "step_kernels.h", "w4_device.cuh",
+HEADERS = ["difr_device.cuh", "difr_host.h", "difr_kernels.h", "difr_plan.h", "mx_device.cuh", "mx_kernels.h",
+           "norm_device.cuh", "logit_plan.h", "logit_tiles.cuh", "step_kernels.h", "w4_device.cuh",
            os.path.join("..", "..", "include", "difr.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC", "--threads", "0"]

@@ -1,4 +1,5 @@
-// C ABI of a decoding step's operators: block norm, 4-bit weights with group scales, verification of drafted tokens.  Argument checks and launches; nothing here computes.
+// C ABI of a decoding step's operators: block norm, 4-bit weights with group scales, verification of drafted tokens.
+// Argument checks and launches; nothing here computes.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <math.h>

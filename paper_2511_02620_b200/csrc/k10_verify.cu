@@ -595,7 +595,6 @@ __global__ void __launch_bounds__(kSumThreads) draft_pick(const VerifyParams p) 
   if (lane == 0 && from < to) *token = at;
 }
 
-template <typename X>
 static cudaError_t launch_next(void (*kernel)(const VerifyParams), dim3 grid, int threads, const VerifyParams& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof cfg);
@@ -615,7 +614,7 @@ template <typename X>
 static cudaError_t launch_typed(const VerifyParams& p, cudaStream_t stream) {
   draft_rows<X><<<dim3((unsigned)(p.n_drafts + p.B), (unsigned)p.chunks), kRowThreads, 0, stream>>>(p);
   cudaError_t e = cudaGetLastError();
-  if (e == cudaSuccess) e = launch_next<X>(draft_merge<X>, dim3((unsigned)p.B), kMergeThreads, p, stream);
+  if (e == cudaSuccess) e = launch_next(draft_merge<X>, dim3((unsigned)p.B), kMergeThreads, p, stream);
   if (p.temperatures == nullptr && p.temperature == 0.f) return e;  // greedy: done
   const unsigned chunks = (unsigned)((p.V + kSumIds - 1) / kSumIds);
   // (a grid's second dimension holds 65535: requests beyond that in further launches)
@@ -623,10 +622,10 @@ static cudaError_t launch_typed(const VerifyParams& p, cudaStream_t stream) {
     VerifyParams q = p;
     q.first_request = b0;
     const dim3 grid(chunks, (unsigned)(p.B - b0 < 65535 ? p.B - b0 : 65535));
-    if (p.probs != nullptr) e = launch_next<X>(draft_sums<X, false>, grid, kSumThreads, q, stream);
-    if (e == cudaSuccess) e = launch_next<X>(draft_sums<X, true>, grid, kSumThreads, q, stream);
+    if (p.probs != nullptr) e = launch_next(draft_sums<X, false>, grid, kSumThreads, q, stream);
+    if (e == cudaSuccess) e = launch_next(draft_sums<X, true>, grid, kSumThreads, q, stream);
   }
-  if (e == cudaSuccess) e = launch_next<X>(draft_pick<X>, dim3((unsigned)p.B), kSumThreads, p, stream);
+  if (e == cudaSuccess) e = launch_next(draft_pick<X>, dim3((unsigned)p.B), kSumThreads, p, stream);
   return e;
 }
 
