@@ -240,3 +240,51 @@ def test_w4_logits_that_a_wait_keeps_from_being_computed_are_nan(T, V, d, ld, ou
     W, values = random_w4(1000, 96, 32, seed=39)
     h = randn(T, 96, seed=40).to(torch.bfloat16)
     check_w4_logits(w4_logits(h, W), h, values)
+
+# ------------------------------------------------------------------ calls at the same time
+def test_calls_on_two_streams_at_once():
+    """Each operator many times on two streams, outputs and workspaces apart, the other stream busy with the other ones: the same
+    results as alone."""
+    V, d, group = 20000, 1030, 64
+    W, _ = random_w4(V, d, group, seed=41)
+    h = randn(300, d, seed=42).to(torch.bfloat16).cuda()
+    x, r, w, pw, g = (t.cuda() for t in block_inputs(300, d, "bf16", "token"))
+    s = make_drafts(40, 4, 3001, "bf16", True, 0.9, seed=43)
+    dev = {k: v.cuda() if isinstance(v, torch.Tensor) else v for k, v in s.items()}
+    D = s["drafted"].numel()
+
+    def calls():
+        """(a call on a stream, its outputs) of each operator, buffers of its own."""
+        for T in (1, 16, 40, 100, 300):
+            logits = torch.empty(T, V, device="cuda")
+            ws = torch.empty(difr.difr_w4_workspace_bytes(T, d), dtype=torch.uint8, device="cuda")
+            yield (lambda st, T=T, l=logits, ws=ws: difr.difr_w4_logits(h[:T], W, l, ws, stream=st)), [logits]
+        o = difr.NormOut(h=torch.empty_like(x), residual=torch.empty_like(x))
+        yield (lambda st: difr.difr_block_norm(x, r, w, 1e-6, o, post_weight=pw, gate=g, stream=st)), [o.h, o.residual]
+        q = difr.W4Tensor.allocate(300, d, group)
+        yield (lambda st: difr.difr_w4_quantize(x, q, stream=st)), [q.codes, q.scales]
+        v = difr.DraftOut.allocate(40, D, 4, 3001)
+        yield (lambda st: difr.difr_verify_drafts(dev["logits"], dev["drafted"], dev["offsets"], dev["accept"], dev["sample"], 0.9, v,
+                                                  draft_probs=dev["probs"], stream=st)), [v.tokens, v.n_accepted, v.p_draft]
+
+    alone = []
+    for call, outs in calls():
+        call(None)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in outs])
+    sides = [list(calls()), list(calls())[::-1]]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for side in sides:
+        for _, outs in side:
+            for t in outs:
+                t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for k in range(len(sides[0])):
+            for side, st in zip(sides, streams):
+                side[k][0](st)
+    torch.cuda.synchronize()
+    for side, want in ((sides[0], alone), (sides[1], alone[::-1])):
+        for (_, outs), expected in zip(side, want):
+            for t, e in zip(outs, expected):
+                assert torch.equal(t, e)
