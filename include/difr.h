@@ -552,7 +552,8 @@ difr_status difr_block_norm(const void* x, int64_t ldx, const void* residual, in
  * scale NaN and zero codes: all its values are NaN, and so are the logits of its id.  (Codes of -8 and scales of either sign
  * come from other quantisers only.)
  * difr_w4_dequantize: DIFR_F32 exact, DIFR_BF16 rounded (a product has up to eleven bits), where it does not leave the
- * normal numbers.
+ * normal numbers.  The bf16 values are another head than the codes': scoring calls, which take bf16 heads, do not replay a
+ * 4-bit one bit for bit.
  */
 size_t difr_w4_codes_bytes(int64_t rows, int64_t d);                /* 0 for sizes the library rejects, as for the */
 size_t difr_w4_scales_bytes(int64_t rows, int64_t d, int32_t group); /* microscaled formats, or an unknown group    */
@@ -565,10 +566,11 @@ difr_status difr_w4_dequantize(const void* codes, const void* scales, int32_t gr
  * logits[t, v] = h[t, :] . W[v, :] with h bf16 [T, d] (row stride ldh >= d) and W [V, d] in 4 bits, accumulated in fp32;
  * `logits` [T, V] (row stride ld >= V elements) is DIFR_F32 or DIFR_BF16.  Any T from 1, any V from 1, any d.
  * The tensor cores add 16 exact products per step and drop low bits there: the tests hold the fp32 sums within (steps + 2)
- * 2^-23 sum |h W| of the exact ones; they lie 4e-6 of their size nearer to zero at d = 4096.  Values below 2^-31 of the
- * largest of their row of h, or whose scale is below 2^-27 of the largest of their id, lose bits below 2^-39 (2^-35) of that
- * largest; an id whose scales are all below 2^-126 has logits of zero.  The logits of a row of h with a NaN or an infinity are NaN, and so are those of
- * an id with such a scale.  A row's logits are the same bits whatever other rows the batch holds.
+ * 2^-23 sum |h W| of the exact ones; they lie 3e-6 of their size nearer to zero at d = 4096, 6e-6 at 8192 (those of
+ * difr_logits 4e-6 and 8e-6).  Values below 2^-31 of the largest of their row of h, or whose scale is below 2^-27 of the
+ * largest of their id, lose bits below 2^-39 (2^-35) of that largest; an id whose scales are all below 2^-126 has logits of
+ * zero.  The logits of a row of h with a NaN or an infinity are NaN, and so are those of an id with such a scale.  A row's
+ * logits are the same bits whatever other rows the batch holds.
  * `workspace`: 16-byte aligned scratch; calls that may run at the same time need one each.  `device_status` as in difr_out,
  * optional: a wait that runs out also leaves NaN in the place of every logit that was not computed.
  */

@@ -17,16 +17,22 @@
 // give the same bits (an MMA adds the same sixteen products in either).
 //
 // Up to 16 tokens, `w4_few`: a warp takes 32 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, two
-// stages of two steps ahead, and meets nobody.  One token x 128256 x 4096 takes 64 us (43 of bytes), 16 tokens 81; a step of 16
-// ids is 167 instructions, 13 of them for each word of codes that becomes fp16.  (The other kernel took 115 for one token.)
+// stages of two steps ahead, and meets nobody.  One token x 128256 x 4096 takes 62 to 64 us (43 of bytes), 16 tokens 80; a step
+// of 16 ids is 167 instructions, 13 of them for each word of codes that becomes fp16.  (The other kernel takes 104 for one token.)
 //
 // More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
 // run as persistent pairs (cta_group::2) on tiles of 256 ids x BN tokens: each CTA loads and converts its own 128 ids and loads
 // half of the tile's tokens, and the pair's first CTA issues the MMAs.  A step is 128 values of k: 64 TMEM columns of
 // converted weights (a slot), a stage of h; a stage of codes is two steps.  TMEM: two accumulators and the slots; with BN =
-// 256 the accumulators overlap by 128 columns, which the epilogue reads first.  4096 tokens x 128256 x 4096 take 2730 us in
-// short runs (1.57 PFLOP/s), 3117 sustained under the power cap (1.38); 64 tokens 114, which is about 1000 clocks at 1965 MHz for each step of seven tiles.  Which of conversion, TMEM store
-// and MMA sets that was not measured.
+// 256 the accumulators overlap by 128 columns, which the epilogue reads first.  4096 tokens x 128256 x 4096 take 2700 us in
+// short runs (1.59 PFLOP/s), 2950 to 3150 sustained under the power cap (1.37 to 1.46); 64 tokens 109 to 115, which is about 1000
+// clocks at 1965 MHz for each step of seven tiles.  Warps issue in 51 of 100 cycles then, DRAM is at 29 %: the chain of a step
+// sets the time, of which no link was measured by itself.
+//
+// The tensor cores drop what lies below an accumulator's last bit, towards zero: logits lose 3e-6 of their size at d = 4096.  Parts of
+// 1024 (2048) values added in fp32 bring that to 7e-7 (1.4e-6) at every d.  It was built, with the sums of a tile of 256 tokens in
+// shared memory, and left out: 4096 tokens x 128256 x 4096 to bf16 3250 us with parts of 2048 for 3020, 777 x 32003 x 1749 to fp32
+// 137 for 111 with parts of 1024, one token 66 for 62.
 // Warps: 0 TMA of h, 1 MMA, 2 TMEM allocation, 3 TMA of codes, 4..11 epilogue (two per lane quarter, half of the tile's columns
 // each), 12..19 conversion (two per lane quarter, even and odd steps).
 //
