@@ -34,7 +34,7 @@
 // shared memory, and left out: 4096 tokens x 128256 x 4096 to bf16 3250 us with parts of 2048 for 3020, 777 x 32003 x 1749 to fp32
 // 137 for 111 with parts of 1024, one token 66 for 62.
 // Warps: 0 TMA of h, 1 MMA, 2 TMEM allocation, 3 TMA of codes, 4..11 epilogue (two per lane quarter, half of the tile's columns
-// each), 12..19 conversion (two per lane quarter, even and odd steps).
+// each), 12..19 conversion (two per lane quarter, even and odd steps, counted on from tile to tile).
 //
 // The order of k.  In mma.sync lane t of four holds, of a block of 128 values, the 32 at 32 t, four words, and an MMA adds pairs
 // q = 0 and 1, or 2 and 3, of all four lanes' words w.  TMEM columns and h follow that: pair q of word w of lane t is column
@@ -83,6 +83,7 @@ struct W4Tile {
   static constexpr int shared_loads = shared_cols / (2 * chunk);
   static_assert(c_stages >= 3 && slots >= 2, "pipeline depth");
   static_assert((slots & (slots - 1)) == 0, "steps are counted modulo 2^32");
+  static_assert(slots >= 2, "the steps of a conversion warp are two apart");
 };
 
 // Instruction descriptor: dense, fp32 accumulator, fp16 A and B, both K-major.
@@ -731,15 +732,18 @@ w4_logits(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CU
       const int v = min(vt * kLogitPairM + (int)cta * 128 + r, p.V - 1);
       const __nv_bfloat16* scales = p.scales + (int64_t)v * spitch;
       const float2 by = scale_factors(scale_exponent(fold_row(scales, 0, 1, (int)(spitch / 8), 0u)));
-      uint2 raw = odd < p.k_steps ? load_step_scales(scales, odd, p.group) : make_uint2(0u, 0u);
+      // The steps of a warp are two apart, from tile to tile as well: a wait for a slot tells its phases apart only while this warp
+      // knows the phase before the awaited one to be complete, from its own last wait, and with two slots that is two steps back.
+      const int first = odd ^ (int)(step0 & 1u);
+      uint2 raw = first < p.k_steps ? load_step_scales(scales, first, p.group) : make_uint2(0u, 0u);
       for (int k = 0; k < c_steps; ++k) {
-        const int step = 2 * k + odd;
+        const int step = 2 * k + first;
         if (!__all_sync(0xffffffffu, mbar_wait_cta(c_full(stage), phase, false, abort_flag))) { ok = false; break; }
         if (step < p.k_steps) {
           const uint32_t from = row_smem + (uint32_t)(stage * kW4CodeBytes);
           uint4 c[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(odd * 4 + j)) ^ swizzle) << 4));
+          for (int j = 0; j < 4; ++j) c[j] = ld_shared_16(from + ((((uint32_t)(first * 4 + j)) ^ swizzle) << 4));
           const bool half_step = p.half_last && step == p.k_steps - 1;
           uint2 here = spread_step_scales(raw, p.group);
           if (step + 2 < p.k_steps) raw = load_step_scales(scales, step + 2, p.group);

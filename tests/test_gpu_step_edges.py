@@ -202,6 +202,20 @@ def test_w4_logits_are_the_same_bits_in_tiles_of_every_width(d, group):
         assert torch.equal(w4_logits(h[t0:t1], W), whole[t0:t1]), (t0, t1)
 
 
+@pytest.mark.parametrize("out,ld", [("f32", 20009), ("f32", 20012), ("bf16", 20016)])
+@pytest.mark.parametrize("d", [274, 384, 600, 1100])
+def test_w4_logits_of_an_odd_number_of_steps(d, out, ld):
+    """3, 3, 5 and 9 steps of 128 values in tiles of 256 tokens, three tiles and more a pair of CTAs: the steps of one tile follow
+    those of another through two slots of converted weights.  Right, and the same bits every time."""
+    T, V = 519, 20001
+    W, values = random_w4(V, d, 32, seed=d)
+    h = randn(T, d, seed=44).to(torch.bfloat16).cuda()
+    got = w4_logits(h, W, DTYPES[out], ld)
+    check_w4_logits(got[:, ::7], h, values[::7])
+    for _ in range(25):
+        assert torch.equal(w4_logits(h, W, DTYPES[out], ld), got)
+
+
 @pytest.mark.parametrize("T,V,d,ld,out", [(1, 5003, 96, 5003, "f32"), (16, 9800, 300, 9808, "bf16"), (20, 50000, 96, 50000, "bf16"),
                                           (40, 9800, 96, 9803, "bf16"), (300, 1100, 160, 1104, "f32"), (600, 9800, 160, 9800, "bf16"),
                                           (600, 9801, 160, 9801, "f32"), (2700, 9800, 40000, 9800, "bf16")])
