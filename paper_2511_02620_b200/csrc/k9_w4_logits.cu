@@ -416,8 +416,9 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
   float acc[kFewTiles][NT][4] = {};
   const __half2 minus24 = __float2half2_rn(-24.f);
   const ConvertBits k = convert_bits();
-  // One step: codes and scales of this lane's ids, and h, of which `words` words are there.
-  auto take = [&](const uint4 (&c)[2 * kFewTiles], const uint32_t (&s)[2 * kFewTiles], auto words) {
+  // One step: codes and scales of this lane's ids, and h, of which `words` words are there.  `between`: called behind the first of
+  // the tiles.
+  auto take = [&](const uint4 (&c)[2 * kFewTiles], const uint32_t (&s)[2 * kFewTiles], auto words, auto between) {
     constexpr int W = decltype(words)::value;
     uint4 b[NT][W];
 #pragma unroll
@@ -443,8 +444,10 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
           mma_f16(acc[m][n], a[2], a8[2], a[3], a8[3], b[n][w].z, b[n][w].w);
         }
       }
+      if (m == 0) between();
     }
   };
+  auto nothing = []() {};
   // of a stage: the line of this lane's first id (the others 8 lines further each), 16 bytes for each of eight chunks of 32
   // codes; of a slot of scales its first id's
   const uint32_t line = code_ring + (uint32_t)(at0 * 128), swizzle = (uint32_t)at0;
@@ -461,6 +464,7 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
       s[r] = ld_shared_2(y + 128u * (uint32_t)r);
     }
   };
+  const uint32_t none = (uint32_t)p.h16_pitch & 63u;  // 0, which the compiler does not know: rows of h16 are whole 64 values
   bool ok = true;
   const int whole = (p.k_steps - (p.half_last ? 1 : 0)) / 2;  // stages of two whole steps
   int slot = 0;
@@ -470,14 +474,25 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
     if (!ok) break;
     const uint32_t from = line + (uint32_t)(slot * kFewStageBytes);
     load(from, t, (uint32_t)(8 * i + t));
-    take(c, s, std::integral_constant<int, 4>());
+    take(c, s, std::integral_constant<int, 4>(), nothing);
     load(from, t + 4, (uint32_t)(8 * i + 4 + t));
-    // The stage is read and may be filled again: __syncwarp orders all lanes' reads before lane 0's arrival in fetch(), which
-    // releases them, so that it waits for loads under way, and the copy goes out behind it.  (With a barrier of its own that
-    // every lane arrives at, one token took 65.3 us instead of 63.0; with the refill behind take(), 65.8, 16 tokens 96 for 80.)
-    __syncwarp();
-    if (next < n_stages) fetch();
-    take(c, s, std::integral_constant<int, 4>());
+    // The stage may be filled again once all lanes' reads of it have returned.  Nothing but their values shows that here: the
+    // arrival in fetch() is waited for by nobody, and a read held up behind others of its SM can be overtaken by a copy from L2.
+    // So the refill hangs on a vote over what was read.  With one tile of tokens it waits until half of that has been worked on,
+    // so that nothing waits for the reads (one token 63.5 us, 69.8 with the vote right behind them); with two the reads have
+    // returned by then anyway, and the loop is better in one piece (16 tokens 82 us, 94 the other way).
+    auto refill = [&]() {
+      uint32_t seen = 0;
+#pragma unroll
+      for (int r = 0; r < 2 * kFewTiles; ++r) seen |= c[r].x | s[r];
+      if (__all_sync(0xffffffffu, (seen & none) == 0u) && next < n_stages) fetch();
+    };
+    if constexpr (NT == 1) {
+      take(c, s, std::integral_constant<int, 4>(), refill);
+    } else {
+      refill();
+      take(c, s, std::integral_constant<int, 4>(), nothing);
+    }
     if (++slot == kFewStages) { slot = 0; phase ^= 1u; }
   }
   if (ok && whole < n_stages) {  // a whole step, a half one, or both
@@ -486,7 +501,7 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
     int step = 2 * whole;
     if (ok && step < p.k_steps - (p.half_last ? 1 : 0)) {
       load(from, t, (uint32_t)(4 * step + t));
-      take(c, s, std::integral_constant<int, 4>());
+      take(c, s, std::integral_constant<int, 4>(), nothing);
       ++step;
     }
     if (ok && step < p.k_steps) {  // lanes t and t + 1 share a chunk, eight bytes each
@@ -498,7 +513,7 @@ w4_few(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUten
           c[r].y = c[r].w;
         }
       }
-      take(c, s, std::integral_constant<int, 2>());
+      take(c, s, std::integral_constant<int, 2>(), nothing);
     }
   }
   few_finish<NT, OUT>(p, acc, id_exp, ok, v0 + at0, t);

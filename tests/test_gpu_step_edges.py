@@ -216,6 +216,28 @@ def test_w4_logits_of_an_odd_number_of_steps(d, out, ld):
         assert torch.equal(w4_logits(h, W, DTYPES[out], ld), got)
 
 
+@pytest.mark.parametrize("V,d,group", [(118775, 3730, 64), (110387, 2252, 64), (128256, 4096, 128), (60000, 8000, 32)])
+def test_w4_logits_of_few_tokens_are_the_same_bits_in_every_call(V, d, group):
+    """Hundreds of calls of 1 to 16 tokens, with weights from L2 and from memory and other work between: the bits of the tiles."""
+    g = torch.Generator(device="cuda").manual_seed(45)
+    W = difr.difr_w4_quantize(torch.randn(V, d, generator=g, device="cuda") * d ** -0.5, difr.W4Tensor.allocate(V, d, group))
+    h = torch.randn(40, d, generator=g, device="cuda").to(torch.bfloat16)
+    run = lambda x: difr.difr_w4_logits(x, W, torch.empty(x.shape[0], V, device="cuda"),
+                                        torch.empty(difr.difr_w4_workspace_bytes(x.shape[0], d), dtype=torch.uint8, device="cuda"))
+    whole = run(h)
+    other = torch.zeros(64 << 20, device="cuda")
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(600):
+        n = (1, 5, 8, 3, 16, 12)[i % 6]
+        at = i * 7 % (41 - n)
+        wrong += (run(h[at:at + n]) != whole[at:at + n]).sum()
+        if i % 10 == 0:
+            other += 1
+        if i % 10 == 5:
+            wrong += (run(h) != whole).sum()
+    assert int(wrong) == 0
+
+
 @pytest.mark.parametrize("T,V,d,ld,out", [(1, 5003, 96, 5003, "f32"), (16, 9800, 300, 9808, "bf16"), (20, 50000, 96, 50000, "bf16"),
                                           (40, 9800, 96, 9803, "bf16"), (300, 1100, 160, 1104, "f32"), (600, 9800, 160, 9800, "bf16"),
                                           (600, 9801, 160, 9801, "f32"), (2700, 9800, 40000, 9800, "bf16")])
