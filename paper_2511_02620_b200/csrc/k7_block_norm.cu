@@ -7,7 +7,7 @@
 //
 // One pass over the row, as in the final norm: x stays in registers as it lies in memory, becomes r there, and r stays for
 // the second norm.  The residual and a gate are loaded together with x, so that their bytes are in flight while the first
-// sum is taken.  Bound by its bytes: 65536 x 2048 in bf16 with a gate per channel 213 us (166 of bytes).  Sums, their order and
+// sum is taken.  Bound by its bytes: 65536 x 2048 in bf16 with a gate per channel 204 to 215 us (166 of bytes).  Sums, their order and
 // the handling of rows at the ends of fp32 are the final norm's.
 #include <cuda_runtime.h>
 

@@ -17,7 +17,7 @@
 // give the same bits (an MMA adds the same sixteen products in either).
 //
 // Up to 16 tokens, `w4_few`: a warp takes 32 ids along all of k with mma.sync.  It brings its own codes and scales by TMA, two
-// stages of two steps ahead, and meets nobody.  One token x 128256 x 4096 takes 62 to 64 us (43 of bytes), 16 tokens 80; a step
+// stages of two steps ahead, and meets nobody.  One token x 128256 x 4096 takes 62 to 64 us (43 of bytes), 16 tokens 84; a step
 // of 16 ids is 167 instructions, 13 of them for each word of codes that becomes fp16.  (The other kernel takes 104 for one token.)
 //
 // More tokens, `w4_logits`: tcgen05.mma takes its A operand from TMEM, where the converted weights go; a lane is an id.  CTAs
@@ -26,7 +26,7 @@
 // converted weights (a slot), a stage of h; a stage of codes is two steps.  TMEM: two accumulators and the slots; with BN =
 // 256 the accumulators overlap by 128 columns, which the epilogue reads first.  4096 tokens x 128256 x 4096 take 2700 us in
 // short runs (1.59 PFLOP/s), 2950 to 3150 sustained under the power cap (1.37 to 1.46); 64 tokens 109 to 115, which is about 1000
-// clocks at 1965 MHz for each step of seven tiles.  Warps issue in 51 of 100 cycles then, DRAM is at 29 %: the chain of a step
+// clocks at 1965 MHz for each step of seven tiles.  Warps issue in 51 of 100 cycles then, DRAM is at 32 %: the chain of a step
 // sets the time, of which no link was measured by itself.
 //
 // The tensor cores drop what lies below an accumulator's last bit, towards zero: logits lose 3e-6 of their size at d = 4096.  Parts of

@@ -53,7 +53,7 @@ struct W4LogitsParams : LogitTiles {
   bool half_last;          // the last one has 64 at most
   bool few;                // launch_w4_few: only the sizes, buffers and strides of the tiles' part are used
 };
-// Tokens that go through `w4_few`.  128256 x 4096, us, few / tiles: one token 62 / 104, 16 80 / 105, 17 128 / 105; 151936 x 2048
+// Tokens that go through `w4_few`.  128256 x 4096, us, few / tiles: one token 62 / 104, 16 84 / 105, 17 128 / 105; 151936 x 2048
 // 43 / 72, 55 / 72, 74 / 73.  (Of 3000 ids, where the tiles are fewer than the pairs, 25 / 20 at four tokens, 29 / 21 at 16.)
 constexpr int kW4Few = 16;
 constexpr int kW4FewIds = 32;  // ids of a warp
